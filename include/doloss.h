@@ -452,6 +452,96 @@ do_status do_rem_allocate(const double *loads, const double *expert_tokens,
                           int32_t *placed_receiver, double *placed_tokens, int32_t *n_placed,
                           double *loads_out);
 
+/* ------------------------------------------------------------------ experts
+ *
+ * The experts of one MoE layer on the dispatch order of do_routing: R = T k
+ * routed rows grouped by expert, rows [R] (the token of each), offsets [E+1] and
+ * pos [T][k] of one of its L problems.  Weights are bf16 (uint16 bit patterns):
+ * W1 [E][2F][H], the F gate rows before the F up rows, and W2 [E][H][F].
+ *  - Every matrix is dense, row-major and 16-byte aligned; its columns are a
+ *    multiple of 8 (F, where it is named, of 16) and at most 2^20; E <= 1024.
+ *    Other sizes return DO_ERR_UNSUPPORTED.
+ *  - Groups may be empty or of any length.  offsets is read as given, clipped to
+ *    [0, R]; routed rows at or past offsets[E] are not written.
+ *  - Products run on the tensor cores or the ALU with bf16 operands, fp32
+ *    accumulation and one rounding of the result; results are identical run to run.
+ *  - A NaN or an infinity in a row of one expert, or in an expert without rows,
+ *    does not reach the results of others.
+ *  - status_flags (256-byte aligned device memory whose first int32 is zero before
+ *    its first use, may be NULL): bit 1 (a bounded device wait ran out) and bit 2
+ *    (a row or position outside its matrix, counted as a row of zeros or left out)
+ *    are ORed into it; do_device_status reads and clears it.
+ *  - Asynchronous on `stream`. */
+
+/* The up projection with its activation, z = W1_e x[rows[r]] (fp32):
+ *   act [R][F] bf16, act[r][f] = silu(z[f]) z[F + f], silu(g) = g / (1 + e^-g)
+ * and, with codes and exponents (both or neither), z itself kept in 8 bits for
+ * the backward pass: codes [R][2F] int8 in [-127, 127] and exponents [R][2F/16]
+ * uint8, the value of a code being code * 2^(e - 127) with e the exponent of its
+ * block of 16 columns: the least e >= 1 with max |z| <= 127 * 2^(e - 127), codes
+ * rounded to nearest even; e = 255 stands for a block of NaNs (it held a NaN or
+ * an infinity).  An error of at most half a step, 2^-7 of the block's largest
+ * value, and 1.0625 bytes a value.
+ * X [T][H] bf16; rows NULL: routed row r reads X[r] (T >= R). */
+do_status do_expert_up(const void *X, const void *W1, const int32_t *rows, const int32_t *offsets,
+                       int64_t T, int32_t H, int32_t F, int32_t E, int64_t R, void *act,
+                       void *codes, void *exponents, int32_t *status_flags, void *stream);
+
+/* values [rows][cols] bf16 of an 8-bit checkpoint (exact: codes have 7 bits). */
+do_status do_checkpoint_values(const void *codes, const void *exponents, int64_t rows,
+                               int32_t cols, void *values, void *stream);
+
+/* Y [R][N] bf16, Y[r] = W_e A[rows[r]] (transposed = 0: W [E][N][K]) or W_e^T
+ * A[rows[r]] (transposed = 1: W [E][K][N], the gradient of the former's input).
+ * A [T][K] bf16; rows NULL: routed row r reads A[r] (T >= R). */
+do_status do_grouped_matmul(const void *A, const void *W, const int32_t *rows,
+                            const int32_t *offsets, int64_t T, int32_t K, int32_t N, int32_t E,
+                            int64_t R, int32_t transposed, void *Y, int32_t *status_flags,
+                            void *stream);
+
+/* do_grouped_matmul on rows A [T k][K] in dispatch order, and the sum of each
+ * token's k rows: out [T][N] bf16 = sum_q weights[t][q] Y[pos[t][q]] in fp32
+ * (weights [T][k] fp32; NULL: one each, as the gradient of a layer's input
+ * wants).  A pos outside [0, offsets[E]) is left out.  workspace:
+ * do_grouped_matmul_join_workspace_size bytes, 256-byte aligned, of any content
+ * (it holds Y); none of it is read by a later call. */
+do_status do_grouped_matmul_join(const void *A, const void *W, const int32_t *offsets,
+                                 const int32_t *pos, const float *weights, int64_t T, int32_t k,
+                                 int32_t K, int32_t N, int32_t E, int32_t transposed, void *out,
+                                 int32_t *status_flags, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+size_t do_grouped_matmul_join_workspace_size(int64_t T, int32_t k, int32_t N);
+
+/* Backward of out[t] = sum_q w_tq W2_e act(z_r), r = pos[t][q], through the join,
+ * the down projection and the activation, for dout [T][H] bf16, with z as the
+ * 8-bit checkpoint of do_expert_up holds it.  With g_r = W2_e^T dout[rows[r]],
+ * s = sigma(z_gate) and a = z_gate s z_up:
+ *   dz [R][2F] bf16     gate: w g z_up s (1 + z_gate (1 - s)); up: w g z_gate s
+ *   act [R][F] bf16     w a, the operand of dW2 beside dout (so that neither the
+ *                       layer's rows of output nor their gradient are ever kept)
+ *   dcombine [T][k] fp32  sum_f g_r[f] a_r[f]
+ * workspace: do_expert_up_backward_workspace_size bytes, 256-byte aligned, of
+ * any content. */
+do_status do_expert_up_backward(const void *dout, const void *W2, const void *codes,
+                                const void *exponents, const float *combine, const int32_t *rows,
+                                const int32_t *offsets, const int32_t *pos, int64_t T, int32_t k,
+                                int32_t H, int32_t F, int32_t E, void *dz, void *act,
+                                float *dcombine, int32_t *status_flags, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+size_t do_expert_up_backward_workspace_size(int64_t T, int32_t k, int32_t F);
+
+/* Weight gradients: dW [E][M][N] fp32, dW[e] = sum over the expert's routed rows r
+ * of P[p_rows[r]]^T Q[q_rows[r]] (P [Tp][M], Q [Tq][N] bf16; p_rows or q_rows
+ * NULL: r itself); zero for an expert without rows.  accumulate = 1 adds it to dW
+ * instead (each entry once). */
+do_status do_grouped_weight_grad(const void *P, const void *Q, const int32_t *p_rows,
+                                 const int32_t *q_rows, const int32_t *offsets, int64_t Tp,
+                                 int64_t Tq, int32_t M, int32_t N, int32_t E, int64_t R,
+                                 int32_t accumulate, float *dW, int32_t *status_flags,
+                                 void *stream);
+
 /* A static description of a status code. */
 const char *do_status_string(int32_t status);
 

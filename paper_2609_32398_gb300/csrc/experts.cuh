@@ -1,0 +1,108 @@
+// Internal declarations of the expert operators (experts.cu holds their C ABI):
+// the products of an MoE layer's experts on the router's dispatch order.
+//
+// Routed rows r = 0 .. R-1 are grouped by expert, offsets[e] .. offsets[e+1]
+// belonging to expert e; the matrix rows they read are rows[r] (gathered) or r.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "dol_internal.cuh"
+
+namespace dol {
+
+typedef __nv_bfloat16 bf16;
+
+// Values that share one exponent byte in an 8-bit checkpoint.
+constexpr int kQBlock = 16;
+
+enum ProductMode {
+    kProductPlain = 0,   // Y[r][n] = sum_k A[r][k] W[n][k]
+    kProductUp = 1,      // act[r][f] = silu(z[f]) z[F + f], and z in 8 bits
+    kProductUpGrad = 2,  // the gradient of kProductUp through W2 (its values in 8 bits)
+};
+
+struct ProductArgs {
+    const bf16 *A;         // [a_rows][K]
+    int64_t a_rows;
+    const int *rows;       // [R] or null: row r reads A[rows[r]] or A[r]
+    const bf16 *W;         // [E][N][K], or [E][K][N] when transposed
+    const int *offsets;    // [E + 1]
+    int64_t R;
+    int K, N, E;           // kProductUp: N = 2 F weight rows
+    bool transposed;
+    bf16 *out;             // plain: Y [R][N]; up: act [R][F]; up_grad: w act [R][F]
+    int8_t *codes;         // up: written (may be null); up_grad: read  [R][2 F]
+    uint8_t *exponents;    //                                           [R][2 F / 16]
+    bf16 *dz;              // up_grad: [R][2 F]
+    const float *row_weight;  // up_grad: [R]
+    float *strips;         // up_grad: [ceil(F / 32)][R], sums of g act over 32 columns
+    int *status;
+};
+
+cudaError_t launch_product(ProductMode mode, const ProductArgs &a, cudaStream_t s);
+
+struct WeightGradArgs {
+    const bf16 *P;  // [p_count][M]
+    const bf16 *Q;  // [q_count][N]
+    int64_t p_count, q_count;
+    const int *p_rows, *q_rows;  // [R] or null
+    const int *offsets;
+    int64_t R;
+    int M, N, E;
+    bool accumulate;
+    float *dW;  // [E][M][N]
+    int *status;
+};
+
+cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s);
+
+// out[t][n] = sum_q weights[t][q] Y[pos[t][q]][n] (weights null: all one) in fp32,
+// rounded once.  A pos outside [0, offsets[E]) is left out and recorded.
+cudaError_t launch_join(const bf16 *Y, const int *pos, const float *weights, const int *offsets,
+                        int64_t T, int k, int N, int E, bf16 *out, int *status, cudaStream_t s);
+// row_weight[pos[t][q]] = combine[t][q]
+cudaError_t launch_row_weights(const float *combine, const int *pos, int64_t R, float *row_weight,
+                               int *status, cudaStream_t s);
+// dcombine[t][q] = sum over the strips of strips[.][pos[t][q]], in order
+cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos, const int *offsets,
+                              int E, int64_t R, float *dcombine, cudaStream_t s);
+cudaError_t launch_checkpoint_values(const int8_t *codes, const uint8_t *exponents, int64_t rows,
+                                     int cols, bf16 *values, cudaStream_t s);
+
+// ---------------------------------------------------------------- device helpers
+
+// 8-bit checkpoint of a block of 16 values: codes in [-127, 127] times 2^(e - 127),
+// e the exponent byte.  e is the least in [1, 250] with max |v| <= 127 * 2^(e - 127):
+// for max |v| = m 2^x with m in [1, 2) that is x - 6 where m <= 127/64 and x - 5
+// otherwise, which the addition carries out on the float's bits.  A block with a NaN
+// or an infinity has e = 255 and stands for 16 NaNs.
+__device__ __forceinline__ int q8_exponent(float amax) {
+    const unsigned b = __float_as_uint(amax);
+    if (b >= 0x7f800000u) return 255;
+    const int e = (int)((b + 0x1ffffu) >> 23) - 6;
+    return e < 1 ? 1 : e;
+}
+// 2^(127 - e) and 2^(e - 127), both normal for 1 <= e <= 250; e = 255: 0 and NaN.
+__device__ __forceinline__ float q8_inverse(int e) {
+    return e == 255 ? 0.0f : __uint_as_float((unsigned)(254 - e) << 23);
+}
+__device__ __forceinline__ float q8_scale(int e) {
+    return __uint_as_float(e == 255 ? 0x7fc00000u : (unsigned)e << 23);
+}
+// round(v * inv), ties to even, as a byte: |v * inv| <= 127, so the sum with 1.5 * 2^23
+// holds the integer in its low bits.
+__device__ __forceinline__ unsigned q8_code(float v, float inv) {
+    return __float_as_uint(fmaf(v, inv, 12582912.0f)) & 0xffu;
+}
+// code of byte b (0..3) of a word as a float
+__device__ __forceinline__ float q8_value(unsigned word, int b) {
+    return (float)(int8_t)(word >> (8 * b));
+}
+
+// sigma(z) = 1 / (1 + e^-z): e^-z overflows to infinity below -88 and gives 0.
+__device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+
+}  // namespace dol

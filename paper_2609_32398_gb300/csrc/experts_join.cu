@@ -1,0 +1,132 @@
+// The small kernels of the expert operators: the weighted join of a token's k
+// routed rows, the combine weights by row, their gradient from the strip sums,
+// and the values of an 8-bit checkpoint.  All are bound by memory (the join and
+// the values) or by their launch (the other two).
+#include "experts.cuh"
+
+namespace dol {
+namespace {
+
+__device__ __forceinline__ void add8(float (&acc)[8], uint4 v, float w) {
+    const unsigned u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        acc[2 * i] = fmaf(w, __uint_as_float(u[i] << 16), acc[2 * i]);
+        acc[2 * i + 1] = fmaf(w, __uint_as_float(u[i] & 0xffff0000u), acc[2 * i + 1]);
+    }
+}
+
+__device__ __forceinline__ unsigned pack2(float lo, float hi) {
+    __nv_bfloat162 p = __float22bfloat162_rn(make_float2(lo, hi));
+    return *reinterpret_cast<unsigned *>(&p);
+}
+
+// One thread per 8 columns of a token; its k rows are read as 16-byte pieces.
+// A choice that is left out adds nothing (its row is not read).
+__global__ void __launch_bounds__(256)
+join_kernel(const bf16 *__restrict__ Y, const int *__restrict__ pos, const float *__restrict__ weights,
+            const int *__restrict__ offsets, int64_t T, int k, int N, int E, bf16 *__restrict__ out,
+            int *status) {
+    const int n8 = N / 8;
+    const int limit = offsets[E];
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < T * n8; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / n8;
+        const int c = (int)(i - t * n8);
+        float acc[8] = {};
+        for (int q0 = 0; q0 < k; q0 += 8) {
+            uint4 v[8];
+            float w[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                v[q] = make_uint4(0, 0, 0, 0);
+                w[q] = 0.0f;
+                if (q0 + q < k) {
+                    const int p = __ldg(pos + t * k + q0 + q);
+                    if (p >= 0 && p < limit && p < T * k) {
+                        v[q] = __ldg(reinterpret_cast<const uint4 *>(Y + (int64_t)p * N) + c);
+                        w[q] = weights ? __ldg(weights + t * k + q0 + q) : 1.0f;
+                    } else if (status) {
+                        atomicOr(status, kDevBadId);
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q0 + q < k) add8(acc, v[q], w[q]);
+        }
+        reinterpret_cast<uint4 *>(out + t * N)[c] = make_uint4(pack2(acc[0], acc[1]), pack2(acc[2], acc[3]),
+                                                               pack2(acc[4], acc[5]), pack2(acc[6], acc[7]));
+    }
+}
+
+__global__ void row_weights_kernel(const float *__restrict__ combine, const int *__restrict__ pos, int64_t R,
+                                   float *__restrict__ row_weight, int *status) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= R) return;
+    const int p = pos[i];
+    if (p >= 0 && p < R) row_weight[p] = combine[i];
+    else if (status) atomicOr(status, kDevBadId);
+}
+
+__global__ void strip_sums_kernel(const float *__restrict__ strips, int n, const int *__restrict__ pos,
+                                  const int *__restrict__ offsets, int E, int64_t R, float *__restrict__ dcombine) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= R) return;
+    const int p = pos[i];
+    float s = 0.0f;
+    if (p >= 0 && p < R && p < offsets[E])
+        for (int j = 0; j < n; ++j) s += strips[(int64_t)j * R + p];
+    dcombine[i] = s;
+}
+
+// One thread per block of 16 codes: 16 bytes and an exponent in, 32 bytes out.
+__global__ void __launch_bounds__(256)
+checkpoint_values_kernel(const uint4 *__restrict__ codes, const uint8_t *__restrict__ exponents, int64_t blocks,
+                         uint4 *__restrict__ values) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < blocks; i += (int64_t)gridDim.x * 256) {
+        const uint4 c = __ldg(codes + i);
+        const float s = q8_scale(__ldg(exponents + i));
+        const unsigned u[4] = {c.x, c.y, c.z, c.w};
+        unsigned o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            o[j] = pack2(q8_value(u[j / 2], 2 * (j & 1)) * s, q8_value(u[j / 2], 2 * (j & 1) + 1) * s);
+        values[2 * i] = make_uint4(o[0], o[1], o[2], o[3]);
+        values[2 * i + 1] = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+}
+
+unsigned blocks_of(int64_t n, int64_t most) {
+    const int64_t b = (n + 255) / 256;
+    return (unsigned)(b < most ? b : most);
+}
+
+}  // namespace
+
+cudaError_t launch_join(const bf16 *Y, const int *pos, const float *weights, const int *offsets, int64_t T,
+                        int k, int N, int E, bf16 *out, int *status, cudaStream_t s) {
+    join_kernel<<<blocks_of(T * (N / 8), 1 << 20), 256, 0, s>>>(Y, pos, weights, offsets, T, k, N, E, out, status);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_row_weights(const float *combine, const int *pos, int64_t R, float *row_weight, int *status,
+                               cudaStream_t s) {
+    row_weights_kernel<<<(unsigned)((R + 255) / 256), 256, 0, s>>>(combine, pos, R, row_weight, status);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos, const int *offsets, int E,
+                              int64_t R, float *dcombine, cudaStream_t s) {
+    strip_sums_kernel<<<(unsigned)((R + 255) / 256), 256, 0, s>>>(strips, n_strips, pos, offsets, E, R, dcombine);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_checkpoint_values(const int8_t *codes, const uint8_t *exponents, int64_t rows, int cols,
+                                     bf16 *values, cudaStream_t s) {
+    const int64_t n = rows * (cols / kQBlock);
+    checkpoint_values_kernel<<<blocks_of(n, 1 << 20), 256, 0, s>>>(reinterpret_cast<const uint4 *>(codes), exponents,
+                                                                   n, reinterpret_cast<uint4 *>(values));
+    return cudaGetLastError();
+}
+
+}  // namespace dol

@@ -62,6 +62,17 @@ EXPORTS = {
     "do_router_forward_backward": (["p", "p", "i64", "i32", "i32", "i32", "i32", "i32", "f32", "p",
                                     "p", "p", "p", "p", "p", "p", "p", "sz", "p"], "i32"),
     "do_rem_allocate": (["p", "p", "p", "i32", "i32", "i32", "p", "p", "p", "p", "p", "p"], "i32"),
+    "do_expert_up": (["p", "p", "p", "p", "i64", "i32", "i32", "i32", "i64", "p", "p", "p", "p", "p"], "i32"),
+    "do_checkpoint_values": (["p", "p", "i64", "i32", "p", "p"], "i32"),
+    "do_grouped_matmul": (["p", "p", "p", "p", "i64", "i32", "i32", "i32", "i64", "i32", "p", "p", "p"], "i32"),
+    "do_grouped_matmul_join_workspace_size": (["i64", "i32", "i32"], "sz"),
+    "do_grouped_matmul_join": (["p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i32", "i32", "p", "p", "p",
+                                "sz", "p"], "i32"),
+    "do_expert_up_backward_workspace_size": (["i64", "i32", "i32"], "sz"),
+    "do_expert_up_backward": (["p", "p", "p", "p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i32", "p", "p",
+                               "p", "p", "p", "sz", "p"], "i32"),
+    "do_grouped_weight_grad": (["p", "p", "p", "p", "p", "i64", "i64", "i32", "i32", "i32", "i64", "i32", "p", "p",
+                                "p"], "i32"),
 }
 
 _CT = {"p": ctypes.c_void_p, "i64": ctypes.c_int64, "i32": ctypes.c_int32,
