@@ -1,0 +1,435 @@
+// Products of each expert's weights with its routed rows on the tcgen05 tensor
+// cores (kind::f16: bf16 operands, fp32 accumulation):
+//
+//   D[m][r] = sum_k W_e[m][k] A[row(r)][k]          m: weight rows, r: routed rows
+//
+// with three epilogues: the rows as they are, the SwiGLU activation with its 8-bit
+// checkpoint, and the gradient of that.  The weights are the M side: their sizes
+// are fixed and fill tiles of 256, while the ragged side, the rows of an expert,
+// is the N side, whose width may be any multiple of 16.  An expert's n rows are
+// ceil(n / 256) tiles of equal width, so that a ragged group wastes at most 15
+// columns a tile (a fixed 256-row tile would waste 128 rows an expert on average)
+// and a decode step's groups of one or two rows take tiles 16 wide.
+//
+// A persistent CTA pair (cta_group::2, 256 weight rows x up to 256 routed rows in
+// 2 x 256 TMEM columns, so that one tile's epilogue runs under the next tile's
+// products) takes tiles in a fixed order.  Per 64-wide step of k each CTA loads
+// its 128 weight rows (one box, or two where the weights are read through their
+// other side) and half of the routed rows, which are gathered four at a time by
+// their row ids (no permuted copy of the tokens exists; rows past the group's end
+// name no row of the matrix and read as zeros).
+//
+// Warps: 0 loads, 1 issues the MMAs (first CTA), 2-9 epilogue.  A TMEM lane is a
+// weight row and a register a routed row, so each epilogue warp turns 32 x 32
+// blocks in shared memory (16-byte pieces xor-swizzled: no bank conflicts) and
+// then has 32 columns of one routed row in a thread, where the activation, the
+// blocks' exponents and the sums over columns need no other thread.
+//
+// Every wait is bounded; one that runs out records kDevTimeout.
+#include <cstdint>
+
+#include "experts_mma.cuh"
+
+namespace dol {
+namespace {
+
+constexpr int kTileN = 256;               // routed rows of a tile at most
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = (2 + kEpiWarps) * 32;
+constexpr uint32_t kABytes = 128 * 128;   // a CTA's weight rows of one step
+constexpr int kMaxStages = 12;
+constexpr uint32_t kTurn = 32 * 128;      // an epilogue warp's block
+constexpr uint32_t kSmemLimit = 232448;
+
+struct PairArgs {
+    ProductArgs p;
+    int m_tiles;    // tiles of 256 weight rows (up: of 128 gate rows and their up rows)
+    int stages;     // of the ring
+    uint32_t b_bytes;  // room for a CTA's routed rows of one step
+};
+
+// Shared memory: ring [stages][weights | rows], turn blocks [8][4 KB], the first
+// tile of each expert [E + 1], barriers.
+__host__ __device__ inline uint32_t off_turn(int stages, uint32_t b_bytes) { return stages * (kABytes + b_bytes); }
+
+struct Tile {
+    int e, m, r0, n, width;  // expert, weight tile, first routed row, rows, MMA width
+};
+
+struct Schedule {
+    const int *first;    // shared [E + 1]
+    const int *offsets;
+    int E, m_tiles;
+    int64_t R;
+
+    __device__ Tile at(int t) const {
+        int lo = 0, hi = E;  // first[lo] <= t < first[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        Tile o;
+        o.e = lo;
+        const int a = max(0, min(__ldg(offsets + lo), (int)R));
+        const int cnt = max(a, min(__ldg(offsets + lo + 1), (int)R)) - a;
+        const int nt = (cnt + kTileN - 1) / kTileN;
+        const int i = t - first[lo];
+        const int j = i / m_tiles;
+        o.m = i - j * m_tiles;
+        const int w = (((cnt + nt - 1) / nt) + 15) & ~15;
+        o.r0 = a + j * w;
+        o.n = min(w, a + cnt - o.r0);
+        o.width = (o.n + 15) & ~15;
+        return o;
+    }
+};
+
+__device__ __forceinline__ unsigned pack2(float lo, float hi) {
+    __nv_bfloat162 p = __float22bfloat162_rn(make_float2(lo, hi));
+    return *reinterpret_cast<unsigned *>(&p);
+}
+
+__device__ __forceinline__ void store8(bf16 *dst, const float *v) {
+    *reinterpret_cast<uint4 *>(dst) =
+        make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+}
+
+// 16 values to their codes and exponent.
+__device__ __forceinline__ uint4 quantise16(const float *v, int *exponent) {
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+    const int e = q8_exponent(__uint_as_float(top));
+    const float inv = q8_inverse(e);
+    unsigned w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        w[j] = q8_code(v[4 * j], inv) | q8_code(v[4 * j + 1], inv) << 8 | q8_code(v[4 * j + 2], inv) << 16 |
+               q8_code(v[4 * j + 3], inv) << 24;
+    if (e == 255) w[0] = w[1] = w[2] = w[3] = 0u;
+    *exponent = e;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// One routed row's 32 values of the tile.  c0: the first weight row of the warp's 32
+// (plain, up_grad), or the first of its 16 gate rows (up).
+template <int kMode>
+__device__ __forceinline__ void finish_row(const ProductArgs &p, int64_t r, int c0, float (&v)[32]) {
+    if (kMode == kProductPlain) {
+        bf16 *dst = p.out + r * p.N + c0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c0 + 8 * j < p.N) store8(dst + 8 * j, v + 8 * j);
+    } else if (kMode == kProductUp) {
+        const int F = p.N / 2;
+        if (c0 >= F) return;
+        if (p.codes) {
+            int eg, eu;
+            const uint4 g = quantise16(v, &eg), u = quantise16(v + 16, &eu);
+            const int64_t at = r * p.N + c0;
+            *reinterpret_cast<uint4 *>(p.codes + at) = g;
+            *reinterpret_cast<uint4 *>(p.codes + at + F) = u;
+            p.exponents[at / kQBlock] = (uint8_t)eg;
+            p.exponents[(at + F) / kQBlock] = (uint8_t)eu;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = v[i] * sigmoid_f(v[i]) * v[16 + i];
+        bf16 *dst = p.out + r * F + c0;
+        store8(dst, v);
+        store8(dst + 8, v + 8);
+    } else {
+        const int F = p.N;
+        const float w = __ldg(p.row_weight + r);
+        float sum = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = c0 + 16 * h;
+            if (c >= F) break;
+            const int64_t cg = r * 2 * F + c, cu = cg + F;
+            const uint4 qg = __ldg(reinterpret_cast<const uint4 *>(p.codes + cg));
+            const uint4 qu = __ldg(reinterpret_cast<const uint4 *>(p.codes + cu));
+            const float sg = q8_scale(__ldg(p.exponents + cg / kQBlock));
+            const float su = q8_scale(__ldg(p.exponents + cu / kQBlock));
+            const unsigned ug[4] = {qg.x, qg.y, qg.z, qg.w}, uu[4] = {qu.x, qu.y, qu.z, qu.w};
+            float dg[16], du[16], act[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float zg = q8_value(ug[i / 4], i & 3) * sg, zu = q8_value(uu[i / 4], i & 3) * su;
+                const float s = sigmoid_f(zg), g = v[16 * h + i];
+                const float silu = zg * s, a = silu * zu, gw = g * w;
+                sum = fmaf(g, a, sum);
+                du[i] = gw * silu;
+                dg[i] = gw * zu * fmaf(silu, 1.0f - s, s);
+                act[i] = a * w;
+            }
+            store8(p.dz + cg, dg);
+            store8(p.dz + cg + 8, dg + 8);
+            store8(p.dz + cu, du);
+            store8(p.dz + cu + 8, du + 8);
+            store8(p.out + r * F + c, act);
+            store8(p.out + r * F + c + 8, act + 8);
+        }
+        if (c0 < F) p.strips[(int64_t)(c0 / 32) * p.R + r] = sum;
+    }
+}
+
+template <int kMode>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const PairArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = smem_align<1024>(smem_raw);
+    const ProductArgs &p = a.p;
+    const int E = p.E, stages = a.stages;
+    const uint32_t stage_bytes = kABytes + a.b_bytes;
+    unsigned char *turn = smem + off_turn(stages, a.b_bytes);
+    int *first = reinterpret_cast<int *>(turn + kEpiWarps * kTurn);
+    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int s_abort, s_part[kThreads / 32];
+    volatile int *abort = &s_abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < stages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&acc_full[i], 1);
+            mbar_init(&acc_empty[i], 2 * kEpiWarps);
+        }
+        mbar_init(&drain, 1);
+        s_abort = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&wmap);
+        prefetch_tensormap(&amap);
+    }
+    if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
+    // the first tile of each expert: a scan of ceil(n / 256) m_tiles over the experts
+    int carry = 0;
+    for (int base = 0; base < E; base += kThreads) {
+        const int e = base + (int)threadIdx.x;
+        int c = 0;
+        if (e < E) {
+            const int lo = max(0, min(__ldg(p.offsets + e), (int)p.R));
+            const int hi = max(lo, min(__ldg(p.offsets + e + 1), (int)p.R));
+            c = (hi - lo + kTileN - 1) / kTileN * a.m_tiles;
+        }
+        int x = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(kFull, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) s_part[warp] = x;
+        __syncthreads();
+        int before = carry, all = 0;
+        for (int i = 0; i < kThreads / 32; ++i) {
+            if (i < warp) before += s_part[i];
+            all += s_part[i];
+        }
+        if (e < E) first[e] = before + x - c;
+        carry += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) first[E] = carry;
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int tiles = carry, pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
+    const int steps = (p.K + 63) / 64;
+    const Schedule sched{first, p.offsets, E, a.m_tiles, p.R};
+    if (warp == 0) {
+        // ---------------------------------------------------------- producer
+        uint32_t bars[1];
+        bars[0] = map_to_rank(&full[0], 0);
+        int it = 0;
+        bool good = true;
+        const int none = (int)p.a_rows;
+        for (int t = pair; good && t < tiles; t += pairs) {
+            const Tile tl = sched.at(t);
+            const int half = tl.width / 2;  // this CTA's routed rows: [rank half, + half)
+            const bool gathers = 4 * lane < half;
+            int4 id = make_int4(none, none, none, none);
+            if (gathers) {
+                int *ids = &id.x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = (int)rank * half + 4 * lane + j;
+                    if (i < tl.n) {
+                        const int r = tl.r0 + i;
+                        const int src = p.rows ? __ldg(p.rows + r) : r;
+                        if (src >= 0 && src < none) ids[j] = src;
+                        else if (p.status) atomicOr(p.status, kDevBadId);
+                    }
+                }
+            }
+            const uint32_t bytes = 2u * (kABytes + (uint32_t)half * 128u);
+            for (int k = 0; k < steps; ++k, ++it) {
+                const int s = it % stages;
+                if (it >= stages) {
+                    good = pair_wait(&empty[s], (uint32_t)(it / stages - 1) & 1u, p.status, abort);
+                    good = __all_sync(kFull, good);
+                    if (!good) break;
+                }
+                unsigned char *st = smem + (size_t)s * stage_bytes;
+                const uint32_t bar = bars[0] + 8u * (uint32_t)s;
+                if (lane == 0) {
+                    if (rank == 0) mbar_arrive_expect_tx(&full[s], bytes);
+                    if (kMode == kProductUp) {
+                        pair_load_5d(st, &wmap, 64 * k, 0, 0, tl.m * 8 + (int)rank * 4, tl.e, bar);
+                    } else if (p.transposed) {
+                        const int m0 = tl.m * 256 + (int)rank * 128;
+                        pair_load_3d(st, &wmap, m0, 64 * k, tl.e, bar);
+                        pair_load_3d(st + kABytes / 2, &wmap, m0 + 64, 64 * k, tl.e, bar);
+                    } else {
+                        pair_load_3d(st, &wmap, 64 * k, tl.m * 256 + (int)rank * 128, tl.e, bar);
+                    }
+                }
+                __syncwarp();
+                if (gathers) pair_gather4(st + kABytes + lane * 512, &amap, 64 * k, id, bar);
+            }
+        }
+        // a run that gave up: the loads in flight complete before the CTA ends (in the
+        // usual case the MMAs waited for them)
+        if (!good && rank == 0 && lane == 0)
+            for (int i = it > stages ? it - stages : 0; i < it; ++i)
+                mbar_wait(&full[i % stages], (uint32_t)(i / stages) & 1u, p.status);
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------------------------------------------------- MMA issuer
+        if (rank == 0 && lane == 0) {
+            int it = 0, done = 0;
+            bool good = true;
+            const uint32_t base = smem_u32(smem);
+            for (int t = pair; good && t < tiles; t += pairs, ++done) {
+                const Tile tl = sched.at(t);
+                const int buf = done & 1;
+                if (done >= 2) good = pair_wait(&acc_empty[buf], (uint32_t)((done >> 1) - 1) & 1u, p.status, abort);
+                if (!good) break;
+                tc_fence_after();
+                const uint32_t d = tmem + (uint32_t)(buf * 256);
+                const uint32_t idesc = pair_idesc(tl.width, p.transposed, false);
+                for (int k = 0; k < steps; ++k, ++it) {
+                    const int s = it % stages;
+                    good = pair_wait(&full[s], (uint32_t)(it / stages) & 1u, p.status, abort);
+                    if (!good) break;
+                    tc_fence_after();
+                    const uint32_t sa = base + (uint32_t)s * stage_bytes, sb = sa + kABytes;
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) {
+                        const uint64_t ad = p.transposed ? desc_mn_sw128(sa + kk * 2048, kABytes / 2)
+                                                         : umma_desc_sw128(sa + kk * 32);
+                        pair_mma(d, ad, umma_desc_sw128(sb + kk * 32), idesc, (k | kk) != 0 ? 1u : 0u);
+                    }
+                    pair_commit(&empty[s]);
+                }
+                if (good) pair_commit(&acc_full[buf]);
+            }
+            if (!good) {  // the tensor cores are done with shared memory before the CTA ends
+                pair_commit(&drain);
+                mbar_wait(&drain, 0u, p.status);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------- epilogue
+        const int quad = warp & 3, part = (warp - 2) >> 2;
+        unsigned char *mine = turn + (warp - 2) * kTurn;
+        const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
+        int done = 0;
+        for (int t = pair; t < tiles; t += pairs, ++done) {
+            const Tile tl = sched.at(t);
+            const int buf = done & 1;
+            const bool good = __all_sync(kFull, pair_wait(&acc_full[buf], (uint32_t)(done >> 1) & 1u, p.status, abort));
+            if (!good) break;
+            tc_fence_after();
+            const int c0 = kMode == kProductUp ? tl.m * 128 + (int)rank * 64 + quad * 16
+                                               : tl.m * 256 + (int)rank * 128 + quad * 32;
+            const uint32_t col = tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)(buf * 256);
+            for (int n0 = 32 * part; n0 < tl.n; n0 += 64) {
+                uint32_t r[32];
+                tmem_ld32(col + (uint32_t)n0, r);
+                tmem_wait_ld();
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    *reinterpret_cast<uint32_t *>(mine + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) = r[i];
+                __syncwarp();
+                float v[32];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float4 f = *reinterpret_cast<const float4 *>(mine + lane * 128 + ((j ^ (lane & 7)) << 4));
+                    v[4 * j] = f.x;
+                    v[4 * j + 1] = f.y;
+                    v[4 * j + 2] = f.z;
+                    v[4 * j + 3] = f.w;
+                }
+                if (n0 + lane < tl.n) finish_row<kMode>(p, tl.r0 + n0 + lane, c0, v);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(empty_addr + 8u * (uint32_t)buf);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    if (warp == 1) pair_tmem_dealloc(tmem, 512);
+}
+
+int sm_count() {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return 0;
+    return n;
+}
+
+template <int kMode>
+cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
+    PairArgs a = {};
+    a.p = p;
+    CUtensorMap wmap, amap;
+    bool ok = encode_gather_map(&amap, p.A, (uint64_t)p.a_rows, (uint64_t)p.K);
+    if (kMode == kProductUp) {
+        a.m_tiles = (p.N / 2 + 127) / 128;
+        ok = ok && encode_gate_up_map(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.N / 2, (uint64_t)p.K);
+    } else {
+        a.m_tiles = (p.N + 255) / 256;
+        ok = ok && (p.transposed ? encode_tensor_map_3d_bf16(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.K, (uint64_t)p.N, 64, 64)
+                                 : encode_tensor_map_3d_bf16(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.N, (uint64_t)p.K, 64, 128));
+    }
+    const int sms = sm_count();
+    if (!ok || sms < 2) return cudaErrorInvalidValue;
+    // a group has at most R rows, so that a step's routed rows fit a narrower ring
+    // (and more of it) in small calls
+    const int widest = (int)(p.R < kTileN ? (p.R + 15) / 16 * 16 : kTileN);
+    a.b_bytes = ((uint32_t)widest / 2 * 128 + 1023) / 1024 * 1024;
+    const uint32_t fixed = 1024 + kEpiWarps * kTurn + ((uint32_t)p.E + 1) * 4 + 2048;
+    a.stages = (int)((kSmemLimit - fixed) / (kABytes + a.b_bytes));
+    if (a.stages > kMaxStages) a.stages = kMaxStages;
+    const uint32_t smem = 1024 + off_turn(a.stages, a.b_bytes) + kEpiWarps * kTurn + ((uint32_t)p.E + 1) * 4;
+    cudaError_t e = ensure_smem_limit<product_kernel<kMode>>(kSmemLimit - 2048);
+    if (e != cudaSuccess) return e;
+    // at most R groups have rows, and a group of n rows has n / 256 + 1 tiles at most
+    const int64_t groups = min64(p.R, p.E);
+    const int64_t most = (p.R / kTileN + groups) * a.m_tiles;
+    const int64_t pairs = min64(most, sms / 2);
+    product_kernel<kMode><<<dim3((unsigned)(2 * pairs)), kThreads, smem, s>>>(wmap, amap, a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_product(ProductMode mode, const ProductArgs &a, cudaStream_t s) {
+    if (mode == kProductPlain) return launch<kProductPlain>(a, s);
+    if (mode == kProductUp) return launch<kProductUp>(a, s);
+    return launch<kProductUpGrad>(a, s);
+}
+
+}  // namespace dol
