@@ -1,6 +1,6 @@
 // PTX of the CTA-pair kernels of the expert operators: thread-block clusters of
-// two, tcgen05 with cta_group::2 (one accumulator of 256 rows over two SMs) and
-// row-gathering TMA loads.
+// two, tcgen05 with cta_group::2 (one accumulator of 256 rows over two SMs), and
+// the copies that gather rows.
 #pragma once
 
 #include "experts.cuh"
@@ -76,14 +76,31 @@ __device__ __forceinline__ void pair_load_5d(void *dst, const CUtensorMap *map, 
         : "memory");
 }
 
-// Four rows of a matrix (64 columns from x on) into four consecutive 128-byte rows;
-// a row outside the matrix reads as zeros.
-__device__ __forceinline__ void pair_gather4(void *dst, const CUtensorMap *map, int x, int4 r, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.cta_group::2"
-        " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "r"(bar)
-        : "memory");
+// 16 bytes global -> shared, zeros where !in (nothing is read then).
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// Arrive on `bar` (one of its expected arrivals) when this thread's copies so far are done.
+__device__ __forceinline__ void cp_async_arrive(uint64_t *bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// The gathering warps of a CTA (kLoadWarps of them) write 16-byte pieces of rows
+// into the ring and leave each step's `landed` barrier to their copies; one thread
+// of another warp waits for it, makes the step visible to the tensor cores and
+// tells the pair's first CTA, so that the gathering warps run as far ahead as the
+// ring allows.  (Rows gathered by TMA, four a copy, took 85 to 100 cycles a copy of
+// 512 bytes, five times the products' time; gathering warps that announced their
+// own steps three steps late no less, as two of five stages were left to run ahead.)
+constexpr int kLoadWarps = 4;
+
+__device__ __forceinline__ bool announce(uint64_t *landed, uint32_t parity, uint32_t full_addr, int *status,
+                                         volatile int *abort) {
+    if (!pair_wait(landed, parity, status, abort)) return false;
+    fence_proxy_async_smem();
+    mbar_arrive_cluster(full_addr);
+    return true;
 }
 
 __device__ __forceinline__ void tma_reduce_add_3d(const CUtensorMap *map, const void *src, int x, int y, int z) {
@@ -138,8 +155,6 @@ __host__ __device__ constexpr uint32_t pair_idesc(int n, bool a_mn, bool b_mn) {
 }
 
 // Host: the pair kernels' tensor maps (128-byte swizzle, zero outside the tensor).
-// Rows of a bf16 matrix, gathered four at a time, 64 columns each.
-bool encode_gather_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols);
 // W1 [E][2F][H] as [E][F/16][2][16][H], box 1 x 4 x 2 x 16 x 64: 64 columns of 64
 // gate rows and their 64 up rows, 16 of each in turn.
 bool encode_gate_up_map(CUtensorMap *map, const void *base, uint64_t E, uint64_t F, uint64_t H);

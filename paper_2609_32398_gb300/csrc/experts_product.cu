@@ -14,12 +14,14 @@
 // A persistent CTA pair (cta_group::2, 256 weight rows x up to 256 routed rows in
 // 2 x 256 TMEM columns, so that one tile's epilogue runs under the next tile's
 // products) takes tiles in a fixed order.  Per 64-wide step of k each CTA loads
-// its 128 weight rows (one box, or two where the weights are read through their
-// other side) and half of the routed rows, which are gathered four at a time by
-// their row ids (no permuted copy of the tokens exists; rows past the group's end
-// name no row of the matrix and read as zeros).
+// its 128 weight rows by TMA (one box, or two where the weights are read through
+// their other side) and half of the routed rows: by TMA where they lie in dispatch
+// order, and gathered by their row ids in 16-byte pieces otherwise, so that no
+// permuted copy of the tokens exists.  What a tile holds past its group's end ends
+// in accumulator columns that nobody reads.
 //
-// Warps: 0 loads, 1 issues the MMAs (first CTA), 2-9 epilogue.  A TMEM lane is a
+// Warps: 0 TMA, 1 issues the MMAs (first CTA), then the epilogue's, and where rows
+// are gathered four that gather and one that announces their steps.  A TMEM lane is a
 // weight row and a register a routed row, so each epilogue warp turns 32 x 32
 // blocks in shared memory (16-byte pieces xor-swizzled: no bank conflicts) and
 // then has 32 columns of one routed row in a thread, where the activation, the
@@ -34,8 +36,13 @@ namespace dol {
 namespace {
 
 constexpr int kTileN = 256;               // routed rows of a tile at most
-constexpr int kEpiWarps = 8;
-constexpr int kThreads = (2 + kEpiWarps) * 32;
+// Epilogue warps: where rows are gathered a longer ring pays more than a faster
+// epilogue (16 KB of turn blocks instead of 32, six stages instead of five).
+__host__ __device__ constexpr int epi_warps(bool gather) { return gather ? 4 : 8; }
+__host__ __device__ constexpr int first_loader(bool gather) { return 2 + epi_warps(gather); }
+__host__ __device__ constexpr int threads_of(bool gather) {
+    return (first_loader(gather) + (gather ? kLoadWarps + 1 : 0)) * 32;
+}
 constexpr uint32_t kABytes = 128 * 128;   // a CTA's weight rows of one step
 constexpr int kMaxStages = 12;
 constexpr uint32_t kTurn = 32 * 128;      // an epilogue warp's block
@@ -46,9 +53,10 @@ struct PairArgs {
     int m_tiles;    // tiles of 256 weight rows (up: of 128 gate rows and their up rows)
     int stages;     // of the ring
     uint32_t b_bytes;  // room for a CTA's routed rows of one step
+    int box;        // routed rows of a TMA box (rows in dispatch order)
 };
 
-// Shared memory: ring [stages][weights | rows], turn blocks [8][4 KB], the first
+// Shared memory: ring [stages][weights | rows], turn blocks [warps][4 KB], the first
 // tile of each expert [E + 1], barriers.
 __host__ __device__ inline uint32_t off_turn(int stages, uint32_t b_bytes) { return stages * (kABytes + b_bytes); }
 
@@ -174,17 +182,19 @@ __device__ __forceinline__ void finish_row(const ProductArgs &p, int64_t r, int 
     }
 }
 
-template <int kMode>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+template <int kMode, bool kGather>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kGather), 1)
 product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const PairArgs a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_align<1024>(smem_raw);
+    constexpr int kEpiWarps = epi_warps(kGather), kFirstLoader = first_loader(kGather);
+    constexpr int kThreads = threads_of(kGather);
     const ProductArgs &p = a.p;
     const int E = p.E, stages = a.stages;
     const uint32_t stage_bytes = kABytes + a.b_bytes;
     unsigned char *turn = smem + off_turn(stages, a.b_bytes);
     int *first = reinterpret_cast<int *>(turn + kEpiWarps * kTurn);
-    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], acc_full[2], acc_empty[2], drain;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort, s_part[kThreads / 32];
     volatile int *abort = &s_abort;
@@ -192,8 +202,9 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < stages; ++i) {
-            mbar_init(&full[i], 1);
+            mbar_init(&full[i], kGather ? 3 : 1);
             mbar_init(&empty[i], 1);
+            mbar_init(&landed[i], 32 * kLoadWarps);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&acc_full[i], 1);
@@ -243,41 +254,24 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const int steps = (p.K + 63) / 64;
     const Schedule sched{first, p.offsets, E, a.m_tiles, p.R};
     if (warp == 0) {
-        // ---------------------------------------------------------- producer
-        uint32_t bars[1];
-        bars[0] = map_to_rank(&full[0], 0);
-        int it = 0;
-        bool good = true;
-        const int none = (int)p.a_rows;
-        for (int t = pair; good && t < tiles; t += pairs) {
-            const Tile tl = sched.at(t);
-            const int half = tl.width / 2;  // this CTA's routed rows: [rank half, + half)
-            const bool gathers = 4 * lane < half;
-            int4 id = make_int4(none, none, none, none);
-            if (gathers) {
-                int *ids = &id.x;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int i = (int)rank * half + 4 * lane + j;
-                    if (i < tl.n) {
-                        const int r = tl.r0 + i;
-                        const int src = p.rows ? __ldg(p.rows + r) : r;
-                        if (src >= 0 && src < none) ids[j] = src;
-                        else if (p.status) atomicOr(p.status, kDevBadId);
+        // ---------------------------------------------------------- TMA
+        if (lane == 0) {
+            const uint32_t bar0 = map_to_rank(&full[0], 0);
+            int it = 0;
+            bool good = true;
+            for (int t = pair; good && t < tiles; t += pairs) {
+                const Tile tl = sched.at(t);
+                const int half = tl.width / 2;  // this CTA's routed rows: [rank half, + half)
+                const int boxes = kGather ? 0 : (half + a.box - 1) / a.box;
+                const uint32_t bytes = 2u * (kABytes + (uint32_t)(boxes * a.box) * 128u);
+                for (int k = 0; k < steps; ++k, ++it) {
+                    const int s = it % stages;
+                    if (it >= stages) {
+                        good = pair_wait(&empty[s], (uint32_t)(it / stages - 1) & 1u, p.status, abort);
+                        if (!good) break;
                     }
-                }
-            }
-            const uint32_t bytes = 2u * (kABytes + (uint32_t)half * 128u);
-            for (int k = 0; k < steps; ++k, ++it) {
-                const int s = it % stages;
-                if (it >= stages) {
-                    good = pair_wait(&empty[s], (uint32_t)(it / stages - 1) & 1u, p.status, abort);
-                    good = __all_sync(kFull, good);
-                    if (!good) break;
-                }
-                unsigned char *st = smem + (size_t)s * stage_bytes;
-                const uint32_t bar = bars[0] + 8u * (uint32_t)s;
-                if (lane == 0) {
+                    unsigned char *st = smem + (size_t)s * stage_bytes;
+                    const uint32_t bar = bar0 + 8u * (uint32_t)s;
                     if (rank == 0) mbar_arrive_expect_tx(&full[s], bytes);
                     if (kMode == kProductUp) {
                         pair_load_5d(st, &wmap, 64 * k, 0, 0, tl.m * 8 + (int)rank * 4, tl.e, bar);
@@ -288,16 +282,74 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                     } else {
                         pair_load_3d(st, &wmap, 64 * k, tl.m * 256 + (int)rank * 128, tl.e, bar);
                     }
+                    for (int b = 0; b < boxes; ++b)
+                        pair_load_3d(st + kABytes + b * a.box * 128, &amap, 64 * k,
+                                     tl.r0 + (int)rank * half + b * a.box, 0, bar);
                 }
-                __syncwarp();
-                if (gathers) pair_gather4(st + kABytes + lane * 512, &amap, 64 * k, id, bar);
             }
+            // a run that gave up: the loads in flight complete before the CTA ends (in the
+            // usual case the MMAs waited for them)
+            if (!good && rank == 0)
+                for (int i = it > stages ? it - stages : 0; i < it; ++i)
+                    mbar_wait(&full[i % stages], (uint32_t)(i / stages) & 1u, p.status);
         }
-        // a run that gave up: the loads in flight complete before the CTA ends (in the
-        // usual case the MMAs waited for them)
-        if (!good && rank == 0 && lane == 0)
-            for (int i = it > stages ? it - stages : 0; i < it; ++i)
-                mbar_wait(&full[i % stages], (uint32_t)(i / stages) & 1u, p.status);
+        __syncwarp();
+    } else if (kGather && warp == kFirstLoader + kLoadWarps) {
+        // ---------------------------------------------------------- announce
+        if (lane == 0) {
+            const uint32_t full0 = map_to_rank(&full[0], 0);
+            int it = 0;
+            bool good = true;
+            for (int t = pair; good && t < tiles; t += pairs)
+                for (int k = 0; good && k < steps; ++k, ++it) {
+                    const int s = it % stages;
+                    good = announce(&landed[s], (uint32_t)(it / stages) & 1u, full0 + 8u * (uint32_t)s, p.status, abort);
+                }
+        }
+        __syncwarp();
+    } else if (kGather && warp >= kFirstLoader) {
+        // ---------------------------------------------------------- gather
+        // Eight lanes copy the 128 bytes of a row, a pass takes 16 rows.
+        {
+            const int i = (int)threadIdx.x - kFirstLoader * 32, piece = i & 7, row = i >> 3;
+            const uint32_t base = smem_u32(smem) + kABytes + (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4));
+            int it = 0;
+            bool good = true;
+            for (int t = pair; good && t < tiles; t += pairs) {
+                const Tile tl = sched.at(t);
+                const int half = tl.width / 2;
+                int src[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int x = row + 16 * j, n = (int)rank * half + x;
+                    src[j] = -1;
+                    if (x < half && n < tl.n) {
+                        const int id = __ldg(p.rows + tl.r0 + n);
+                        if (id >= 0 && id < p.a_rows) src[j] = id;
+                        else if (p.status) atomicOr(p.status, kDevBadId);
+                    }
+                }
+                for (int k = 0; k < steps; ++k, ++it) {
+                    const int s = it % stages;
+                    if (it >= stages) {
+                        good = pair_wait(&empty[s], (uint32_t)(it / stages - 1) & 1u, p.status, abort);
+                        good = __all_sync(kFull, good);
+                        if (!good) break;
+                    }
+                    const int c = 64 * k + 8 * piece;
+                    const uint32_t dst = base + (uint32_t)s * stage_bytes;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        if (row + 16 * j < half) {
+                            const bool in = src[j] >= 0 && c < p.K;
+                            cp_async16(dst + j * 2048, p.A + (in ? (int64_t)src[j] * p.K + c : 0), in);
+                        }
+                    }
+                    cp_async_arrive(&landed[s]);
+                }
+            }
+            cp_async_wait_all();
+        }
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
@@ -350,7 +402,7 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             const int c0 = kMode == kProductUp ? tl.m * 128 + (int)rank * 64 + quad * 16
                                                : tl.m * 256 + (int)rank * 128 + quad * 32;
             const uint32_t col = tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)(buf * 256);
-            for (int n0 = 32 * part; n0 < tl.n; n0 += 64) {
+            for (int n0 = 32 * part; n0 < tl.n; n0 += 8 * kEpiWarps) {
                 uint32_t r[32];
                 tmem_ld32(col + (uint32_t)n0, r);
                 tmem_wait_ld();
@@ -390,12 +442,13 @@ int sm_count() {
     return n;
 }
 
-template <int kMode>
+template <int kMode, bool kGather>
 cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
+    constexpr int kEpiWarps = epi_warps(kGather);
     PairArgs a = {};
     a.p = p;
     CUtensorMap wmap, amap;
-    bool ok = encode_gather_map(&amap, p.A, (uint64_t)p.a_rows, (uint64_t)p.K);
+    bool ok = true;
     if (kMode == kProductUp) {
         a.m_tiles = (p.N / 2 + 127) / 128;
         ok = ok && encode_gate_up_map(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.N / 2, (uint64_t)p.K);
@@ -405,31 +458,33 @@ cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
                                  : encode_tensor_map_3d_bf16(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.N, (uint64_t)p.K, 64, 128));
     }
     const int sms = sm_count();
-    if (!ok || sms < 2) return cudaErrorInvalidValue;
     // a group has at most R rows, so that a step's routed rows fit a narrower ring
     // (and more of it) in small calls
     const int widest = (int)(p.R < kTileN ? (p.R + 15) / 16 * 16 : kTileN);
-    a.b_bytes = ((uint32_t)widest / 2 * 128 + 1023) / 1024 * 1024;
+    a.box = widest / 2 < 32 ? widest / 2 : 32;
+    a.b_bytes = (uint32_t)((widest / 2 + a.box - 1) / a.box * a.box) * 128;
+    ok = ok && encode_tensor_map_3d_bf16(&amap, p.A, 1, (uint64_t)p.a_rows, (uint64_t)p.K, 64, (uint32_t)a.box);
+    if (!ok || sms < 2) return cudaErrorInvalidValue;
     const uint32_t fixed = 1024 + kEpiWarps * kTurn + ((uint32_t)p.E + 1) * 4 + 2048;
     a.stages = (int)((kSmemLimit - fixed) / (kABytes + a.b_bytes));
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     const uint32_t smem = 1024 + off_turn(a.stages, a.b_bytes) + kEpiWarps * kTurn + ((uint32_t)p.E + 1) * 4;
-    cudaError_t e = ensure_smem_limit<product_kernel<kMode>>(kSmemLimit - 2048);
+    cudaError_t e = ensure_smem_limit<product_kernel<kMode, kGather>>(kSmemLimit - 2048);
     if (e != cudaSuccess) return e;
     // at most R groups have rows, and a group of n rows has n / 256 + 1 tiles at most
     const int64_t groups = min64(p.R, p.E);
     const int64_t most = (p.R / kTileN + groups) * a.m_tiles;
     const int64_t pairs = min64(most, sms / 2);
-    product_kernel<kMode><<<dim3((unsigned)(2 * pairs)), kThreads, smem, s>>>(wmap, amap, a);
+    product_kernel<kMode, kGather><<<dim3((unsigned)(2 * pairs)), threads_of(kGather), smem, s>>>(wmap, amap, a);
     return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_product(ProductMode mode, const ProductArgs &a, cudaStream_t s) {
-    if (mode == kProductPlain) return launch<kProductPlain>(a, s);
-    if (mode == kProductUp) return launch<kProductUp>(a, s);
-    return launch<kProductUpGrad>(a, s);
+    if (mode == kProductPlain) return a.rows ? launch<kProductPlain, true>(a, s) : launch<kProductPlain, false>(a, s);
+    if (mode == kProductUp) return a.rows ? launch<kProductUp, true>(a, s) : launch<kProductUp, false>(a, s);
+    return launch<kProductUpGrad, true>(a, s);
 }
 
 }  // namespace dol

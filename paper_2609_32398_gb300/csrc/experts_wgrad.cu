@@ -5,15 +5,16 @@
 // The contraction runs over the ragged rows, both operands being read as stored
 // (MN-major).  A CTA pair (cta_group::2) owns a 256 x 256 tile of one expert's dW
 // and walks the expert's rows in steps of 64; each CTA loads 128 columns of P and
-// of Q by gathering rows four at a time, so that neither the tokens nor the
-// outputs' gradient is ever permuted in memory.  Rows past the expert's end name
-// no row of the matrices and read as zeros on both sides, whatever the next
-// expert's rows hold.  Two accumulators in TMEM let one tile's 256 KB of fp32
+// of Q: by TMA where the rows lie in dispatch order, and gathered in 16-byte pieces
+// otherwise, so that neither the tokens nor the outputs' gradient is ever permuted
+// in memory.  An expert's last, partial step is gathered on both sides: what lies
+// past its end are zeros on both, whatever the next expert's rows hold.  Two accumulators in TMEM let one tile's 256 KB of fp32
 // leave while the next tile's products run; an expert without rows gets zeros
 // from the epilogue alone.  The result is stored (or added, once per entry) by
 // TMA from 32 x 32 blocks.
 //
-// Warps: 0 loads, 1 issues the MMAs (first CTA), 2-9 epilogue.
+// Warps: 0 TMA, 1 issues the MMAs (first CTA), 2-5 epilogue, 6-9 gather, 10
+// announces their steps.
 #include <cstdint>
 
 #include "experts_mma.cuh"
@@ -21,13 +22,14 @@
 namespace dol {
 namespace {
 
-constexpr int kEpiWarps = 8;
-constexpr int kThreads = (2 + kEpiWarps) * 32;
+constexpr int kEpiWarps = 4;
+constexpr int kFirstLoader = 2 + kEpiWarps;
+constexpr int kThreads = (kFirstLoader + kLoadWarps + 1) * 32;
 constexpr int kStep = 64;                       // rows of a step
 constexpr uint32_t kBlockBytes = kStep * 128;   // 64 columns of a step
 constexpr uint32_t kSide = 2 * kBlockBytes;     // a CTA's 128 columns of one operand
 constexpr uint32_t kStage = 2 * kSide;
-constexpr int kStages = 5;
+constexpr int kStages = 6;
 constexpr uint32_t kOut = 32 * 128;             // an epilogue warp's 32 x 32 block
 constexpr uint32_t kSmem = 1024 + kStages * kStage + kEpiWarps * kOut;
 static_assert(kSmem <= 232448 - 2048, "shared memory");
@@ -47,27 +49,42 @@ struct Tiles {
     }
 };
 
-// The row ids of four routed rows from r on: ids (or r itself), `none` past the end.
-__device__ __forceinline__ int4 row_ids(const int *rows, int r, int end, int none, int *status) {
-    int v[4];
+// A gathering thread's share of one operand's step: 16 bytes of 8 of the 64 rows.
+struct Side {
+    const bf16 *mat;
+    const int *rows;
+    int64_t count;
+    int cols, x;      // columns, and this thread's first one
+    uint32_t dst;     // its place in a stage for row 0 of its eight (8 rows apart)
+
+    // the matrix rows of routed rows r, r + 8, ..., r + 56; -1: none (zeros)
+    __device__ void ids(int r, int end, int *status, int (&id)[8]) const {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        v[j] = none;
-        if (r + j < end) {
-            const int src = rows ? __ldg(rows + r + j) : r + j;
-            if (src >= 0 && src < none) v[j] = src;
-            else if (status) atomicOr(status, kDevBadId);
+        for (int j = 0; j < 8; ++j) {
+            const int i = r + 8 * j;
+            id[j] = -1;
+            if (i < end) {
+                const int src = rows ? __ldg(rows + i) : i;
+                if (src >= 0 && src < count) id[j] = src;
+                else if (status) atomicOr(status, kDevBadId);
+            }
         }
     }
-    return make_int4(v[0], v[1], v[2], v[3]);
-}
+    __device__ void copy(uint32_t stage, const int (&id)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = id[j] >= 0 && x < cols;
+            cp_async16(stage + dst + j * 1024, mat + (in ? (int64_t)id[j] * cols + x : 0), in);
+        }
+    }
+};
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_constant__ CUtensorMap qmap,
                    const __grid_constant__ CUtensorMap omap, const WeightGradArgs a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_align<1024>(smem_raw);
-    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], landed[kStages], acc_full[2], acc_empty[2], drain;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     volatile int *abort = &s_abort;
@@ -75,7 +92,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(&full[i], 1);
+            mbar_init(&full[i], 3);
+            mbar_init(&landed[i], 32 * kLoadWarps);
             mbar_init(&empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -100,16 +118,71 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     const int pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
     int e, m, n, r0, r1;
     if (warp == 0) {
-        // ---------------------------------------------------------- producer
-        const uint32_t bar0 = map_to_rank(&full[0], 0);
-        const int block = lane >> 4, row = 4 * (lane & 15);  // this lane's 4 rows of one block
+        // ---------------------------------------------------------- TMA
+        if (lane == 0) {
+            const uint32_t bar0 = map_to_rank(&full[0], 0);
+            const uint32_t whole = (a.p_rows ? 0u : 2u * kSide) + (a.q_rows ? 0u : 2u * kSide);
+            int it = 0;
+            bool good = true;
+            for (int t = pair; good && t < tiles; t += pairs) {
+                sched.at(t, &e, &m, &n, &r0, &r1);
+                const int px = m * 256 + (int)rank * 128, qx = n * 256 + (int)rank * 128;
+                for (int r = r0; r < r1; r += kStep, ++it) {
+                    const int s = it % kStages;
+                    if (it >= kStages) {
+                        good = pair_wait(&empty[s], (uint32_t)(it / kStages - 1) & 1u, a.status, abort);
+                        if (!good) break;
+                    }
+                    const bool tail = r + kStep > r1 || whole == 0;
+                    if (rank == 0) {
+                        if (tail) mbar_arrive(&full[s]);
+                        else mbar_arrive_expect_tx(&full[s], whole);
+                    }
+                    if (tail) continue;
+                    unsigned char *st = smem + (size_t)s * kStage;
+                    const uint32_t bar = bar0 + 8u * (uint32_t)s;
+                    for (int b = 0; b < 2; ++b) {
+                        if (!a.p_rows) pair_load_3d(st + b * kBlockBytes, &pmap, px + 64 * b, r, 0, bar);
+                        if (!a.q_rows) pair_load_3d(st + kSide + b * kBlockBytes, &qmap, qx + 64 * b, r, 0, bar);
+                    }
+                }
+            }
+            if (!good && rank == 0)
+                for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
+                    mbar_wait(&full[i % kStages], (uint32_t)(i / kStages) & 1u, a.status);
+        }
+        __syncwarp();
+    } else if (warp == kFirstLoader + kLoadWarps) {
+        // ---------------------------------------------------------- announce
+        if (lane == 0) {
+            const uint32_t full0 = map_to_rank(&full[0], 0);
+            int it = 0;
+            bool good = true;
+            for (int t = pair; good && t < tiles; t += pairs) {
+                sched.at(t, &e, &m, &n, &r0, &r1);
+                for (int r = r0; good && r < r1; r += kStep, ++it) {
+                    const int s = it % kStages;
+                    good = announce(&landed[s], (uint32_t)(it / kStages) & 1u, full0 + 8u * (uint32_t)s, a.status, abort);
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp >= kFirstLoader) {
+        // ---------------------------------------------------------- gather
+        // Sixteen lanes copy a row's 256 bytes of one operand, a pass takes 8 rows.
+        const int i = (int)threadIdx.x - kFirstLoader * 32, piece = i & 15, row = i >> 4;
+        const uint32_t place = (uint32_t)((piece >> 3) * kBlockBytes + row * 128 + (((piece & 7) ^ row) << 4));
+        const uint32_t base = smem_u32(smem);
         int it = 0;
         bool good = true;
         for (int t = pair; good && t < tiles; t += pairs) {
             sched.at(t, &e, &m, &n, &r0, &r1);
-            const int px = m * 256 + (int)rank * 128 + 64 * block, qx = n * 256 + (int)rank * 128 + 64 * block;
-            int4 pi = row_ids(a.p_rows, r0 + row, r1, (int)a.p_count, a.status);
-            int4 qi = row_ids(a.q_rows, r0 + row, r1, (int)a.q_count, a.status);
+            const int c = (int)rank * 128 + 8 * piece;
+            const Side sp{a.P, a.p_rows, a.p_count, a.M, m * 256 + c, place};
+            const Side sq{a.Q, a.q_rows, a.q_count, a.N, n * 256 + c, place + kSide};
+            int pi[8], qi[8];  // of the step, read under the wait for the one before
+            if (a.p_rows || r0 + kStep > r1) sp.ids(r0 + row, r1, a.status, pi);
+            if (a.q_rows || r0 + kStep > r1) sq.ids(r0 + row, r1, a.status, qi);
             for (int r = r0; r < r1; r += kStep, ++it) {
                 const int s = it % kStages;
                 if (it >= kStages) {
@@ -117,21 +190,15 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
                     good = __all_sync(kFull, good);
                     if (!good) break;
                 }
-                unsigned char *st = smem + (size_t)s * kStage + block * kBlockBytes + row * 128;
-                const uint32_t bar = bar0 + 8u * (uint32_t)s;
-                if (rank == 0 && lane == 0) mbar_arrive_expect_tx(&full[s], 2 * kStage);
-                __syncwarp();
-                pair_gather4(st, &pmap, px, pi, bar);
-                pair_gather4(st + kSide, &qmap, qx, qi, bar);
-                if (r + kStep < r1) {  // the next step's ids, under its wait
-                    pi = row_ids(a.p_rows, r + kStep + row, r1, (int)a.p_count, a.status);
-                    qi = row_ids(a.q_rows, r + kStep + row, r1, (int)a.q_count, a.status);
-                }
+                const bool tail = r + kStep > r1, tail_next = r + 2 * kStep > r1;
+                if (a.p_rows || tail) sp.copy(base + (uint32_t)s * kStage, pi);
+                if (a.q_rows || tail) sq.copy(base + (uint32_t)s * kStage, qi);
+                cp_async_arrive(&landed[s]);
+                if (a.p_rows || tail_next) sp.ids(r + kStep + row, r1, a.status, pi);
+                if (a.q_rows || tail_next) sq.ids(r + kStep + row, r1, a.status, qi);
             }
         }
-        if (!good && rank == 0 && lane == 0)
-            for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
-                mbar_wait(&full[i % kStages], (uint32_t)(i / kStages) & 1u, a.status);
+        cp_async_wait_all();
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
@@ -186,7 +253,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
             }
             const int m0 = m * 256 + (int)rank * 128 + 32 * quad;
             const uint32_t col = tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)(buf * 256);
-            for (int c = 32 * part; c < 256; c += 64) {
+            for (int c = 32 * part; c < 256; c += 8 * kEpiWarps) {
                 const int n0 = n * 256 + c;
                 if (n0 >= a.N || m0 >= a.M) break;
                 uint32_t r[32];
@@ -232,8 +299,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 
 cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s) {
     CUtensorMap pmap, qmap, omap;
-    if (!encode_gather_map(&pmap, a.P, (uint64_t)a.p_count, (uint64_t)a.M) ||
-        !encode_gather_map(&qmap, a.Q, (uint64_t)a.q_count, (uint64_t)a.N) ||
+    if (!encode_tensor_map_3d_bf16(&pmap, a.P, 1, (uint64_t)a.p_count, (uint64_t)a.M, 64, kStep) ||
+        !encode_tensor_map_3d_bf16(&qmap, a.Q, 1, (uint64_t)a.q_count, (uint64_t)a.N, 64, kStep) ||
         !encode_tensor_map_3d_f32(&omap, a.dW, (uint64_t)a.E, (uint64_t)a.M, (uint64_t)a.N, 32))
         return cudaErrorInvalidValue;
     cudaError_t e = ensure_smem_limit<weight_grad_kernel>(kSmem);
