@@ -26,8 +26,14 @@ __device__ __forceinline__ uint32_t map_to_rank(const void *p, uint32_t rank) {
     return a;
 }
 
+// Arrive on a barrier of either CTA of the pair.  What the arrival stands for lies in
+// this CTA's shared memory or TMEM and has been completed and fenced by the caller
+// (a proxy fence after the copies' wait, or tcgen05.wait and its fence), and the tensor
+// core that uses it next is this SM's own, so that the arrival need not be a release
+// over the cluster: that one waits for every access in flight, and made a step of the
+// ring cost 690 ns instead of 270.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity) {
@@ -42,19 +48,32 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t pa
     return ok != 0;
 }
 
-// Bounded wait (as mbar_wait) with cluster scope; gives up at once when the CTA
-// has given up elsewhere.
+// Bounded wait (as mbar_wait) with cluster scope; gives up when the CTA has given
+// up elsewhere.  The clock is read every 1024 tries only, as reading it takes longer
+// than most waits.
 __device__ __forceinline__ bool pair_wait(uint64_t *bar, uint32_t parity, int *status, volatile int *abort) {
-    if (mbar_try_wait_cluster(bar, parity)) return true;
-    const unsigned long long t0 = global_ns();
+    unsigned long long t0 = 0;
     for (uint32_t it = 1;; ++it) {
         if (mbar_try_wait_cluster(bar, parity)) return true;
-        if ((it & 63u) == 0u && (*abort || global_ns() - t0 > kWaitLimitNs)) {
-            if (status) atomicOr(status, kDevTimeout);
-            *abort = 1;
-            return false;
+        if ((it & 1023u) == 0u) {
+            const unsigned long long t = global_ns();
+            if (t0 == 0) t0 = t;
+            if (*abort || t - t0 > kWaitLimitNs) {
+                if (status) atomicOr(status, kDevTimeout);
+                *abort = 1;
+                return false;
+            }
         }
     }
+}
+
+// The same by a whole warp: one lane polls (32 lanes polling cost the shared memory
+// that the tensor cores read from), the others follow it.
+__device__ __forceinline__ bool pair_wait_warp(uint64_t *bar, uint32_t parity, int *status, volatile int *abort,
+                                               int lane) {
+    int ok = 1;
+    if (lane == 0) ok = pair_wait(bar, parity, status, abort);
+    return __shfl_sync(kFull, ok, 0) != 0;
 }
 
 // TMA loads of a CTA pair: the data goes to this CTA, the bytes are counted on
@@ -64,6 +83,15 @@ __device__ __forceinline__ void pair_load_3d(void *dst, const CUtensorMap *map, 
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
         " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void pair_load_4d(void *dst, const CUtensorMap *map, int x, int y, int z, int u,
+                                             uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(u), "r"(bar)
         : "memory");
 }
 
@@ -80,27 +108,22 @@ __device__ __forceinline__ void pair_load_5d(void *dst, const CUtensorMap *map, 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool in) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-// Arrive on `bar` (one of its expected arrivals) when this thread's copies so far are done.
-__device__ __forceinline__ void cp_async_arrive(uint64_t *bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
+// Where rows are gathered, warp w of a CTA's kLoadWarps gathering warps fills the
+// steps w, w + kLoadWarps, ... of the ring alone, in 16-byte pieces, and then tells
+// the pair's first CTA: as many steps are under way as there are warps.  The ring
+// has at least kLoadWarps stages: a warp that has finished step m - kLoadWarps knows
+// step m - kLoadWarps - stages to be consumed, so that a stage's barrier is at most
+// one phase behind what it waits for, which a parity can tell.  (Rows
+// gathered by TMA, four a copy, took 85 to 100 cycles a copy of 512 bytes, five
+// times the products' time; the arrivals of 128 threads a step on one barrier took
+// twice the products' time.)
+constexpr int kLoadWarps = 6;
 
-// The gathering warps of a CTA (kLoadWarps of them) write 16-byte pieces of rows
-// into the ring and leave each step's `landed` barrier to their copies; one thread
-// of another warp waits for it, makes the step visible to the tensor cores and
-// tells the pair's first CTA, so that the gathering warps run as far ahead as the
-// ring allows.  (Rows gathered by TMA, four a copy, took 85 to 100 cycles a copy of
-// 512 bytes, five times the products' time; gathering warps that announced their
-// own steps three steps late no less, as two of five stages were left to run ahead.)
-constexpr int kLoadWarps = 4;
-
-__device__ __forceinline__ bool announce(uint64_t *landed, uint32_t parity, uint32_t full_addr, int *status,
-                                         volatile int *abort) {
-    if (!pair_wait(landed, parity, status, abort)) return false;
+__device__ __forceinline__ void gathered(uint32_t full_addr, int lane) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
     fence_proxy_async_smem();
-    mbar_arrive_cluster(full_addr);
-    return true;
+    __syncwarp();
+    if (lane == 0) mbar_arrive_cluster(full_addr);
 }
 
 __device__ __forceinline__ void tma_reduce_add_3d(const CUtensorMap *map, const void *src, int x, int y, int z) {
@@ -158,5 +181,10 @@ __host__ __device__ constexpr uint32_t pair_idesc(int n, bool a_mn, bool b_mn) {
 // W1 [E][2F][H] as [E][F/16][2][16][H], box 1 x 4 x 2 x 16 x 64: 64 columns of 64
 // gate rows and their 64 up rows, 16 of each in turn.
 bool encode_gate_up_map(CUtensorMap *map, const void *base, uint64_t E, uint64_t F, uint64_t H);
+
+// A bf16 tensor [planes][rows][cols], cols a multiple of 64, as [planes][cols / 64]
+// [rows][64], box 1 x 2 x 64 x 64: 128 columns of 64 rows, MN-major, in one copy (a
+// copy costs its thread 60 ns, whatever it carries).
+bool encode_mn_pair_map(CUtensorMap *map, const void *base, uint64_t planes, uint64_t rows, uint64_t cols);
 
 }  // namespace dol

@@ -20,8 +20,8 @@
 // permuted copy of the tokens exists.  What a tile holds past its group's end ends
 // in accumulator columns that nobody reads.
 //
-// Warps: 0 TMA, 1 issues the MMAs (first CTA), then the epilogue's, and where rows
-// are gathered four that gather and one that announces their steps.  A TMEM lane is a
+// Warps: 0 weights by TMA, 1 issues the MMAs (first CTA), then the epilogue's, then
+// six that gather rows or one that loads them by TMA.  A TMEM lane is a
 // weight row and a register a routed row, so each epilogue warp turns 32 x 32
 // blocks in shared memory (16-byte pieces xor-swizzled: no bank conflicts) and
 // then has 32 columns of one routed row in a thread, where the activation, the
@@ -36,16 +36,18 @@ namespace dol {
 namespace {
 
 constexpr int kTileN = 256;               // routed rows of a tile at most
-// Epilogue warps: where rows are gathered a longer ring pays more than a faster
-// epilogue (16 KB of turn blocks instead of 32, six stages instead of five).
-__host__ __device__ constexpr int epi_warps(bool gather) { return gather ? 4 : 8; }
-__host__ __device__ constexpr int first_loader(bool gather) { return 2 + epi_warps(gather); }
-__host__ __device__ constexpr int threads_of(bool gather) {
-    return (first_loader(gather) + (gather ? kLoadWarps + 1 : 0)) * 32;
+// The epilogue's blocks take 16 KB in every mode, so that the ring has six stages of
+// 32 KB: four warps with 32 routed rows each, or, where a thread can do with 16 of a
+// row's 32 columns, eight warps with 16 (the gate and up values of a column are 16
+// TMEM lanes apart and want one thread).
+__host__ __device__ constexpr int epi_warps(int mode) { return mode == kProductUp ? 4 : 8; }
+__host__ __device__ constexpr int first_loader(int mode) { return 2 + epi_warps(mode); }
+__host__ __device__ constexpr int threads_of(int mode, bool gather) {
+    return (first_loader(mode) + (gather ? kLoadWarps : 1)) * 32;
 }
+constexpr uint32_t kTurnAll = 16384;
 constexpr uint32_t kABytes = 128 * 128;   // a CTA's weight rows of one step
 constexpr int kMaxStages = 12;
-constexpr uint32_t kTurn = 32 * 128;      // an epilogue warp's block
 constexpr uint32_t kSmemLimit = 232448;
 
 struct PairArgs {
@@ -53,10 +55,10 @@ struct PairArgs {
     int m_tiles;    // tiles of 256 weight rows (up: of 128 gate rows and their up rows)
     int stages;     // of the ring
     uint32_t b_bytes;  // room for a CTA's routed rows of one step
-    int box;        // routed rows of a TMA box (rows in dispatch order)
+    bool paired;    // transposed weights with N a multiple of 64: one box a step
 };
 
-// Shared memory: ring [stages][weights | rows], turn blocks [warps][4 KB], the first
+// Shared memory: ring [stages][weights | rows], turn blocks [16 KB], the first
 // tile of each expert [E + 1], barriers.
 __host__ __device__ inline uint32_t off_turn(int stages, uint32_t b_bytes) { return stages * (kABytes + b_bytes); }
 
@@ -120,81 +122,90 @@ __device__ __forceinline__ uint4 quantise16(const float *v, int *exponent) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// One routed row's 32 values of the tile.  c0: the first weight row of the warp's 32
-// (plain, up_grad), or the first of its 16 gate rows (up).
-template <int kMode>
-__device__ __forceinline__ void finish_row(const ProductArgs &p, int64_t r, int c0, float (&v)[32]) {
-    if (kMode == kProductPlain) {
-        bf16 *dst = p.out + r * p.N + c0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c0 + 8 * j < p.N) store8(dst + 8 * j, v + 8 * j);
-    } else if (kMode == kProductUp) {
-        const int F = p.N / 2;
-        if (c0 >= F) return;
-        if (p.codes) {
-            int eg, eu;
-            const uint4 g = quantise16(v, &eg), u = quantise16(v + 16, &eu);
-            const int64_t at = r * p.N + c0;
-            *reinterpret_cast<uint4 *>(p.codes + at) = g;
-            *reinterpret_cast<uint4 *>(p.codes + at + F) = u;
-            p.exponents[at / kQBlock] = (uint8_t)eg;
-            p.exponents[(at + F) / kQBlock] = (uint8_t)eu;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = v[i] * sigmoid_f(v[i]) * v[16 + i];
-        bf16 *dst = p.out + r * F + c0;
-        store8(dst, v);
-        store8(dst + 8, v + 8);
-    } else {
-        const int F = p.N;
-        const float w = __ldg(p.row_weight + r);
-        float sum = 0.0f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = c0 + 16 * h;
-            if (c >= F) break;
-            const int64_t cg = r * 2 * F + c, cu = cg + F;
-            const uint4 qg = __ldg(reinterpret_cast<const uint4 *>(p.codes + cg));
-            const uint4 qu = __ldg(reinterpret_cast<const uint4 *>(p.codes + cu));
-            const float sg = q8_scale(__ldg(p.exponents + cg / kQBlock));
-            const float su = q8_scale(__ldg(p.exponents + cu / kQBlock));
-            const unsigned ug[4] = {qg.x, qg.y, qg.z, qg.w}, uu[4] = {qu.x, qu.y, qu.z, qu.w};
-            float dg[16], du[16], act[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float zg = q8_value(ug[i / 4], i & 3) * sg, zu = q8_value(uu[i / 4], i & 3) * su;
-                const float s = sigmoid_f(zg), g = v[16 * h + i];
-                const float silu = zg * s, a = silu * zu, gw = g * w;
-                sum = fmaf(g, a, sum);
-                du[i] = gw * silu;
-                dg[i] = gw * zu * fmaf(silu, 1.0f - s, s);
-                act[i] = a * w;
-            }
-            store8(p.dz + cg, dg);
-            store8(p.dz + cg + 8, dg + 8);
-            store8(p.dz + cu, du);
-            store8(p.dz + cu + 8, du + 8);
-            store8(p.out + r * F + c, act);
-            store8(p.out + r * F + c + 8, act + 8);
-        }
-        if (c0 < F) p.strips[(int64_t)(c0 / 32) * p.R + r] = sum;
+// One routed row's values of the tile: up, 16 of the gate from column c0 on and their
+// 16 of the up side; otherwise 16 columns from c0 on.
+__device__ __forceinline__ void finish_plain(const ProductArgs &p, int64_t r, int c0, const float (&v)[16]) {
+    bf16 *dst = p.out + r * p.N + c0;
+    if (c0 < p.N) store8(dst, v);
+    if (c0 + 8 < p.N) store8(dst + 8, v + 8);
+}
+
+__device__ __forceinline__ void finish_up(const ProductArgs &p, int64_t r, int c0, float (&v)[32]) {
+    const int F = p.N / 2;
+    if (c0 >= F) return;
+    if (p.codes) {
+        int eg, eu;
+        const uint4 g = quantise16(v, &eg), u = quantise16(v + 16, &eu);
+        const int64_t at = r * p.N + c0;
+        *reinterpret_cast<uint4 *>(p.codes + at) = g;
+        *reinterpret_cast<uint4 *>(p.codes + at + F) = u;
+        p.exponents[at / kQBlock] = (uint8_t)eg;
+        p.exponents[(at + F) / kQBlock] = (uint8_t)eu;
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = v[i] * sigmoid_f(v[i]) * v[16 + i];
+    bf16 *dst = p.out + r * F + c0;
+    store8(dst, v);
+    store8(dst + 8, v + 8);
+}
+
+// What finish_grad reads of its row, ahead of the products.
+struct Kept {
+    uint4 gate, up;
+    float gate_scale, up_scale, weight;
+};
+__device__ __forceinline__ Kept read_kept(const ProductArgs &p, int64_t r, int c0) {
+    Kept k = {};
+    if (c0 < p.N) {
+        const int64_t cg = r * 2 * p.N + c0, cu = cg + p.N;
+        k.gate = __ldg(reinterpret_cast<const uint4 *>(p.codes + cg));
+        k.up = __ldg(reinterpret_cast<const uint4 *>(p.codes + cu));
+        k.gate_scale = q8_scale(__ldg(p.exponents + cg / kQBlock));
+        k.up_scale = q8_scale(__ldg(p.exponents + cu / kQBlock));
+        k.weight = __ldg(p.row_weight + r);
+    }
+    return k;
+}
+// Returns the sum of g act over the 16 columns.
+__device__ __forceinline__ float finish_grad(const ProductArgs &p, int64_t r, int c0, const float (&v)[16],
+                                             const Kept &k) {
+    const int F = p.N;
+    if (c0 >= F) return 0.0f;
+    const unsigned ug[4] = {k.gate.x, k.gate.y, k.gate.z, k.gate.w}, uu[4] = {k.up.x, k.up.y, k.up.z, k.up.w};
+    float sum = 0.0f, dg[16], du[16], act[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float zg = q8_value(ug[i / 4], i & 3) * k.gate_scale, zu = q8_value(uu[i / 4], i & 3) * k.up_scale;
+        const float s = sigmoid_f(zg), g = v[i];
+        const float silu = zg * s, a = silu * zu, gw = g * k.weight;
+        sum = fmaf(g, a, sum);
+        du[i] = gw * silu;
+        dg[i] = gw * zu * fmaf(silu, 1.0f - s, s);
+        act[i] = a * k.weight;
+    }
+    bf16 *dz = p.dz + r * 2 * F + c0, *out = p.out + r * F + c0;
+    store8(dz, dg);
+    store8(dz + 8, dg + 8);
+    store8(dz + F, du);
+    store8(dz + F + 8, du + 8);
+    store8(out, act);
+    store8(out + 8, act + 8);
+    return sum;
 }
 
 template <int kMode, bool kGather>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kGather), 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kMode, kGather), 1)
 product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const PairArgs a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_align<1024>(smem_raw);
-    constexpr int kEpiWarps = epi_warps(kGather), kFirstLoader = first_loader(kGather);
-    constexpr int kThreads = threads_of(kGather);
+    constexpr int kEpiWarps = epi_warps(kMode), kFirstLoader = first_loader(kMode);
+    constexpr int kThreads = threads_of(kMode, kGather);
     const ProductArgs &p = a.p;
     const int E = p.E, stages = a.stages;
     const uint32_t stage_bytes = kABytes + a.b_bytes;
     unsigned char *turn = smem + off_turn(stages, a.b_bytes);
-    int *first = reinterpret_cast<int *>(turn + kEpiWarps * kTurn);
-    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], acc_full[2], acc_empty[2], drain;
+    int *first = reinterpret_cast<int *>(turn + kTurnAll);
+    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort, s_part[kThreads / 32];
     volatile int *abort = &s_abort;
@@ -204,7 +215,6 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         for (int i = 0; i < stages; ++i) {
             mbar_init(&full[i], kGather ? 3 : 1);
             mbar_init(&empty[i], 1);
-            mbar_init(&landed[i], 32 * kLoadWarps);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&acc_full[i], 1);
@@ -254,16 +264,14 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const int steps = (p.K + 63) / 64;
     const Schedule sched{first, p.offsets, E, a.m_tiles, p.R};
     if (warp == 0) {
-        // ---------------------------------------------------------- TMA
+        // ---------------------------------------------------------- weights
         if (lane == 0) {
             const uint32_t bar0 = map_to_rank(&full[0], 0);
             int it = 0;
             bool good = true;
             for (int t = pair; good && t < tiles; t += pairs) {
                 const Tile tl = sched.at(t);
-                const int half = tl.width / 2;  // this CTA's routed rows: [rank half, + half)
-                const int boxes = kGather ? 0 : (half + a.box - 1) / a.box;
-                const uint32_t bytes = 2u * (kABytes + (uint32_t)(boxes * a.box) * 128u);
+                const int m0 = tl.m * 256 + (int)rank * 128;
                 for (int k = 0; k < steps; ++k, ++it) {
                     const int s = it % stages;
                     if (it >= stages) {
@@ -272,19 +280,17 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                     }
                     unsigned char *st = smem + (size_t)s * stage_bytes;
                     const uint32_t bar = bar0 + 8u * (uint32_t)s;
-                    if (rank == 0) mbar_arrive_expect_tx(&full[s], bytes);
+                    if (rank == 0) mbar_arrive_expect_tx(&full[s], 2u * (kABytes + (kGather ? 0u : a.b_bytes)));
                     if (kMode == kProductUp) {
                         pair_load_5d(st, &wmap, 64 * k, 0, 0, tl.m * 8 + (int)rank * 4, tl.e, bar);
-                    } else if (p.transposed) {
-                        const int m0 = tl.m * 256 + (int)rank * 128;
+                    } else if (!p.transposed) {
+                        pair_load_3d(st, &wmap, 64 * k, m0, tl.e, bar);
+                    } else if (a.paired) {
+                        pair_load_4d(st, &wmap, 0, 64 * k, m0 / 64, tl.e, bar);
+                    } else {
                         pair_load_3d(st, &wmap, m0, 64 * k, tl.e, bar);
                         pair_load_3d(st + kABytes / 2, &wmap, m0 + 64, 64 * k, tl.e, bar);
-                    } else {
-                        pair_load_3d(st, &wmap, 64 * k, tl.m * 256 + (int)rank * 128, tl.e, bar);
                     }
-                    for (int b = 0; b < boxes; ++b)
-                        pair_load_3d(st + kABytes + b * a.box * 128, &amap, 64 * k,
-                                     tl.r0 + (int)rank * half + b * a.box, 0, bar);
                 }
             }
             // a run that gave up: the loads in flight complete before the CTA ends (in the
@@ -294,61 +300,77 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                     mbar_wait(&full[i % stages], (uint32_t)(i / stages) & 1u, p.status);
         }
         __syncwarp();
-    } else if (kGather && warp == kFirstLoader + kLoadWarps) {
-        // ---------------------------------------------------------- announce
+    } else if (!kGather && warp == kFirstLoader) {
+        // ---------------------------------------------------------- rows in dispatch order
+        // One box as high as the widest tile's half: what it holds past this tile's half
+        // is not used.
         if (lane == 0) {
-            const uint32_t full0 = map_to_rank(&full[0], 0);
-            int it = 0;
-            bool good = true;
-            for (int t = pair; good && t < tiles; t += pairs)
-                for (int k = 0; good && k < steps; ++k, ++it) {
-                    const int s = it % stages;
-                    good = announce(&landed[s], (uint32_t)(it / stages) & 1u, full0 + 8u * (uint32_t)s, p.status, abort);
-                }
-        }
-        __syncwarp();
-    } else if (kGather && warp >= kFirstLoader) {
-        // ---------------------------------------------------------- gather
-        // Eight lanes copy the 128 bytes of a row, a pass takes 16 rows.
-        {
-            const int i = (int)threadIdx.x - kFirstLoader * 32, piece = i & 7, row = i >> 3;
-            const uint32_t base = smem_u32(smem) + kABytes + (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4));
+            const uint32_t bar0 = map_to_rank(&full[0], 0);
             int it = 0;
             bool good = true;
             for (int t = pair; good && t < tiles; t += pairs) {
                 const Tile tl = sched.at(t);
-                const int half = tl.width / 2;
-                int src[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int x = row + 16 * j, n = (int)rank * half + x;
-                    src[j] = -1;
-                    if (x < half && n < tl.n) {
-                        const int id = __ldg(p.rows + tl.r0 + n);
-                        if (id >= 0 && id < p.a_rows) src[j] = id;
-                        else if (p.status) atomicOr(p.status, kDevBadId);
-                    }
-                }
+                const int r = tl.r0 + (int)rank * (tl.width / 2);
                 for (int k = 0; k < steps; ++k, ++it) {
                     const int s = it % stages;
                     if (it >= stages) {
                         good = pair_wait(&empty[s], (uint32_t)(it / stages - 1) & 1u, p.status, abort);
-                        good = __all_sync(kFull, good);
                         if (!good) break;
                     }
-                    const int c = 64 * k + 8 * piece;
-                    const uint32_t dst = base + (uint32_t)s * stage_bytes;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        if (row + 16 * j < half) {
-                            const bool in = src[j] >= 0 && c < p.K;
-                            cp_async16(dst + j * 2048, p.A + (in ? (int64_t)src[j] * p.K + c : 0), in);
-                        }
-                    }
-                    cp_async_arrive(&landed[s]);
+                    pair_load_3d(smem + (size_t)s * stage_bytes + kABytes, &amap, 64 * k, r, 0, bar0 + 8u * (uint32_t)s);
                 }
             }
-            cp_async_wait_all();
+        }
+        __syncwarp();
+    } else if (kGather && warp >= kFirstLoader) {
+        // ---------------------------------------------------------- gather
+        // Eight lanes copy the 128 bytes of a row, four rows at a time.
+        const int piece = lane & 7, row = lane >> 3;
+        const uint32_t base = smem_u32(smem) + kABytes + (uint32_t)(row * 128);
+        const uint32_t swz[2] = {(uint32_t)((piece ^ row) << 4), (uint32_t)((piece ^ (row + 4)) << 4)};
+        const uint32_t full0 = map_to_rank(&full[0], 0);
+        int it = 0, mine = warp - kFirstLoader;  // steps so far, this warp's next one
+        bool good = true;
+        for (int t = pair; good && t < tiles; t += pairs) {
+            const Tile tl = sched.at(t);
+            const int half = tl.width / 2;
+            // the rows' ids, 32 at a time, then those of this lane's rows row + 4 j
+            int id[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = (int)rank * half + lane + 32 * j;
+                id[j] = lane + 32 * j < half && n < tl.n ? __ldg(p.rows + tl.r0 + n) : -1;
+            }
+            bool bad = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool out = id[j] < 0 || id[j] >= p.a_rows;
+                bad |= out && lane + 32 * j < half && (int)rank * half + lane + 32 * j < tl.n;
+                if (out) id[j] = -1;
+            }
+            if (bad && p.status) atomicOr(p.status, kDevBadId);
+            int src[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) src[j] = __shfl_sync(kFull, id[j >> 3], (4 * j + row) & 31);
+            const int end = it + steps;
+            for (; mine < end; mine += kLoadWarps) {
+                const int s = mine % stages, c = 64 * (mine - it) + 8 * piece;
+                if (mine >= stages) {
+                    good = pair_wait_warp(&empty[s], (uint32_t)(mine / stages - 1) & 1u, p.status, abort, lane);
+                    if (!good) break;
+                }
+                const uint32_t dst = base + (uint32_t)s * stage_bytes;
+                const bool inside = c < p.K;
+                const bf16 *from = p.A + c;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    if (4 * j >= half) break;
+                    const bool in = inside && src[j] >= 0;
+                    cp_async16(dst + j * 512 + swz[j & 1], in ? from + (int64_t)src[j] * p.K : p.A, in);
+                }
+                gathered(full0 + 8u * (uint32_t)s, lane);
+            }
+            it = end;
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -390,37 +412,73 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     } else {
         // ---------------------------------------------------------- epilogue
         const int quad = warp & 3, part = (warp - 2) >> 2;
-        unsigned char *mine = turn + (warp - 2) * kTurn;
+        unsigned char *mine = turn + (warp - 2) * (kTurnAll / kEpiWarps);
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
         int done = 0;
         for (int t = pair; t < tiles; t += pairs, ++done) {
             const Tile tl = sched.at(t);
             const int buf = done & 1;
-            const bool good = __all_sync(kFull, pair_wait(&acc_full[buf], (uint32_t)(done >> 1) & 1u, p.status, abort));
+            const bool good = pair_wait_warp(&acc_full[buf], (uint32_t)(done >> 1) & 1u, p.status, abort, lane);
             if (!good) break;
             tc_fence_after();
-            const int c0 = kMode == kProductUp ? tl.m * 128 + (int)rank * 64 + quad * 16
-                                               : tl.m * 256 + (int)rank * 128 + quad * 32;
             const uint32_t col = tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)(buf * 256);
-            for (int n0 = 32 * part; n0 < tl.n; n0 += 8 * kEpiWarps) {
-                uint32_t r[32];
-                tmem_ld32(col + (uint32_t)n0, r);
-                tmem_wait_ld();
-                __syncwarp();
+            if constexpr (kMode == kProductUp) {
+                // 32 routed rows at a time, one a thread with its 16 gate and 16 up values
+                const int c0 = tl.m * 128 + (int)rank * 64 + quad * 16;
+                for (int n0 = 0; n0 < tl.n; n0 += 32) {
+                    uint32_t r[32];
+                    tmem_ld32(col + (uint32_t)n0, r);
+                    tmem_wait_ld();
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    *reinterpret_cast<uint32_t *>(mine + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) = r[i];
-                __syncwarp();
-                float v[32];
+                    for (int i = 0; i < 32; ++i)
+                        *reinterpret_cast<uint32_t *>(mine + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) = r[i];
+                    __syncwarp();
+                    float v[32];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float4 f = *reinterpret_cast<const float4 *>(mine + lane * 128 + ((j ^ (lane & 7)) << 4));
-                    v[4 * j] = f.x;
-                    v[4 * j + 1] = f.y;
-                    v[4 * j + 2] = f.z;
-                    v[4 * j + 3] = f.w;
+                    for (int j = 0; j < 8; ++j) {
+                        const float4 f = *reinterpret_cast<const float4 *>(mine + lane * 128 + ((j ^ (lane & 7)) << 4));
+                        v[4 * j] = f.x;
+                        v[4 * j + 1] = f.y;
+                        v[4 * j + 2] = f.z;
+                        v[4 * j + 3] = f.w;
+                    }
+                    if (n0 + lane < tl.n) finish_up(p, tl.r0 + n0 + lane, c0, v);
                 }
-                if (n0 + lane < tl.n) finish_row<kMode>(p, tl.r0 + n0 + lane, c0, v);
+            } else {
+                // 16 routed rows at a time, two threads a row with 16 columns each
+                const int row = lane & 15, h = lane >> 4;
+                const int c0 = tl.m * 256 + (int)rank * 128 + quad * 32 + 16 * h;
+                for (int n0 = 16 * part; n0 < tl.n; n0 += 32) {
+                    const bool in = n0 + row < tl.n;
+                    const int64_t at = tl.r0 + n0 + row;
+                    Kept kept;
+                    if (kMode == kProductUpGrad && in) kept = read_kept(p, at, c0);
+                    uint32_t r[16];
+                    tmem_ld16(col + (uint32_t)n0, r);
+                    tmem_wait_ld();
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        *reinterpret_cast<uint32_t *>(mine + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) = r[i];
+                    __syncwarp();
+                    float v[16];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 f = *reinterpret_cast<const float4 *>(mine + row * 128 + (((4 * h + j) ^ (row & 7)) << 4));
+                        v[4 * j] = f.x;
+                        v[4 * j + 1] = f.y;
+                        v[4 * j + 2] = f.z;
+                        v[4 * j + 3] = f.w;
+                    }
+                    if constexpr (kMode == kProductPlain) {
+                        if (in) finish_plain(p, at, c0, v);
+                    } else {
+                        float sum = in ? finish_grad(p, at, c0, v, kept) : 0.0f;
+                        sum += __shfl_xor_sync(kFull, sum, 16);
+                        if (in && h == 0 && c0 < p.N) p.strips[(int64_t)(c0 / 32) * p.R + at] = sum;
+                    }
+                }
             }
             tc_fence_before();
             __syncwarp();
@@ -444,7 +502,6 @@ int sm_count() {
 
 template <int kMode, bool kGather>
 cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
-    constexpr int kEpiWarps = epi_warps(kGather);
     PairArgs a = {};
     a.p = p;
     CUtensorMap wmap, amap;
@@ -454,28 +511,29 @@ cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
         ok = ok && encode_gate_up_map(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.N / 2, (uint64_t)p.K);
     } else {
         a.m_tiles = (p.N + 255) / 256;
-        ok = ok && (p.transposed ? encode_tensor_map_3d_bf16(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.K, (uint64_t)p.N, 64, 64)
+        a.paired = p.transposed && p.N % 64 == 0;
+        ok = ok && (a.paired ? encode_mn_pair_map(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.K, (uint64_t)p.N) : p.transposed ? encode_tensor_map_3d_bf16(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.K, (uint64_t)p.N, 64, 64)
                                  : encode_tensor_map_3d_bf16(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.N, (uint64_t)p.K, 64, 128));
     }
     const int sms = sm_count();
     // a group has at most R rows, so that a step's routed rows fit a narrower ring
     // (and more of it) in small calls
     const int widest = (int)(p.R < kTileN ? (p.R + 15) / 16 * 16 : kTileN);
-    a.box = widest / 2 < 32 ? widest / 2 : 32;
-    a.b_bytes = (uint32_t)((widest / 2 + a.box - 1) / a.box * a.box) * 128;
-    ok = ok && encode_tensor_map_3d_bf16(&amap, p.A, 1, (uint64_t)p.a_rows, (uint64_t)p.K, 64, (uint32_t)a.box);
+    a.b_bytes = (uint32_t)(widest / 2) * 128;
+    ok = ok && encode_tensor_map_3d_bf16(&amap, p.A, 1, (uint64_t)p.a_rows, (uint64_t)p.K, 64, (uint32_t)widest / 2);
     if (!ok || sms < 2) return cudaErrorInvalidValue;
-    const uint32_t fixed = 1024 + kEpiWarps * kTurn + ((uint32_t)p.E + 1) * 4 + 2048;
+    const uint32_t fixed = 1024 + kTurnAll + ((uint32_t)p.E + 1) * 4 + 2048;
     a.stages = (int)((kSmemLimit - fixed) / (kABytes + a.b_bytes));
     if (a.stages > kMaxStages) a.stages = kMaxStages;
-    const uint32_t smem = 1024 + off_turn(a.stages, a.b_bytes) + kEpiWarps * kTurn + ((uint32_t)p.E + 1) * 4;
+    if (kGather && a.stages < kLoadWarps) return cudaErrorInvalidConfiguration;
+    const uint32_t smem = 1024 + off_turn(a.stages, a.b_bytes) + kTurnAll + ((uint32_t)p.E + 1) * 4;
     cudaError_t e = ensure_smem_limit<product_kernel<kMode, kGather>>(kSmemLimit - 2048);
     if (e != cudaSuccess) return e;
     // at most R groups have rows, and a group of n rows has n / 256 + 1 tiles at most
     const int64_t groups = min64(p.R, p.E);
     const int64_t most = (p.R / kTileN + groups) * a.m_tiles;
     const int64_t pairs = min64(most, sms / 2);
-    product_kernel<kMode, kGather><<<dim3((unsigned)(2 * pairs)), threads_of(kGather), smem, s>>>(wmap, amap, a);
+    product_kernel<kMode, kGather><<<dim3((unsigned)(2 * pairs)), threads_of(kMode, kGather), smem, s>>>(wmap, amap, a);
     return cudaGetLastError();
 }
 

@@ -13,8 +13,7 @@
 // from the epilogue alone.  The result is stored (or added, once per entry) by
 // TMA from 32 x 32 blocks.
 //
-// Warps: 0 TMA, 1 issues the MMAs (first CTA), 2-5 epilogue, 6-9 gather, 10
-// announces their steps.
+// Warps: 0 TMA, 1 issues the MMAs (first CTA), 2-5 epilogue, 6-11 gather.
 #include <cstdint>
 
 #include "experts_mma.cuh"
@@ -24,7 +23,7 @@ namespace {
 
 constexpr int kEpiWarps = 4;
 constexpr int kFirstLoader = 2 + kEpiWarps;
-constexpr int kThreads = (kFirstLoader + kLoadWarps + 1) * 32;
+constexpr int kThreads = (kFirstLoader + kLoadWarps) * 32;
 constexpr int kStep = 64;                       // rows of a step
 constexpr uint32_t kBlockBytes = kStep * 128;   // 64 columns of a step
 constexpr uint32_t kSide = 2 * kBlockBytes;     // a CTA's 128 columns of one operand
@@ -33,6 +32,7 @@ constexpr int kStages = 6;
 constexpr uint32_t kOut = 32 * 128;             // an epilogue warp's 32 x 32 block
 constexpr uint32_t kSmem = 1024 + kStages * kStage + kEpiWarps * kOut;
 static_assert(kSmem <= 232448 - 2048, "shared memory");
+static_assert(kStages >= kLoadWarps, "see kLoadWarps");
 
 struct Tiles {
     const int *offsets;
@@ -49,42 +49,69 @@ struct Tiles {
     }
 };
 
-// A gathering thread's share of one operand's step: 16 bytes of 8 of the 64 rows.
+// One operand as a gathering warp sees it.
 struct Side {
     const bf16 *mat;
     const int *rows;
     int64_t count;
-    int cols, x;      // columns, and this thread's first one
-    uint32_t dst;     // its place in a stage for row 0 of its eight (8 rows apart)
+    int cols, x;      // columns, and this lane's first one
+    uint32_t dst;     // its place in a stage for row lane / 16
 
-    // the matrix rows of routed rows r, r + 8, ..., r + 56; -1: none (zeros)
-    __device__ void ids(int r, int end, int *status, int (&id)[8]) const {
+    // the matrix rows of routed rows r + lane and r + 32 + lane; -1: none (zeros)
+    __device__ int2 ids(int r, int end, int lane, int *status) const {
+        int v[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = r + 8 * j;
-            id[j] = -1;
-            if (i < end) {
-                const int src = rows ? __ldg(rows + i) : i;
-                if (src >= 0 && src < count) id[j] = src;
-                else if (status) atomicOr(status, kDevBadId);
-            }
+        for (int j = 0; j < 2; ++j) {
+            const int i = r + 32 * j + lane;
+            v[j] = i < end ? (rows ? __ldg(rows + i) : i) : -1;
         }
-    }
-    __device__ void copy(uint32_t stage, const int (&id)[8]) const {
+        bool bad = false;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool in = id[j] >= 0 && x < cols;
-            cp_async16(stage + dst + j * 1024, mat + (in ? (int64_t)id[j] * cols + x : 0), in);
+        for (int j = 0; j < 2; ++j) {
+            const bool out = v[j] < 0 || v[j] >= count;
+            bad |= out && r + 32 * j + lane < end;
+            if (out) v[j] = -1;
+        }
+        if (bad && status) atomicOr(status, kDevBadId);
+        return make_int2(v[0], v[1]);
+    }
+    // Sixteen lanes copy a row's 256 bytes, two rows at a time.
+    __device__ void copy(uint32_t stage, int2 id, int lane) const {
+        const int row = lane >> 4, piece = lane & 7;
+        const bf16 *from = mat + x;
+        const bool inside = x < cols;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const int src = __shfl_sync(kFull, j < 16 ? id.x : id.y, (2 * j + row) & 31);
+            const bool in = inside && src >= 0;
+            cp_async16(stage + dst + j * 256 + ((piece ^ ((2 * j + row) & 7)) << 4),
+                       in ? from + (int64_t)src * cols : mat, in);
         }
     }
 };
+
+// 128 columns from x on of 64 rows from r on, by TMA.
+__device__ __forceinline__ void load_side(unsigned char *dst, const CUtensorMap *map, int cols, int x, int r,
+                                          uint32_t bar) {
+    if (cols % 64 == 0) {
+        pair_load_4d(dst, map, 0, r, x / 64, 0, bar);
+    } else {
+        pair_load_3d(dst, map, x, r, 0, bar);
+        pair_load_3d(dst + kBlockBytes, map, x + 64, r, 0, bar);
+    }
+}
+
+bool encode_side(CUtensorMap *map, const bf16 *base, int64_t rows, int cols) {
+    return cols % 64 == 0 ? encode_mn_pair_map(map, base, 1, (uint64_t)rows, (uint64_t)cols)
+                          : encode_tensor_map_3d_bf16(map, base, 1, (uint64_t)rows, (uint64_t)cols, 64, kStep);
+}
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_constant__ CUtensorMap qmap,
                    const __grid_constant__ CUtensorMap omap, const WeightGradArgs a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_align<1024>(smem_raw);
-    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], landed[kStages], acc_full[2], acc_empty[2], drain;
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     volatile int *abort = &s_abort;
@@ -93,7 +120,6 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&full[i], 3);
-            mbar_init(&landed[i], 32 * kLoadWarps);
             mbar_init(&empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -141,10 +167,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
                     if (tail) continue;
                     unsigned char *st = smem + (size_t)s * kStage;
                     const uint32_t bar = bar0 + 8u * (uint32_t)s;
-                    for (int b = 0; b < 2; ++b) {
-                        if (!a.p_rows) pair_load_3d(st + b * kBlockBytes, &pmap, px + 64 * b, r, 0, bar);
-                        if (!a.q_rows) pair_load_3d(st + kSide + b * kBlockBytes, &qmap, qx + 64 * b, r, 0, bar);
-                    }
+                    if (!a.p_rows) load_side(st, &pmap, a.M, px, r, bar);
+                    if (!a.q_rows) load_side(st + kSide, &qmap, a.N, qx, r, bar);
                 }
             }
             if (!good && rank == 0)
@@ -152,53 +176,34 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
                     mbar_wait(&full[i % kStages], (uint32_t)(i / kStages) & 1u, a.status);
         }
         __syncwarp();
-    } else if (warp == kFirstLoader + kLoadWarps) {
-        // ---------------------------------------------------------- announce
-        if (lane == 0) {
-            const uint32_t full0 = map_to_rank(&full[0], 0);
-            int it = 0;
-            bool good = true;
-            for (int t = pair; good && t < tiles; t += pairs) {
-                sched.at(t, &e, &m, &n, &r0, &r1);
-                for (int r = r0; good && r < r1; r += kStep, ++it) {
-                    const int s = it % kStages;
-                    good = announce(&landed[s], (uint32_t)(it / kStages) & 1u, full0 + 8u * (uint32_t)s, a.status, abort);
-                }
-            }
-        }
-        __syncwarp();
     } else if (warp >= kFirstLoader) {
         // ---------------------------------------------------------- gather
-        // Sixteen lanes copy a row's 256 bytes of one operand, a pass takes 8 rows.
-        const int i = (int)threadIdx.x - kFirstLoader * 32, piece = i & 15, row = i >> 4;
-        const uint32_t place = (uint32_t)((piece >> 3) * kBlockBytes + row * 128 + (((piece & 7) ^ row) << 4));
-        const uint32_t base = smem_u32(smem);
-        int it = 0;
+        const uint32_t place = (uint32_t)(((lane >> 3) & 1) * kBlockBytes + (lane >> 4) * 128);
+        const uint32_t base = smem_u32(smem), full0 = map_to_rank(&full[0], 0);
+        int it = 0, mine = warp - kFirstLoader;  // steps so far, this warp's next one
         bool good = true;
         for (int t = pair; good && t < tiles; t += pairs) {
             sched.at(t, &e, &m, &n, &r0, &r1);
-            const int c = (int)rank * 128 + 8 * piece;
+            const int c = (int)rank * 128 + 8 * (lane & 15);
             const Side sp{a.P, a.p_rows, a.p_count, a.M, m * 256 + c, place};
             const Side sq{a.Q, a.q_rows, a.q_count, a.N, n * 256 + c, place + kSide};
-            int pi[8], qi[8];  // of the step, read under the wait for the one before
-            if (a.p_rows || r0 + kStep > r1) sp.ids(r0 + row, r1, a.status, pi);
-            if (a.q_rows || r0 + kStep > r1) sq.ids(r0 + row, r1, a.status, qi);
-            for (int r = r0; r < r1; r += kStep, ++it) {
-                const int s = it % kStages;
-                if (it >= kStages) {
-                    good = pair_wait(&empty[s], (uint32_t)(it / kStages - 1) & 1u, a.status, abort);
-                    good = __all_sync(kFull, good);
+            const int end = it + (r1 - r0 + kStep - 1) / kStep;
+            for (; mine < end; mine += kLoadWarps) {
+                const int s = mine % kStages, r = r0 + (mine - it) * kStep;
+                const bool tail = r + kStep > r1, do_p = a.p_rows || tail, do_q = a.q_rows || tail;
+                int2 pi, qi;
+                if (do_p) pi = sp.ids(r, r1, lane, a.status);
+                if (do_q) qi = sq.ids(r, r1, lane, a.status);
+                if (mine >= kStages) {
+                    good = pair_wait_warp(&empty[s], (uint32_t)(mine / kStages - 1) & 1u, a.status, abort, lane);
                     if (!good) break;
                 }
-                const bool tail = r + kStep > r1, tail_next = r + 2 * kStep > r1;
-                if (a.p_rows || tail) sp.copy(base + (uint32_t)s * kStage, pi);
-                if (a.q_rows || tail) sq.copy(base + (uint32_t)s * kStage, qi);
-                cp_async_arrive(&landed[s]);
-                if (a.p_rows || tail_next) sp.ids(r + kStep + row, r1, a.status, pi);
-                if (a.q_rows || tail_next) sq.ids(r + kStep + row, r1, a.status, qi);
+                if (do_p) sp.copy(base + (uint32_t)s * kStage, pi, lane);
+                if (do_q) sq.copy(base + (uint32_t)s * kStage, qi, lane);
+                gathered(full0 + 8u * (uint32_t)s, lane);
             }
+            it = end;
         }
-        cp_async_wait_all();
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
@@ -247,7 +252,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
             if (!any && a.accumulate) continue;
             const int buf = done & 1;
             if (any) {
-                const bool good = __all_sync(kFull, pair_wait(&acc_full[buf], (uint32_t)(done >> 1) & 1u, a.status, abort));
+                const bool good = pair_wait_warp(&acc_full[buf], (uint32_t)(done >> 1) & 1u, a.status, abort, lane);
                 if (!good) break;
                 tc_fence_after();
             }
@@ -299,8 +304,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 
 cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s) {
     CUtensorMap pmap, qmap, omap;
-    if (!encode_tensor_map_3d_bf16(&pmap, a.P, 1, (uint64_t)a.p_count, (uint64_t)a.M, 64, kStep) ||
-        !encode_tensor_map_3d_bf16(&qmap, a.Q, 1, (uint64_t)a.q_count, (uint64_t)a.N, 64, kStep) ||
+    if (!encode_side(&pmap, a.P, a.p_count, a.M) || !encode_side(&qmap, a.Q, a.q_count, a.N) ||
         !encode_tensor_map_3d_f32(&omap, a.dW, (uint64_t)a.E, (uint64_t)a.M, (uint64_t)a.N, 32))
         return cudaErrorInvalidValue;
     cudaError_t e = ensure_smem_limit<weight_grad_kernel>(kSmem);

@@ -94,4 +94,17 @@ bool encode_gate_up_map(CUtensorMap *map, const void *base, uint64_t E, uint64_t
     return r == CUDA_SUCCESS;
 }
 
+bool encode_mn_pair_map(CUtensorMap *map, const void *base, uint64_t planes, uint64_t rows, uint64_t cols) {
+    PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
+    if (!fn || cols % 64 != 0) return false;
+    const cuuint64_t dims[4] = {64, rows, cols / 64, planes};
+    const cuuint64_t strides[3] = {cols * 2, 128, rows * cols * 2};
+    const cuuint32_t box[4] = {64, 64, 2, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides,
+                    box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
 }  // namespace dol
