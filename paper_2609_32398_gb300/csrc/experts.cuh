@@ -55,6 +55,7 @@ struct WeightGradArgs {
     bool accumulate;
     float *dW;  // [E][M][N]
     int *status;
+    uint32_t m_magic;  // of the tiles along M, set by the launch
 };
 
 cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s);

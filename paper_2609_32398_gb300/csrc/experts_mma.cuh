@@ -36,25 +36,25 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_try_wait_addr(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
+        : "r"(bar), "r"(parity)
         : "memory");
     return ok != 0;
 }
 
-// Bounded wait (as mbar_wait) with cluster scope; gives up when the CTA has given
-// up elsewhere.  The clock is read every 1024 tries only, as reading it takes longer
-// than most waits.
-__device__ __forceinline__ bool pair_wait(uint64_t *bar, uint32_t parity, int *status, volatile int *abort) {
+// Bounded wait (as mbar_wait) with cluster scope on the barrier at a shared address;
+// gives up when the CTA has given up elsewhere.  The clock is read every 1024 tries
+// only, as reading it takes longer than most waits.
+__device__ __forceinline__ bool pair_wait_slow(uint32_t bar, uint32_t parity, int *status, volatile int *abort) {
     unsigned long long t0 = 0;
     for (uint32_t it = 1;; ++it) {
-        if (mbar_try_wait_cluster(bar, parity)) return true;
+        if (mbar_try_wait_addr(bar, parity)) return true;
         if ((it & 1023u) == 0u) {
             const unsigned long long t = global_ns();
             if (t0 == 0) t0 = t;
@@ -66,40 +66,71 @@ __device__ __forceinline__ bool pair_wait(uint64_t *bar, uint32_t parity, int *s
         }
     }
 }
+__device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, int *status, volatile int *abort) {
+    if (mbar_try_wait_addr(bar, parity)) return true;
+    return pair_wait_slow(bar, parity, status, abort);
+}
 
 // The same by a whole warp: one lane polls (32 lanes polling cost the shared memory
 // that the tensor cores read from), the others follow it.
-__device__ __forceinline__ bool pair_wait_warp(uint64_t *bar, uint32_t parity, int *status, volatile int *abort,
+__device__ __forceinline__ bool pair_wait_warp(uint32_t bar, uint32_t parity, int *status, volatile int *abort,
                                                int lane) {
     int ok = 1;
     if (lane == 0) ok = pair_wait(bar, parity, status, abort);
     return __shfl_sync(kFull, ok, 0) != 0;
 }
 
+__device__ __forceinline__ void mbar_expect_tx_addr(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_addr(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// A place in the ring, as a thread walks it: the threads that issue copies and MMAs
+// are each one thread deep in a dependent chain, where the division of a step number
+// by the number of stages alone costs 60 ns a step.
+struct Ring {
+    uint32_t s, phase;  // stage; how often the ring has been walked, mod 2
+    __device__ __forceinline__ void next(uint32_t stages) {
+        if (++s == stages) {
+            s = 0;
+            phase ^= 1u;
+        }
+    }
+    __device__ __forceinline__ void skip(uint32_t n, uint32_t stages) {  // n <= stages
+        s += n;
+        if (s >= stages) {
+            s -= stages;
+            phase ^= 1u;
+        }
+    }
+};
+
 // TMA loads of a CTA pair: the data goes to this CTA, the bytes are counted on
 // `bar`, an address in the cluster's shared window (the pair's first CTA).
-__device__ __forceinline__ void pair_load_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+__device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-        " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+        " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
 
-__device__ __forceinline__ void pair_load_4d(void *dst, const CUtensorMap *map, int x, int y, int z, int u,
+__device__ __forceinline__ void pair_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int u,
                                              uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(u), "r"(bar)
         : "memory");
 }
 
-__device__ __forceinline__ void pair_load_5d(void *dst, const CUtensorMap *map, int x, int y, int z, int u, int v,
+__device__ __forceinline__ void pair_load_5d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int u, int v,
                                              uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-        " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(smem_u32(dst)),
+        " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(u), "r"(v), "r"(bar)
         : "memory");
 }
@@ -154,10 +185,10 @@ __device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uin
 }
 
 // Arrive on `bar` of both CTAs when the MMAs issued so far by this thread are done.
-__device__ __forceinline__ void pair_commit(uint64_t *bar) {
+__device__ __forceinline__ void pair_commit(uint32_t bar) {
     asm volatile(
         "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
-            smem_u32(bar)),
+            bar),
         "h"((uint16_t)3)
         : "memory");
 }
@@ -175,6 +206,12 @@ __device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t addr, uint32_t mn_str
 __host__ __device__ constexpr uint32_t pair_idesc(int n, bool a_mn, bool b_mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
            ((uint32_t)(n / 8) << 17) | ((uint32_t)(256 / 16) << 24);
+}
+
+// i / d for i d < 2^32, by the product with ceil(2^32 / d) (0 stands for d = 1).
+__host__ __device__ inline uint32_t divide_magic(uint32_t d) { return d == 1 ? 0u : 0xffffffffu / d + 1u; }
+__device__ __forceinline__ int divide_by(int i, uint32_t magic) {
+    return magic ? (int)__umulhi((uint32_t)i, magic) : i;
 }
 
 // Host: the pair kernels' tensor maps (128-byte swizzle, zero outside the tensor).

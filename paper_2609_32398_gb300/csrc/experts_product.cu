@@ -53,45 +53,44 @@ constexpr uint32_t kSmemLimit = 232448;
 struct PairArgs {
     ProductArgs p;
     int m_tiles;    // tiles of 256 weight rows (up: of 128 gate rows and their up rows)
+    uint32_t m_magic;  // divide_magic(m_tiles)
     int stages;     // of the ring
     uint32_t b_bytes;  // room for a CTA's routed rows of one step
     bool paired;    // transposed weights with N a multiple of 64: one box a step
 };
 
-// Shared memory: ring [stages][weights | rows], turn blocks [16 KB], the first
-// tile of each expert [E + 1], barriers.
+// Shared memory: ring [stages][weights | rows], turn blocks [16 KB], and for each
+// expert its first tile [E + 1], first row [E + 1] and the width of its tiles [E].
+__host__ __device__ inline uint32_t table_bytes(int E) { return 4u * (3u * (uint32_t)E + 2u); }
 __host__ __device__ inline uint32_t off_turn(int stages, uint32_t b_bytes) { return stages * (kABytes + b_bytes); }
 
 struct Tile {
     int e, m, r0, n, width;  // expert, weight tile, first routed row, rows, MMA width
 };
 
-struct Schedule {
-    const int *first;    // shared [E + 1]
-    const int *offsets;
-    int E, m_tiles;
-    int64_t R;
+// The tiles of a pair in turn: t = pair, pair + pairs, ..., the expert found by going on
+// from the last one's.
+struct Walk {
+    const int *first, *start, *width;  // shared
+    int tiles, pairs, m_tiles;
+    uint32_t m_magic;
+    int t, e;
+    Tile tile;
 
-    __device__ Tile at(int t) const {
-        int lo = 0, hi = E;  // first[lo] <= t < first[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (first[mid] <= t) lo = mid;
-            else hi = mid;
-        }
-        Tile o;
-        o.e = lo;
-        const int a = max(0, min(__ldg(offsets + lo), (int)R));
-        const int cnt = max(a, min(__ldg(offsets + lo + 1), (int)R)) - a;
-        const int nt = (cnt + kTileN - 1) / kTileN;
-        const int i = t - first[lo];
-        const int j = i / m_tiles;
-        o.m = i - j * m_tiles;
-        const int w = (((cnt + nt - 1) / nt) + 15) & ~15;
-        o.r0 = a + j * w;
-        o.n = min(w, a + cnt - o.r0);
-        o.width = (o.n + 15) & ~15;
-        return o;
+    __device__ __forceinline__ bool find() {
+        if (t >= tiles) return false;
+        while (first[e + 1] <= t) ++e;
+        const int i = t - first[e], j = divide_by(i, m_magic), w = width[e], a = start[e];
+        tile.e = e;
+        tile.m = i - j * m_tiles;
+        tile.r0 = a + j * w;
+        tile.n = min(w, start[e + 1] - tile.r0);
+        tile.width = (tile.n + 15) & ~15;
+        return true;
+    }
+    __device__ __forceinline__ bool next() {
+        t += pairs;
+        return find();
     }
 };
 
@@ -193,7 +192,7 @@ __device__ __forceinline__ float finish_grad(const ProductArgs &p, int64_t r, in
     return sum;
 }
 
-template <int kMode, bool kGather>
+template <int kMode, bool kGather, bool kTransposed>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kMode, kGather), 1)
 product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const PairArgs a) {
     extern __shared__ unsigned char smem_raw[];
@@ -204,7 +203,7 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const int E = p.E, stages = a.stages;
     const uint32_t stage_bytes = kABytes + a.b_bytes;
     unsigned char *turn = smem + off_turn(stages, a.b_bytes);
-    int *first = reinterpret_cast<int *>(turn + kTurnAll);
+    int *first = reinterpret_cast<int *>(turn + kTurnAll), *start = first + E + 1, *width = start + E + 1;
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort, s_part[kThreads / 32];
@@ -229,13 +228,15 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
     // the first tile of each expert: a scan of ceil(n / 256) m_tiles over the experts
     int carry = 0;
-    for (int base = 0; base < E; base += kThreads) {
+    for (int base = 0; base <= E; base += kThreads) {
         const int e = base + (int)threadIdx.x;
         int c = 0;
+        if (e <= E) start[e] = max(0, min(__ldg(p.offsets + e), (int)p.R));
         if (e < E) {
-            const int lo = max(0, min(__ldg(p.offsets + e), (int)p.R));
-            const int hi = max(lo, min(__ldg(p.offsets + e + 1), (int)p.R));
-            c = (hi - lo + kTileN - 1) / kTileN * a.m_tiles;
+            const int n = max(0, max(0, min(__ldg(p.offsets + e + 1), (int)p.R)) - start[e]);
+            const int nt = (n + kTileN - 1) / kTileN;
+            width[e] = nt > 0 ? ((n + nt - 1) / nt + 15) & ~15 : 0;
+            c = nt * a.m_tiles;
         }
         int x = c;
 #pragma unroll
@@ -260,37 +261,36 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
-    const int tiles = carry, pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
     const int steps = (p.K + 63) / 64;
-    const Schedule sched{first, p.offsets, E, a.m_tiles, p.R};
+    Walk walk{first, start, width, carry, (int)(gridDim.x >> 1), a.m_tiles, a.m_magic, (int)(blockIdx.x >> 1), 0, {}};
+    const Tile &tl = walk.tile;
+    const uint32_t ring = smem_u32(smem), full0 = smem_u32(full), empty0 = smem_u32(empty);
+    const uint32_t full_pair = map_to_rank(full, 0);  // the first CTA's
     if (warp == 0) {
         // ---------------------------------------------------------- weights
         if (lane == 0) {
-            const uint32_t bar0 = map_to_rank(&full[0], 0);
-            int it = 0;
+            const uint32_t bytes = 2u * (kABytes + (kGather ? 0u : a.b_bytes));
+            Ring at{0, 0};
             bool good = true;
-            for (int t = pair; good && t < tiles; t += pairs) {
-                const Tile tl = sched.at(t);
-                const int m0 = tl.m * 256 + (int)rank * 128;
-                for (int k = 0; k < steps; ++k, ++it) {
-                    const int s = it % stages;
-                    if (it >= stages) {
-                        good = pair_wait(&empty[s], (uint32_t)(it / stages - 1) & 1u, p.status, abort);
-                        if (!good) break;
-                    }
-                    unsigned char *st = smem + (size_t)s * stage_bytes;
-                    const uint32_t bar = bar0 + 8u * (uint32_t)s;
-                    if (rank == 0) mbar_arrive_expect_tx(&full[s], 2u * (kABytes + (kGather ? 0u : a.b_bytes)));
-                    if (kMode == kProductUp) {
-                        pair_load_5d(st, &wmap, 64 * k, 0, 0, tl.m * 8 + (int)rank * 4, tl.e, bar);
-                    } else if (!p.transposed) {
-                        pair_load_3d(st, &wmap, 64 * k, m0, tl.e, bar);
+            int it = 0;
+            for (bool any = walk.find(); good && any; any = walk.next()) {
+                const int m0 = tl.m * 256 + (int)rank * 128, mb = tl.m * 8 + (int)rank * 4;
+                for (int k = 0; k < p.K; k += 64, ++it) {
+                    good = pair_wait(empty0 + 8 * at.s, at.phase ^ 1u, p.status, abort);
+                    if (!good) break;
+                    const uint32_t st = ring + at.s * stage_bytes, bar = full_pair + 8 * at.s;
+                    if (rank == 0) mbar_expect_tx_addr(full0 + 8 * at.s, bytes);
+                    if constexpr (kMode == kProductUp) {
+                        pair_load_5d(st, &wmap, k, 0, 0, mb, tl.e, bar);
+                    } else if constexpr (!kTransposed) {
+                        pair_load_3d(st, &wmap, k, m0, tl.e, bar);
                     } else if (a.paired) {
-                        pair_load_4d(st, &wmap, 0, 64 * k, m0 / 64, tl.e, bar);
+                        pair_load_4d(st, &wmap, 0, k, m0 / 64, tl.e, bar);
                     } else {
-                        pair_load_3d(st, &wmap, m0, 64 * k, tl.e, bar);
-                        pair_load_3d(st + kABytes / 2, &wmap, m0 + 64, 64 * k, tl.e, bar);
+                        pair_load_3d(st, &wmap, m0, k, tl.e, bar);
+                        pair_load_3d(st + kABytes / 2, &wmap, m0 + 64, k, tl.e, bar);
                     }
+                    at.next(stages);
                 }
             }
             // a run that gave up: the loads in flight complete before the CTA ends (in the
@@ -305,19 +305,15 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         // One box as high as the widest tile's half: what it holds past this tile's half
         // is not used.
         if (lane == 0) {
-            const uint32_t bar0 = map_to_rank(&full[0], 0);
-            int it = 0;
+            Ring at{0, 0};
             bool good = true;
-            for (int t = pair; good && t < tiles; t += pairs) {
-                const Tile tl = sched.at(t);
+            for (bool any = walk.find(); good && any; any = walk.next()) {
                 const int r = tl.r0 + (int)rank * (tl.width / 2);
-                for (int k = 0; k < steps; ++k, ++it) {
-                    const int s = it % stages;
-                    if (it >= stages) {
-                        good = pair_wait(&empty[s], (uint32_t)(it / stages - 1) & 1u, p.status, abort);
-                        if (!good) break;
-                    }
-                    pair_load_3d(smem + (size_t)s * stage_bytes + kABytes, &amap, 64 * k, r, 0, bar0 + 8u * (uint32_t)s);
+                for (int k = 0; k < p.K; k += 64) {
+                    good = pair_wait(empty0 + 8 * at.s, at.phase ^ 1u, p.status, abort);
+                    if (!good) break;
+                    pair_load_3d(ring + at.s * stage_bytes + kABytes, &amap, k, r, 0, full_pair + 8 * at.s);
+                    at.next(stages);
                 }
             }
         }
@@ -326,37 +322,39 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         // ---------------------------------------------------------- gather
         // Eight lanes copy the 128 bytes of a row, four rows at a time.
         const int piece = lane & 7, row = lane >> 3;
-        const uint32_t base = smem_u32(smem) + kABytes + (uint32_t)(row * 128);
+        const uint32_t base = ring + kABytes + (uint32_t)(row * 128);
         const uint32_t swz[2] = {(uint32_t)((piece ^ row) << 4), (uint32_t)((piece ^ (row + 4)) << 4)};
-        const uint32_t full0 = map_to_rank(&full[0], 0);
-        int it = 0, mine = warp - kFirstLoader;  // steps so far, this warp's next one
-        bool good = true;
-        for (int t = pair; good && t < tiles; t += pairs) {
-            const Tile tl = sched.at(t);
+        int id[4];  // of this CTA's routed rows lane + 32 j; outside the matrix: recorded and -1
+        auto read_ids = [&]() {
             const int half = tl.width / 2;
-            // the rows' ids, 32 at a time, then those of this lane's rows row + 4 j
-            int id[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = (int)rank * half + lane + 32 * j;
-                id[j] = lane + 32 * j < half && n < tl.n ? __ldg(p.rows + tl.r0 + n) : -1;
-            }
             bool bad = false;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const bool out = id[j] < 0 || id[j] >= p.a_rows;
-                bad |= out && lane + 32 * j < half && (int)rank * half + lane + 32 * j < tl.n;
-                if (out) id[j] = -1;
+                const int n = (int)rank * half + lane + 32 * j;
+                id[j] = lane + 32 * j < half && n < tl.n ? __ldg(p.rows + tl.r0 + n) : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = (int)rank * half + lane + 32 * j;
+                const bool in = lane + 32 * j < half && n < tl.n, out = id[j] < 0 || id[j] >= p.a_rows;
+                bad |= in && out;
+                if (!in || out) id[j] = -1;
             }
             if (bad && p.status) atomicOr(p.status, kDevBadId);
-            int src[32];
+        };
+        int it = 0, mine = warp - kFirstLoader;  // steps so far, this warp's next one
+        bool good = true, any = walk.find();
+        if (any) read_ids();
+        while (good && any) {
+            const int half = tl.width / 2, end = it + steps;
+            int src[32];  // of this lane's rows row + 4 j
 #pragma unroll
             for (int j = 0; j < 32; ++j) src[j] = __shfl_sync(kFull, id[j >> 3], (4 * j + row) & 31);
-            const int end = it + steps;
+            bool ahead = false;
             for (; mine < end; mine += kLoadWarps) {
                 const int s = mine % stages, c = 64 * (mine - it) + 8 * piece;
                 if (mine >= stages) {
-                    good = pair_wait_warp(&empty[s], (uint32_t)(mine / stages - 1) & 1u, p.status, abort, lane);
+                    good = pair_wait_warp(empty0 + 8 * s, (uint32_t)(mine / stages - 1) & 1u, p.status, abort, lane);
                     if (!good) break;
                 }
                 const uint32_t dst = base + (uint32_t)s * stage_bytes;
@@ -368,7 +366,16 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                     const bool in = inside && src[j] >= 0;
                     cp_async16(dst + j * 512 + swz[j & 1], in ? from + (int64_t)src[j] * p.K : p.A, in);
                 }
-                gathered(full0 + 8u * (uint32_t)s, lane);
+                if (mine + kLoadWarps >= end) {  // the next tile's ids come under these copies
+                    any = walk.next();
+                    if (any) read_ids();
+                    ahead = true;
+                }
+                gathered(full_pair + 8 * s, lane);
+            }
+            if (!ahead) {  // no step of this tile was this warp's
+                any = walk.next();
+                if (any) read_ids();
             }
             it = end;
         }
@@ -376,35 +383,40 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
         if (rank == 0 && lane == 0) {
-            int it = 0, done = 0;
+            Ring at{0, 0};
+            int done = 0;
             bool good = true;
-            const uint32_t base = smem_u32(smem);
-            for (int t = pair; good && t < tiles; t += pairs, ++done) {
-                const Tile tl = sched.at(t);
-                const int buf = done & 1;
-                if (done >= 2) good = pair_wait(&acc_empty[buf], (uint32_t)((done >> 1) - 1) & 1u, p.status, abort);
+            // descriptors of stage 0: a step along k is 32 bytes in a K-major row, 16 rows
+            // of 128 bytes in an MN-major block
+            const uint64_t ad0 = kTransposed ? desc_mn_sw128(ring, kABytes / 2) : umma_desc_sw128(ring);
+            const uint64_t bd0 = umma_desc_sw128(ring + kABytes);
+            constexpr uint32_t kAStep = kTransposed ? 2048 / 16 : 32 / 16, kBStep = 32 / 16;
+            const uint32_t acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
+            for (bool any = walk.find(); good && any; any = walk.next(), ++done) {
+                const uint32_t buf = done & 1, turns = (uint32_t)done >> 1;
+                good = pair_wait(acc_empty0 + 8 * buf, (turns & 1u) ^ 1u, p.status, abort);
                 if (!good) break;
                 tc_fence_after();
-                const uint32_t d = tmem + (uint32_t)(buf * 256);
-                const uint32_t idesc = pair_idesc(tl.width, p.transposed, false);
-                for (int k = 0; k < steps; ++k, ++it) {
-                    const int s = it % stages;
-                    good = pair_wait(&full[s], (uint32_t)(it / stages) & 1u, p.status, abort);
+                const uint32_t d = tmem + buf * 256;
+                const uint32_t idesc = pair_idesc(tl.width, kTransposed, false);
+                uint32_t more = 0;
+                for (int k = 0; k < steps; ++k) {
+                    good = pair_wait(full0 + 8 * at.s, at.phase, p.status, abort);
                     if (!good) break;
                     tc_fence_after();
-                    const uint32_t sa = base + (uint32_t)s * stage_bytes, sb = sa + kABytes;
+                    const uint32_t off = at.s * (stage_bytes / 16);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) {
-                        const uint64_t ad = p.transposed ? desc_mn_sw128(sa + kk * 2048, kABytes / 2)
-                                                         : umma_desc_sw128(sa + kk * 32);
-                        pair_mma(d, ad, umma_desc_sw128(sb + kk * 32), idesc, (k | kk) != 0 ? 1u : 0u);
+                        pair_mma(d, ad0 + off + kk * kAStep, bd0 + off + kk * kBStep, idesc, more);
+                        more = 1;
                     }
-                    pair_commit(&empty[s]);
+                    pair_commit(empty0 + 8 * at.s);
+                    at.next(stages);
                 }
-                if (good) pair_commit(&acc_full[buf]);
+                if (good) pair_commit(acc_full0 + 8 * buf);
             }
             if (!good) {  // the tensor cores are done with shared memory before the CTA ends
-                pair_commit(&drain);
+                pair_commit(smem_u32(&drain));
                 mbar_wait(&drain, 0u, p.status);
             }
         }
@@ -415,10 +427,9 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         unsigned char *mine = turn + (warp - 2) * (kTurnAll / kEpiWarps);
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
         int done = 0;
-        for (int t = pair; t < tiles; t += pairs, ++done) {
-            const Tile tl = sched.at(t);
+        for (bool any = walk.find(); any; any = walk.next(), ++done) {
             const int buf = done & 1;
-            const bool good = pair_wait_warp(&acc_full[buf], (uint32_t)(done >> 1) & 1u, p.status, abort, lane);
+            const bool good = pair_wait_warp(smem_u32(&acc_full[buf]), (uint32_t)(done >> 1) & 1u, p.status, abort, lane);
             if (!good) break;
             tc_fence_after();
             const uint32_t col = tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)(buf * 256);
@@ -500,49 +511,56 @@ int sm_count() {
     return n;
 }
 
-template <int kMode, bool kGather>
+template <int kMode, bool kGather, bool kTransposed>
 cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
     PairArgs a = {};
     a.p = p;
     CUtensorMap wmap, amap;
-    bool ok = true;
+    const uint64_t E = p.E, N = p.N, K = p.K;
+    bool ok;
+    a.m_tiles = kMode == kProductUp ? (p.N / 2 + 127) / 128 : (p.N + 255) / 256;
+    a.m_magic = divide_magic((uint32_t)a.m_tiles);
     if (kMode == kProductUp) {
-        a.m_tiles = (p.N / 2 + 127) / 128;
-        ok = ok && encode_gate_up_map(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.N / 2, (uint64_t)p.K);
+        ok = encode_gate_up_map(&wmap, p.W, E, N / 2, K);
+    } else if (!kTransposed) {
+        ok = encode_tensor_map_3d_bf16(&wmap, p.W, E, N, K, 64, 128);
     } else {
-        a.m_tiles = (p.N + 255) / 256;
-        a.paired = p.transposed && p.N % 64 == 0;
-        ok = ok && (a.paired ? encode_mn_pair_map(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.K, (uint64_t)p.N) : p.transposed ? encode_tensor_map_3d_bf16(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.K, (uint64_t)p.N, 64, 64)
-                                 : encode_tensor_map_3d_bf16(&wmap, p.W, (uint64_t)p.E, (uint64_t)p.N, (uint64_t)p.K, 64, 128));
+        a.paired = N % 64 == 0;
+        ok = a.paired ? encode_mn_pair_map(&wmap, p.W, E, K, N) : encode_tensor_map_3d_bf16(&wmap, p.W, E, K, N, 64, 64);
     }
-    const int sms = sm_count();
     // a group has at most R rows, so that a step's routed rows fit a narrower ring
     // (and more of it) in small calls
-    const int widest = (int)(p.R < kTileN ? (p.R + 15) / 16 * 16 : kTileN);
-    a.b_bytes = (uint32_t)(widest / 2) * 128;
-    ok = ok && encode_tensor_map_3d_bf16(&amap, p.A, 1, (uint64_t)p.a_rows, (uint64_t)p.K, 64, (uint32_t)widest / 2);
+    const uint32_t half = (uint32_t)(p.R < kTileN ? (p.R + 15) / 16 * 16 : kTileN) / 2;
+    a.b_bytes = half * 128;
+    ok = ok && encode_tensor_map_3d_bf16(&amap, p.A, 1, (uint64_t)p.a_rows, K, 64, half);
+    const int sms = sm_count();
     if (!ok || sms < 2) return cudaErrorInvalidValue;
-    const uint32_t fixed = 1024 + kTurnAll + ((uint32_t)p.E + 1) * 4 + 2048;
+    const uint32_t fixed = 1024 + kTurnAll + table_bytes(p.E) + 2048;
     a.stages = (int)((kSmemLimit - fixed) / (kABytes + a.b_bytes));
     if (a.stages > kMaxStages) a.stages = kMaxStages;
-    if (kGather && a.stages < kLoadWarps) return cudaErrorInvalidConfiguration;
-    const uint32_t smem = 1024 + off_turn(a.stages, a.b_bytes) + kTurnAll + ((uint32_t)p.E + 1) * 4;
-    cudaError_t e = ensure_smem_limit<product_kernel<kMode, kGather>>(kSmemLimit - 2048);
+    if (a.stages < kLoadWarps) return cudaErrorInvalidConfiguration;
+    const uint32_t smem = 1024 + off_turn(a.stages, a.b_bytes) + kTurnAll + table_bytes(p.E);
+    constexpr auto kernel = product_kernel<kMode, kGather, kTransposed>;
+    cudaError_t e = ensure_smem_limit<kernel>(kSmemLimit - 2048);
     if (e != cudaSuccess) return e;
     // at most R groups have rows, and a group of n rows has n / 256 + 1 tiles at most
-    const int64_t groups = min64(p.R, p.E);
-    const int64_t most = (p.R / kTileN + groups) * a.m_tiles;
+    const int64_t most = (p.R / kTileN + min64(p.R, p.E)) * a.m_tiles;
     const int64_t pairs = min64(most, sms / 2);
-    product_kernel<kMode, kGather><<<dim3((unsigned)(2 * pairs)), threads_of(kMode, kGather), smem, s>>>(wmap, amap, a);
+    kernel<<<dim3((unsigned)(2 * pairs)), threads_of(kMode, kGather), smem, s>>>(wmap, amap, a);
     return cudaGetLastError();
+}
+
+template <bool kGather>
+cudaError_t launch_mode(ProductMode mode, const ProductArgs &a, cudaStream_t s) {
+    if (mode == kProductUp) return launch<kProductUp, kGather, false>(a, s);
+    return a.transposed ? launch<kProductPlain, kGather, true>(a, s) : launch<kProductPlain, kGather, false>(a, s);
 }
 
 }  // namespace
 
 cudaError_t launch_product(ProductMode mode, const ProductArgs &a, cudaStream_t s) {
-    if (mode == kProductPlain) return a.rows ? launch<kProductPlain, true>(a, s) : launch<kProductPlain, false>(a, s);
-    if (mode == kProductUp) return a.rows ? launch<kProductUp, true>(a, s) : launch<kProductUp, false>(a, s);
-    return launch<kProductUpGrad, true>(a, s);
+    if (mode == kProductUpGrad) return launch<kProductUpGrad, true, true>(a, s);
+    return a.rows ? launch_mode<true>(mode, a, s) : launch_mode<false>(mode, a, s);
 }
 
 }  // namespace dol

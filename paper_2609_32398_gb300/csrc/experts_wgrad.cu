@@ -32,20 +32,33 @@ constexpr int kStages = 6;
 constexpr uint32_t kOut = 32 * 128;             // an epilogue warp's 32 x 32 block
 constexpr uint32_t kSmem = 1024 + kStages * kStage + kEpiWarps * kOut;
 static_assert(kSmem <= 232448 - 2048, "shared memory");
-static_assert(kStages >= kLoadWarps, "see kLoadWarps");
+static_assert(kStages == kLoadWarps, "a gathering warp has one stage of its own");
 
-struct Tiles {
+// The tiles of a pair in turn: t = pair, pair + pairs, ...
+struct Walk {
     const int *offsets;
-    int m_tiles, n_tiles;
-    int64_t R;
-    __device__ void at(int t, int *e, int *m, int *n, int *r0, int *r1) const {
-        const int per = m_tiles * n_tiles;
-        *e = t / per;
-        const int i = t - *e * per;
-        *n = i / m_tiles;
-        *m = i - *n * m_tiles;
-        *r0 = max(0, min(__ldg(offsets + *e), (int)R));
-        *r1 = max(*r0, min(__ldg(offsets + *e + 1), (int)R));
+    int R, E, m_tiles, per;  // per: tiles of an expert
+    uint32_t m_magic;
+    int step_e, step_i;      // pairs in experts and tiles
+    int e, i;                // expert, and tile of it
+    int m, n, r0, r1;
+
+    __device__ __forceinline__ bool find() {
+        if (e >= E) return false;
+        n = divide_by(i, m_magic);
+        m = i - n * m_tiles;
+        r0 = max(0, min(__ldg(offsets + e), R));
+        r1 = max(r0, min(__ldg(offsets + e + 1), R));
+        return true;
+    }
+    __device__ __forceinline__ bool next() {
+        e += step_e;
+        i += step_i;
+        if (i >= per) {
+            i -= per;
+            ++e;
+        }
+        return find();
     }
 };
 
@@ -91,7 +104,7 @@ struct Side {
 };
 
 // 128 columns from x on of 64 rows from r on, by TMA.
-__device__ __forceinline__ void load_side(unsigned char *dst, const CUtensorMap *map, int cols, int x, int r,
+__device__ __forceinline__ void load_side(uint32_t dst, const CUtensorMap *map, int cols, int x, int r,
                                           uint32_t bar) {
     if (cols % 64 == 0) {
         pair_load_4d(dst, map, 0, r, x / 64, 0, bar);
@@ -139,36 +152,34 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
-    const Tiles sched{a.offsets, (a.M + 255) / 256, (a.N + 255) / 256, a.R};
-    const int tiles = a.E * sched.m_tiles * sched.n_tiles;
+    const int m_tiles = (a.M + 255) / 256, per = m_tiles * ((a.N + 255) / 256);
     const int pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
-    int e, m, n, r0, r1;
+    Walk w{a.offsets, (int)a.R, a.E, m_tiles, per, a.m_magic, pairs / per, pairs % per, pair / per, pair % per, 0, 0, 0, 0};
+    const uint32_t ring = smem_u32(smem), full0 = smem_u32(full), empty0 = smem_u32(empty);
+    const uint32_t full_pair = map_to_rank(full, 0);  // the first CTA's
     if (warp == 0) {
         // ---------------------------------------------------------- TMA
         if (lane == 0) {
-            const uint32_t bar0 = map_to_rank(&full[0], 0);
             const uint32_t whole = (a.p_rows ? 0u : 2u * kSide) + (a.q_rows ? 0u : 2u * kSide);
+            Ring at{0, 0};
             int it = 0;
             bool good = true;
-            for (int t = pair; good && t < tiles; t += pairs) {
-                sched.at(t, &e, &m, &n, &r0, &r1);
-                const int px = m * 256 + (int)rank * 128, qx = n * 256 + (int)rank * 128;
-                for (int r = r0; r < r1; r += kStep, ++it) {
-                    const int s = it % kStages;
-                    if (it >= kStages) {
-                        good = pair_wait(&empty[s], (uint32_t)(it / kStages - 1) & 1u, a.status, abort);
-                        if (!good) break;
-                    }
-                    const bool tail = r + kStep > r1 || whole == 0;
+            for (bool any = w.find(); good && any; any = w.next()) {
+                const int px = w.m * 256 + (int)rank * 128, qx = w.n * 256 + (int)rank * 128;
+                for (int r = w.r0; r < w.r1; r += kStep, ++it) {
+                    good = pair_wait(empty0 + 8 * at.s, at.phase ^ 1u, a.status, abort);
+                    if (!good) break;
+                    const bool tail = r + kStep > w.r1 || whole == 0;
                     if (rank == 0) {
-                        if (tail) mbar_arrive(&full[s]);
-                        else mbar_arrive_expect_tx(&full[s], whole);
+                        if (tail) mbar_arrive_addr(full0 + 8 * at.s);
+                        else mbar_expect_tx_addr(full0 + 8 * at.s, whole);
                     }
-                    if (tail) continue;
-                    unsigned char *st = smem + (size_t)s * kStage;
-                    const uint32_t bar = bar0 + 8u * (uint32_t)s;
-                    if (!a.p_rows) load_side(st, &pmap, a.M, px, r, bar);
-                    if (!a.q_rows) load_side(st + kSide, &qmap, a.N, qx, r, bar);
+                    if (!tail) {
+                        const uint32_t st = ring + at.s * kStage, bar = full_pair + 8 * at.s;
+                        if (!a.p_rows) load_side(st, &pmap, a.M, px, r, bar);
+                        if (!a.q_rows) load_side(st + kSide, &qmap, a.N, qx, r, bar);
+                    }
+                    at.next(kStages);
                 }
             }
             if (!good && rank == 0)
@@ -179,63 +190,80 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     } else if (warp >= kFirstLoader) {
         // ---------------------------------------------------------- gather
         const uint32_t place = (uint32_t)(((lane >> 3) & 1) * kBlockBytes + (lane >> 4) * 128);
-        const uint32_t base = smem_u32(smem), full0 = map_to_rank(&full[0], 0);
-        int it = 0, mine = warp - kFirstLoader;  // steps so far, this warp's next one
-        bool good = true;
-        for (int t = pair; good && t < tiles; t += pairs) {
-            sched.at(t, &e, &m, &n, &r0, &r1);
-            const int c = (int)rank * 128 + 8 * (lane & 15);
-            const Side sp{a.P, a.p_rows, a.p_count, a.M, m * 256 + c, place};
-            const Side sq{a.Q, a.q_rows, a.q_count, a.N, n * 256 + c, place + kSide};
-            const int end = it + (r1 - r0 + kStep - 1) / kStep;
-            for (; mine < end; mine += kLoadWarps) {
-                const int s = mine % kStages, r = r0 + (mine - it) * kStep;
-                const bool tail = r + kStep > r1, do_p = a.p_rows || tail, do_q = a.q_rows || tail;
-                int2 pi, qi;
-                if (do_p) pi = sp.ids(r, r1, lane, a.status);
-                if (do_q) qi = sq.ids(r, r1, lane, a.status);
-                if (mine >= kStages) {
-                    good = pair_wait_warp(&empty[s], (uint32_t)(mine / kStages - 1) & 1u, a.status, abort, lane);
-                    if (!good) break;
-                }
-                if (do_p) sp.copy(base + (uint32_t)s * kStage, pi, lane);
-                if (do_q) sq.copy(base + (uint32_t)s * kStage, qi, lane);
-                gathered(full0 + 8u * (uint32_t)s, lane);
+        const int s = warp - kFirstLoader;  // this warp's stage of the ring
+        const int c = (int)rank * 128 + 8 * (lane & 15);
+        const uint32_t st = ring + (uint32_t)s * kStage;
+        int k = s, steps = 0, lap = 0;  // the next step of the tile, the tile's steps
+        bool good = true, do_p = false, do_q = false;
+        int2 pi, qi;
+        Side sp{a.P, a.p_rows, a.p_count, a.M, 0, place}, sq{a.Q, a.q_rows, a.q_count, a.N, 0, place + kSide};
+        // moves on to this warp's next step and reads its row ids
+        auto seek = [&](bool any) {
+            while (any) {
+                steps = (w.r1 - w.r0 + kStep - 1) / kStep;
+                if (k < steps) break;
+                k -= steps;
+                any = w.next();
             }
-            it = end;
+            if (any) {
+                const int r = w.r0 + k * kStep;
+                const bool tail = r + kStep > w.r1;
+                do_p = a.p_rows || tail;
+                do_q = a.q_rows || tail;
+                sp.x = w.m * 256 + c;
+                sq.x = w.n * 256 + c;
+                if (do_p) pi = sp.ids(r, w.r1, lane, a.status);
+                if (do_q) qi = sq.ids(r, w.r1, lane, a.status);
+            }
+            return any;
+        };
+        for (bool any = seek(w.find()); any; ++lap) {
+            if (lap > 0) {
+                good = pair_wait_warp(empty0 + 8 * s, (uint32_t)(lap - 1) & 1u, a.status, abort, lane);
+                if (!good) break;
+            }
+            if (do_p) sp.copy(st, pi, lane);
+            if (do_q) sq.copy(st, qi, lane);
+            k += kLoadWarps;
+            any = seek(any);  // under the copies
+            gathered(full_pair + 8 * s, lane);
         }
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
         if (rank == 0 && lane == 0) {
-            const uint32_t idesc = pair_idesc(256, true, true);
-            const uint32_t base = smem_u32(smem);
-            int it = 0, done = 0;  // done: tiles with rows
+            constexpr uint32_t idesc = pair_idesc(256, true, true);
+            const uint64_t pd0 = desc_mn_sw128(ring, kBlockBytes), qd0 = desc_mn_sw128(ring + kSide, kBlockBytes);
+            const uint32_t acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
+            Ring at{0, 0};
+            int done = 0;  // tiles with rows
             bool good = true;
-            for (int t = pair; good && t < tiles; t += pairs) {
-                sched.at(t, &e, &m, &n, &r0, &r1);
-                if (r0 == r1) continue;
-                const int buf = done & 1;
-                if (done >= 2) good = pair_wait(&acc_empty[buf], (uint32_t)((done >> 1) - 1) & 1u, a.status, abort);
+            for (bool any = w.find(); good && any; any = w.next()) {
+                if (w.r0 == w.r1) continue;
+                const uint32_t buf = done & 1, turns = (uint32_t)done >> 1;
+                good = pair_wait(acc_empty0 + 8 * buf, (turns & 1u) ^ 1u, a.status, abort);
                 if (!good) break;
                 tc_fence_after();
-                for (int r = r0; r < r1; r += kStep, ++it) {
-                    const int s = it % kStages;
-                    good = pair_wait(&full[s], (uint32_t)(it / kStages) & 1u, a.status, abort);
+                const uint32_t d = tmem + buf * 256;
+                uint32_t more = 0;
+                for (int r = w.r0; r < w.r1; r += kStep) {
+                    good = pair_wait(full0 + 8 * at.s, at.phase, a.status, abort);
                     if (!good) break;
                     tc_fence_after();
-                    const uint32_t sp = base + (uint32_t)s * kStage, sq = sp + kSide;
+                    const uint32_t off = at.s * (kStage / 16);
 #pragma unroll
-                    for (int kk = 0; kk < kStep / 16; ++kk)
-                        pair_mma(tmem + (uint32_t)(buf * 256), desc_mn_sw128(sp + kk * 2048, kBlockBytes),
-                                 desc_mn_sw128(sq + kk * 2048, kBlockBytes), idesc, (r > r0 || kk > 0) ? 1u : 0u);
-                    pair_commit(&empty[s]);
+                    for (int kk = 0; kk < kStep / 16; ++kk) {
+                        pair_mma(d, pd0 + off + kk * (2048 / 16), qd0 + off + kk * (2048 / 16), idesc, more);
+                        more = 1;
+                    }
+                    pair_commit(empty0 + 8 * at.s);
+                    at.next(kStages);
                 }
-                if (good) pair_commit(&acc_full[buf]);
+                if (good) pair_commit(acc_full0 + 8 * buf);
                 ++done;
             }
             if (!good) {  // the tensor cores are done with shared memory before the CTA ends
-                pair_commit(&drain);
+                pair_commit(smem_u32(&drain));
                 mbar_wait(&drain, 0u, a.status);
             }
         }
@@ -246,20 +274,19 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
         unsigned char *mine = smem + kStages * kStage + (warp - 2) * kOut;
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
         int done = 0;
-        for (int t = pair; t < tiles; t += pairs) {
-            sched.at(t, &e, &m, &n, &r0, &r1);
-            const bool any = r1 > r0;
+        for (bool more = w.find(); more; more = w.next()) {
+            const bool any = w.r1 > w.r0;
             if (!any && a.accumulate) continue;
             const int buf = done & 1;
             if (any) {
-                const bool good = pair_wait_warp(&acc_full[buf], (uint32_t)(done >> 1) & 1u, a.status, abort, lane);
+                const bool good = pair_wait_warp(smem_u32(&acc_full[buf]), (uint32_t)(done >> 1) & 1u, a.status, abort, lane);
                 if (!good) break;
                 tc_fence_after();
             }
-            const int m0 = m * 256 + (int)rank * 128 + 32 * quad;
+            const int m0 = w.m * 256 + (int)rank * 128 + 32 * quad;
             const uint32_t col = tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)(buf * 256);
             for (int c = 32 * part; c < 256; c += 8 * kEpiWarps) {
-                const int n0 = n * 256 + c;
+                const int n0 = w.n * 256 + c;
                 if (n0 >= a.N || m0 >= a.M) break;
                 uint32_t r[32];
                 if (any) {
@@ -278,8 +305,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if (a.accumulate) tma_reduce_add_3d(&omap, mine, n0, m0, e);
-                    else tma_store_3d(&omap, mine, n0, m0, e);
+                    if (a.accumulate) tma_reduce_add_3d(&omap, mine, n0, m0, w.e);
+                    else tma_store_3d(&omap, mine, n0, m0, w.e);
                     bulk_commit_group();
                 }
             }
@@ -313,9 +340,11 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s) {
     e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
+    WeightGradArgs b = a;
+    b.m_magic = divide_magic((uint32_t)(a.M + 255) / 256);
     const int64_t tiles = (int64_t)a.E * ((a.M + 255) / 256) * ((a.N + 255) / 256);
     const int64_t pairs = min64(tiles, sms / 2);
-    weight_grad_kernel<<<dim3((unsigned)(2 * pairs)), kThreads, kSmem, s>>>(pmap, qmap, omap, a);
+    weight_grad_kernel<<<dim3((unsigned)(2 * pairs)), kThreads, kSmem, s>>>(pmap, qmap, omap, b);
     return cudaGetLastError();
 }
 
