@@ -73,6 +73,23 @@ cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos,
 cudaError_t launch_checkpoint_values(const int8_t *codes, const uint8_t *exponents, int64_t rows,
                                      int cols, bf16 *values, cudaStream_t s);
 
+// Launch as a programmatic dependent of the kernel before on `s`: the kernel calls
+// griddepcontrol.wait before it touches global memory.
+template <class... P, class... A>
+inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, const A &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // ---------------------------------------------------------------- device helpers
 
 // 8-bit checkpoint of a block of 16 values: codes in [-127, 127] times 2^(e - 127),
@@ -105,5 +122,26 @@ __device__ __forceinline__ float q8_value(unsigned word, int b) {
 
 // sigma(z) = 1 / (1 + e^-z): e^-z overflows to infinity below -88 and gives 0.
 __device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+
+__device__ __forceinline__ unsigned pack2(float lo, float hi) {
+    __nv_bfloat162 p = __float22bfloat162_rn(make_float2(lo, hi));
+    return *reinterpret_cast<unsigned *>(&p);
+}
+
+// 16 values rounded to bf16: 32 bytes, one whole sector in one store where dst is
+// aligned to it (a half sector a store costs the L2 twice the writes).
+__device__ __forceinline__ void store16(bf16 *dst, const float *v) {
+    unsigned w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
+    if ((reinterpret_cast<uintptr_t>(dst) & 31u) == 0) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(w[0]), "r"(w[1]),
+                     "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(dst)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4 *>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
 
 }  // namespace dol

@@ -3,6 +3,7 @@
 // and the values of an 8-bit checkpoint.  All are bound by memory (the join and
 // the values) or by their launch (the other two).
 #include "experts.cuh"
+#include "tma.cuh"
 
 namespace dol {
 namespace {
@@ -16,17 +17,14 @@ __device__ __forceinline__ void add8(float (&acc)[8], uint4 v, float w) {
     }
 }
 
-__device__ __forceinline__ unsigned pack2(float lo, float hi) {
-    __nv_bfloat162 p = __float22bfloat162_rn(make_float2(lo, hi));
-    return *reinterpret_cast<unsigned *>(&p);
-}
-
 // One thread per 8 columns of a token; its k rows are read as 16-byte pieces.
 // A choice that is left out adds nothing (its row is not read).
 __global__ void __launch_bounds__(256)
 join_kernel(const bf16 *__restrict__ Y, const int *__restrict__ pos, const float *__restrict__ weights,
             const int *__restrict__ offsets, int64_t T, int k, int N, int E, bf16 *__restrict__ out,
             int *status) {
+    pdl_trigger();
+    pdl_wait();
     const int n8 = N / 8;
     const int limit = offsets[E];
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < T * n8; i += (int64_t)gridDim.x * 256) {
@@ -61,6 +59,8 @@ join_kernel(const bf16 *__restrict__ Y, const int *__restrict__ pos, const float
 
 __global__ void row_weights_kernel(const float *__restrict__ combine, const int *__restrict__ pos, int64_t R,
                                    float *__restrict__ row_weight, int *status) {
+    pdl_trigger();
+    pdl_wait();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= R) return;
     const int p = pos[i];
@@ -70,6 +70,8 @@ __global__ void row_weights_kernel(const float *__restrict__ combine, const int 
 
 __global__ void strip_sums_kernel(const float *__restrict__ strips, int n, const int *__restrict__ pos,
                                   const int *__restrict__ offsets, int E, int64_t R, float *__restrict__ dcombine) {
+    pdl_trigger();
+    pdl_wait();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= R) return;
     const int p = pos[i];
@@ -83,6 +85,8 @@ __global__ void strip_sums_kernel(const float *__restrict__ strips, int n, const
 __global__ void __launch_bounds__(256)
 checkpoint_values_kernel(const uint4 *__restrict__ codes, const uint8_t *__restrict__ exponents, int64_t blocks,
                          uint4 *__restrict__ values) {
+    pdl_trigger();
+    pdl_wait();
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < blocks; i += (int64_t)gridDim.x * 256) {
         const uint4 c = __ldg(codes + i);
         const float s = q8_scale(__ldg(exponents + i));
@@ -105,28 +109,27 @@ unsigned blocks_of(int64_t n, int64_t most) {
 
 cudaError_t launch_join(const bf16 *Y, const int *pos, const float *weights, const int *offsets, int64_t T,
                         int k, int N, int E, bf16 *out, int *status, cudaStream_t s) {
-    join_kernel<<<blocks_of(T * (N / 8), 1 << 20), 256, 0, s>>>(Y, pos, weights, offsets, T, k, N, E, out, status);
-    return cudaGetLastError();
+    return launch_after(join_kernel, dim3(blocks_of(T * (N / 8), 1 << 20)), 256, 0, s, Y, pos, weights, offsets, T, k, N, E,
+                        out, status);
 }
 
 cudaError_t launch_row_weights(const float *combine, const int *pos, int64_t R, float *row_weight, int *status,
                                cudaStream_t s) {
-    row_weights_kernel<<<(unsigned)((R + 255) / 256), 256, 0, s>>>(combine, pos, R, row_weight, status);
-    return cudaGetLastError();
+    return launch_after(row_weights_kernel, dim3((unsigned)((R + 255) / 256)), 256, 0, s, combine, pos, R, row_weight,
+                        status);
 }
 
 cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos, const int *offsets, int E,
                               int64_t R, float *dcombine, cudaStream_t s) {
-    strip_sums_kernel<<<(unsigned)((R + 255) / 256), 256, 0, s>>>(strips, n_strips, pos, offsets, E, R, dcombine);
-    return cudaGetLastError();
+    return launch_after(strip_sums_kernel, dim3((unsigned)((R + 255) / 256)), 256, 0, s, strips, n_strips, pos, offsets,
+                        E, R, dcombine);
 }
 
 cudaError_t launch_checkpoint_values(const int8_t *codes, const uint8_t *exponents, int64_t rows, int cols,
                                      bf16 *values, cudaStream_t s) {
     const int64_t n = rows * (cols / kQBlock);
-    checkpoint_values_kernel<<<blocks_of(n, 1 << 20), 256, 0, s>>>(reinterpret_cast<const uint4 *>(codes), exponents,
-                                                                   n, reinterpret_cast<uint4 *>(values));
-    return cudaGetLastError();
+    return launch_after(checkpoint_values_kernel, dim3(blocks_of(n, 1 << 20)), 256, 0, s,
+                        reinterpret_cast<const uint4 *>(codes), exponents, n, reinterpret_cast<uint4 *>(values));
 }
 
 }  // namespace dol

@@ -60,8 +60,9 @@ struct PairArgs {
 };
 
 // Shared memory: ring [stages][weights | rows], turn blocks [16 KB], and for each
-// expert its first tile [E + 1], first row [E + 1] and the width of its tiles [E].
-__host__ __device__ inline uint32_t table_bytes(int E) { return 4u * (3u * (uint32_t)E + 2u); }
+// expert its first tile [E + 1], first row [E + 1] and the width of its tiles [E + 1];
+// then, for the up projection, a tile's exponents [256][2][4].
+__host__ __device__ inline uint32_t table_bytes(int E) { return 4u * 3u * ((uint32_t)E + 1u) + 8u * kTileN; }
 __host__ __device__ inline uint32_t off_turn(int stages, uint32_t b_bytes) { return stages * (kABytes + b_bytes); }
 
 struct Tile {
@@ -94,16 +95,6 @@ struct Walk {
     }
 };
 
-__device__ __forceinline__ unsigned pack2(float lo, float hi) {
-    __nv_bfloat162 p = __float22bfloat162_rn(make_float2(lo, hi));
-    return *reinterpret_cast<unsigned *>(&p);
-}
-
-__device__ __forceinline__ void store8(bf16 *dst, const float *v) {
-    *reinterpret_cast<uint4 *>(dst) =
-        make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
-}
-
 // 16 values to their codes and exponent.
 __device__ __forceinline__ uint4 quantise16(const float *v, int *exponent) {
     unsigned top = 0;
@@ -125,27 +116,27 @@ __device__ __forceinline__ uint4 quantise16(const float *v, int *exponent) {
 // 16 of the up side; otherwise 16 columns from c0 on.
 __device__ __forceinline__ void finish_plain(const ProductArgs &p, int64_t r, int c0, const float (&v)[16]) {
     bf16 *dst = p.out + r * p.N + c0;
-    if (c0 < p.N) store8(dst, v);
-    if (c0 + 8 < p.N) store8(dst + 8, v + 8);
+    if (c0 + 16 <= p.N) store16(dst, v);
+    else if (c0 < p.N)  // N is a multiple of 8
+        *reinterpret_cast<uint4 *>(dst) =
+            make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
 }
 
-__device__ __forceinline__ void finish_up(const ProductArgs &p, int64_t r, int c0, float (&v)[32]) {
+// Returns the two exponents (gate, then up in the second byte).
+__device__ __forceinline__ unsigned finish_up(const ProductArgs &p, int64_t r, int c0, float (&v)[32]) {
     const int F = p.N / 2;
-    if (c0 >= F) return;
+    if (c0 >= F) return 0;
+    int eg = 0, eu = 0;
     if (p.codes) {
-        int eg, eu;
         const uint4 g = quantise16(v, &eg), u = quantise16(v + 16, &eu);
-        const int64_t at = r * p.N + c0;
-        *reinterpret_cast<uint4 *>(p.codes + at) = g;
-        *reinterpret_cast<uint4 *>(p.codes + at + F) = u;
-        p.exponents[at / kQBlock] = (uint8_t)eg;
-        p.exponents[(at + F) / kQBlock] = (uint8_t)eu;
+        int8_t *at = p.codes + r * p.N + c0;
+        *reinterpret_cast<uint4 *>(at) = g;
+        *reinterpret_cast<uint4 *>(at + F) = u;
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = v[i] * sigmoid_f(v[i]) * v[16 + i];
-    bf16 *dst = p.out + r * F + c0;
-    store8(dst, v);
-    store8(dst + 8, v + 8);
+    store16(p.out + r * F + c0, v);
+    return (unsigned)eg | (unsigned)eu << 8;
 }
 
 // What finish_grad reads of its row, ahead of the products.
@@ -183,12 +174,9 @@ __device__ __forceinline__ float finish_grad(const ProductArgs &p, int64_t r, in
         act[i] = a * k.weight;
     }
     bf16 *dz = p.dz + r * 2 * F + c0, *out = p.out + r * F + c0;
-    store8(dz, dg);
-    store8(dz + 8, dg + 8);
-    store8(dz + F, du);
-    store8(dz + F + 8, du + 8);
-    store8(out, act);
-    store8(out + 8, act + 8);
+    store16(dz, dg);
+    store16(dz + F, du);
+    store16(out, act);
     return sum;
 }
 
@@ -226,6 +214,8 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         prefetch_tensormap(&amap);
     }
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
+    pdl_trigger();
+    pdl_wait();
     // the first tile of each expert: a scan of ceil(n / 256) m_tiles over the experts
     int carry = 0;
     for (int base = 0; base <= E; base += kThreads) {
@@ -426,6 +416,7 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         const int quad = warp & 3, part = (warp - 2) >> 2;
         unsigned char *mine = turn + (warp - 2) * (kTurnAll / kEpiWarps);
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
+        unsigned char *exps = reinterpret_cast<unsigned char *>(width + E + 1);  // up: [256][2][4]
         int done = 0;
         for (bool any = walk.find(); any; any = walk.next(), ++done) {
             const int buf = done & 1;
@@ -454,7 +445,29 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                         v[4 * j + 2] = f.z;
                         v[4 * j + 3] = f.w;
                     }
-                    if (n0 + lane < tl.n) finish_up(p, tl.r0 + n0 + lane, c0, v);
+                    unsigned ex = 0;
+                    if (n0 + lane < tl.n) ex = finish_up(p, tl.r0 + n0 + lane, c0, v);
+                    if (p.codes) {
+                        exps[(n0 + lane) * 8 + quad] = (unsigned char)ex;
+                        exps[(n0 + lane) * 8 + 4 + quad] = (unsigned char)(ex >> 8);
+                    }
+                }
+                // the exponents of the four warps' blocks leave together, gate and up
+                // four bytes a row where the row's place allows it
+                if (p.codes) {
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                    const int blocks = p.N / 32, b0 = tl.m * 8 + (int)rank * 4;  // of F, the first of this CTA's
+                    for (int i = (warp - 2) * 32 + lane; i < 2 * tl.n; i += 128) {
+                        const int row = i >> 1, side = i & 1;
+                        uint8_t *to = p.exponents + (int64_t)(tl.r0 + row) * 2 * blocks + side * blocks + b0;
+                        const unsigned w = *reinterpret_cast<const unsigned *>(exps + row * 8 + 4 * side);
+                        if (b0 + 4 <= blocks && (reinterpret_cast<uintptr_t>(to) & 3u) == 0) {
+                            *reinterpret_cast<unsigned *>(to) = w;
+                        } else {
+                            for (int j = 0; j < 4 && b0 + j < blocks; ++j) to[j] = (uint8_t)(w >> (8 * j));
+                        }
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
                 }
             } else {
                 // 16 routed rows at a time, two threads a row with 16 columns each
@@ -546,8 +559,7 @@ cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
     // at most R groups have rows, and a group of n rows has n / 256 + 1 tiles at most
     const int64_t most = (p.R / kTileN + min64(p.R, p.E)) * a.m_tiles;
     const int64_t pairs = min64(most, sms / 2);
-    kernel<<<dim3((unsigned)(2 * pairs)), threads_of(kMode, kGather), smem, s>>>(wmap, amap, a);
-    return cudaGetLastError();
+    return launch_after(kernel, dim3((unsigned)(2 * pairs)), threads_of(kMode, kGather), smem, s, wmap, amap, a);
 }
 
 template <bool kGather>

@@ -147,6 +147,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
         prefetch_tensormap(&omap);
     }
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
+    pdl_trigger();
+    pdl_wait();
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();
@@ -344,8 +346,7 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s) {
     b.m_magic = divide_magic((uint32_t)(a.M + 255) / 256);
     const int64_t tiles = (int64_t)a.E * ((a.M + 255) / 256) * ((a.N + 255) / 256);
     const int64_t pairs = min64(tiles, sms / 2);
-    weight_grad_kernel<<<dim3((unsigned)(2 * pairs)), kThreads, kSmem, s>>>(pmap, qmap, omap, b);
-    return cudaGetLastError();
+    return launch_after(weight_grad_kernel, dim3((unsigned)(2 * pairs)), kThreads, kSmem, s, pmap, qmap, omap, b);
 }
 
 }  // namespace dol
