@@ -513,6 +513,20 @@ do_status do_grouped_matmul_join(const void *A, const void *W, const int32_t *of
 
 size_t do_grouped_matmul_join_workspace_size(int64_t T, int32_t k, int32_t N);
 
+/* The experts of a layer forward, in one call: out [T][H] bf16,
+ *   out[t] = sum_q combine[t][q] W2_e act(W1_e X[t]),  e the q-th expert of t,
+ * with act, rows, offsets and pos as above and the activations rounded to bf16
+ * between the two products (do_expert_up, then do_grouped_matmul_join).
+ * workspace: do_expert_ffn_workspace_size bytes, 256-byte aligned, of any
+ * content. */
+do_status do_expert_ffn(const void *X, const void *W1, const void *W2, const float *combine,
+                        const int32_t *rows, const int32_t *offsets, const int32_t *pos,
+                        int64_t T, int32_t k, int32_t H, int32_t F, int32_t E, void *out,
+                        int32_t *status_flags, void *workspace, size_t workspace_bytes,
+                        void *stream);
+
+size_t do_expert_ffn_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F);
+
 /* Backward of out[t] = sum_q w_tq W2_e act(z_r), r = pos[t][q], through the join,
  * the down projection and the activation, for dout [T][H] bf16, with z as the
  * 8-bit checkpoint of do_expert_up holds it.  With g_r = W2_e^T dout[rows[r]],

@@ -18,7 +18,50 @@ do_status check(int64_t R, int32_t E, int32_t c0, int32_t c1, int step0, int ste
     return DO_OK;
 }
 
+// The rows that a join adds are kept in fp32 where they stay in the L2 anyway: the sum
+// is then rounded once, and nothing is read from memory twice as wide.
+bool join_wide(int64_t R, int32_t N) { return R * N <= (int64_t)(96 << 20) / 4; }
+
 do_status of(cudaError_t e) { return e == cudaSuccess ? DO_OK : DO_ERR_CUDA; }
+
+cudaError_t product(ProductMode mode, const ProductArgs &a, cudaStream_t s) {
+    if (a.R <= kFewRows && !a.transposed && !a.codes) return launch_few_product(mode, a, s);
+    return launch_product(mode, a, s);
+}
+
+size_t join_bytes(int64_t R, int32_t N) {
+    return round256((join_wide(R, N) ? sizeof(float) : sizeof(bf16)) * (size_t)R * (size_t)N);
+}
+
+// a.out: [T][N]; workspace: join_bytes (not used by the few-row kernel).
+cudaError_t product_join(ProductArgs a, const int *pos, const float *weights, int64_t T, int k, void *workspace,
+                         cudaStream_t s) {
+    if (a.R <= kFewRows && !a.transposed) return launch_few_join(a, pos, weights, T, k, s);
+    bf16 *out = a.out;
+    const bool wide = join_wide(a.R, a.N);
+    a.wide = wide ? static_cast<float *>(workspace) : nullptr;
+    a.out = static_cast<bf16 *>(workspace);
+    const cudaError_t e = launch_product(kProductPlain, a, s);
+    return e != cudaSuccess ? e : launch_join(workspace, wide, pos, weights, a.offsets, T, k, a.N, a.E, out, a.status, s);
+}
+
+ProductArgs product_args(const void *A, int64_t a_rows, const int32_t *rows, const void *W, const int32_t *offsets,
+                         int64_t R, int32_t K, int32_t N, int32_t E, bool transposed, void *out, int32_t *status) {
+    ProductArgs a = {};
+    a.A = static_cast<const bf16 *>(A);
+    a.a_rows = a_rows;
+    a.rows = rows;
+    a.W = static_cast<const bf16 *>(W);
+    a.offsets = offsets;
+    a.R = R;
+    a.K = K;
+    a.N = N;
+    a.E = E;
+    a.transposed = transposed;
+    a.out = static_cast<bf16 *>(out);
+    a.status = status;
+    return a;
+}
 
 }  // namespace
 }  // namespace dol
@@ -38,21 +81,10 @@ do_status do_expert_up(const void *X, const void *W1, const int32_t *rows, const
         off(status_flags, 4))
         return DO_ERR_INVALID_ARG;
     if (T > INT32_MAX - 256) return DO_ERR_UNSUPPORTED;
-    dol::ProductArgs a = {};
-    a.A = static_cast<const dol::bf16 *>(X);
-    a.a_rows = T;
-    a.rows = rows;
-    a.W = static_cast<const dol::bf16 *>(W1);
-    a.offsets = offsets;
-    a.R = R;
-    a.K = H;
-    a.N = 2 * F;
-    a.E = E;
-    a.out = static_cast<dol::bf16 *>(act);
+    dol::ProductArgs a = dol::product_args(X, T, rows, W1, offsets, R, H, 2 * F, E, false, act, status_flags);
     a.codes = static_cast<int8_t *>(codes);
     a.exponents = static_cast<uint8_t *>(exponents);
-    a.status = status_flags;
-    return dol::of(dol::launch_product(dol::kProductUp, a, static_cast<cudaStream_t>(stream)));
+    return dol::of(dol::product(dol::kProductUp, a, static_cast<cudaStream_t>(stream)));
 }
 
 do_status do_checkpoint_values(const void *codes, const void *exponents, int64_t rows, int32_t cols, void *values,
@@ -75,25 +107,14 @@ do_status do_grouped_matmul(const void *A, const void *W, const int32_t *rows, c
     if (off(A, 16) || off(W, 16) || off(Y, 16) || off(offsets, 4) || off(rows, 4) || off(status_flags, 4))
         return DO_ERR_INVALID_ARG;
     if (T > INT32_MAX - 256) return DO_ERR_UNSUPPORTED;
-    dol::ProductArgs a = {};
-    a.A = static_cast<const dol::bf16 *>(A);
-    a.a_rows = T;
-    a.rows = rows;
-    a.W = static_cast<const dol::bf16 *>(W);
-    a.offsets = offsets;
-    a.R = R;
-    a.K = K;
-    a.N = N;
-    a.E = E;
-    a.transposed = transposed != 0;
-    a.out = static_cast<dol::bf16 *>(Y);
-    a.status = status_flags;
-    return dol::of(dol::launch_product(dol::kProductPlain, a, static_cast<cudaStream_t>(stream)));
+    return dol::of(dol::product(dol::kProductPlain,
+                                dol::product_args(A, T, rows, W, offsets, R, K, N, E, transposed != 0, Y, status_flags),
+                                static_cast<cudaStream_t>(stream)));
 }
 
 size_t do_grouped_matmul_join_workspace_size(int64_t T, int32_t k, int32_t N) {
     if (T < 1 || k < 1 || N < 1 || T > INT32_MAX / k) return 0;
-    return dol::round256(sizeof(dol::bf16) * (size_t)T * k * N);
+    return dol::join_bytes((int64_t)T * k, N);
 }
 
 do_status do_grouped_matmul_join(const void *A, const void *W, const int32_t *offsets, const int32_t *pos,
@@ -111,22 +132,39 @@ do_status do_grouped_matmul_join(const void *A, const void *W, const int32_t *of
         return DO_ERR_INVALID_ARG;
     if (!workspace || off(workspace, 256) || workspace_bytes < do_grouped_matmul_join_workspace_size(T, k, N))
         return DO_ERR_WORKSPACE;
+    return dol::of(dol::product_join(
+        dol::product_args(A, R, nullptr, W, offsets, R, K, N, E, transposed != 0, out, status_flags), pos, weights, T, k,
+        workspace, static_cast<cudaStream_t>(stream)));
+}
+
+size_t do_expert_ffn_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F) {
+    if (T < 1 || k < 1 || H < 1 || F < 1 || T > INT32_MAX / k) return 0;
+    return dol::round256(sizeof(dol::bf16) * (size_t)T * k * F) + dol::join_bytes((int64_t)T * k, H);
+}
+
+do_status do_expert_ffn(const void *X, const void *W1, const void *W2, const float *combine, const int32_t *rows,
+                        const int32_t *offsets, const int32_t *pos, int64_t T, int32_t k, int32_t H, int32_t F,
+                        int32_t E, void *out, int32_t *status_flags, void *workspace, size_t workspace_bytes,
+                        void *stream) {
+    if (T < 1 || k < 1) return DO_ERR_INVALID_ARG;
+    if (T > INT32_MAX / k) return DO_ERR_UNSUPPORTED;
+    const int64_t R = T * k;
+    do_status st = dol::check(R, E, H, F, 8, dol::kQBlock);
+    if (st != DO_OK) return st;
+    if (!X || !W1 || !W2 || !combine || !rows || !offsets || !pos || !out) return DO_ERR_INVALID_ARG;
+    if (off(X, 16) || off(W1, 16) || off(W2, 16) || off(out, 16) || off(combine, 4) || off(rows, 4) ||
+        off(offsets, 4) || off(pos, 4) || off(status_flags, 4))
+        return DO_ERR_INVALID_ARG;
+    if (!workspace || off(workspace, 256) || workspace_bytes < do_expert_ffn_workspace_size(T, k, H, F))
+        return DO_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    dol::ProductArgs a = {};
-    a.A = static_cast<const dol::bf16 *>(A);
-    a.a_rows = R;
-    a.W = static_cast<const dol::bf16 *>(W);
-    a.offsets = offsets;
-    a.R = R;
-    a.K = K;
-    a.N = N;
-    a.E = E;
-    a.transposed = transposed != 0;
-    a.out = static_cast<dol::bf16 *>(workspace);
-    a.status = status_flags;
-    cudaError_t e = dol::launch_product(dol::kProductPlain, a, s);
+    void *y = static_cast<char *>(workspace) + dol::round256(sizeof(dol::bf16) * (size_t)R * F);
+    cudaError_t e = dol::product(
+        dol::kProductUp, dol::product_args(X, T, rows, W1, offsets, R, H, 2 * F, E, false, workspace, status_flags), s);
     if (e == cudaSuccess)
-        e = dol::launch_join(a.out, pos, weights, offsets, T, k, N, E, static_cast<dol::bf16 *>(out), status_flags, s);
+        e = dol::product_join(
+            dol::product_args(workspace, R, nullptr, W2, offsets, R, F, H, E, false, out, status_flags), pos, combine, T,
+            k, y, s);
     return dol::of(e);
 }
 
@@ -154,24 +192,12 @@ do_status do_expert_up_backward(const void *dout, const void *W2, const void *co
         return DO_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     float *row_weight = static_cast<float *>(workspace);
-    dol::ProductArgs a = {};
-    a.A = static_cast<const dol::bf16 *>(dout);
-    a.a_rows = T;
-    a.rows = rows;
-    a.W = static_cast<const dol::bf16 *>(W2);
-    a.offsets = offsets;
-    a.R = R;
-    a.K = H;
-    a.N = F;
-    a.E = E;
-    a.transposed = true;
-    a.out = static_cast<dol::bf16 *>(act);
+    dol::ProductArgs a = dol::product_args(dout, T, rows, W2, offsets, R, H, F, E, true, act, status_flags);
     a.codes = const_cast<int8_t *>(static_cast<const int8_t *>(codes));
     a.exponents = const_cast<uint8_t *>(static_cast<const uint8_t *>(exponents));
     a.dz = static_cast<dol::bf16 *>(dz);
     a.row_weight = row_weight;
     a.strips = row_weight + R;
-    a.status = status_flags;
     cudaError_t e = dol::launch_row_weights(combine, pos, R, row_weight, status_flags, s);
     if (e == cudaSuccess) e = dol::launch_product(dol::kProductUpGrad, a, s);
     if (e == cudaSuccess) e = dol::launch_strip_sums(a.strips, (F + 31) / 32, pos, offsets, E, R, dcombine, s);

@@ -34,6 +34,7 @@ struct ProductArgs {
     int K, N, E;           // kProductUp: N = 2 F weight rows
     bool transposed;
     bf16 *out;             // plain: Y [R][N]; up: act [R][F]; up_grad: w act [R][F]
+    float *wide;           // plain: Y [R][N] in fp32 instead of out (may be null)
     int8_t *codes;         // up: written (may be null); up_grad: read  [R][2 F]
     uint8_t *exponents;    //                                           [R][2 F / 16]
     bf16 *dz;              // up_grad: [R][2 F]
@@ -43,6 +44,13 @@ struct ProductArgs {
 };
 
 cudaError_t launch_product(ProductMode mode, const ProductArgs &a, cudaStream_t s);
+
+// The products of at most kFewRows routed rows without checkpoint, weights as they
+// are (not transposed), and the joined ones, where out is [T][N] (experts_few.cu).
+constexpr int64_t kFewRows = 32;
+cudaError_t launch_few_product(ProductMode mode, const ProductArgs &a, cudaStream_t s);
+cudaError_t launch_few_join(const ProductArgs &a, const int *pos, const float *weights, int64_t T, int k,
+                            cudaStream_t s);
 
 struct WeightGradArgs {
     const bf16 *P;  // [p_count][M]
@@ -62,7 +70,8 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s);
 
 // out[t][n] = sum_q weights[t][q] Y[pos[t][q]][n] (weights null: all one) in fp32,
 // rounded once.  A pos outside [0, offsets[E]) is left out and recorded.
-cudaError_t launch_join(const bf16 *Y, const int *pos, const float *weights, const int *offsets,
+// Y is fp32 where `wide`, else bf16.
+cudaError_t launch_join(const void *Y, bool wide, const int *pos, const float *weights, const int *offsets,
                         int64_t T, int k, int N, int E, bf16 *out, int *status, cudaStream_t s);
 // row_weight[pos[t][q]] = combine[t][q]
 cudaError_t launch_row_weights(const float *combine, const int *pos, int64_t R, float *row_weight,
@@ -115,9 +124,11 @@ __device__ __forceinline__ float q8_scale(int e) {
 __device__ __forceinline__ unsigned q8_code(float v, float inv) {
     return __float_as_uint(fmaf(v, inv, 12582912.0f)) & 0xffu;
 }
-// code of byte b (0..3) of a word as a float
+// Code of byte b (0..3) of a word as a float: the byte with its sign bit turned over is
+// code + 128 in the low bits of 2^23 (the conversion instruction shares its pipe with
+// sigma's exponential and division and is four times slower).
 __device__ __forceinline__ float q8_value(unsigned word, int b) {
-    return (float)(int8_t)(word >> (8 * b));
+    return __uint_as_float(__byte_perm(word ^ 0x80808080u, 0x4b000000u, 0x7440u + (unsigned)b)) - 8388736.0f;
 }
 
 // sigma(z) = 1 / (1 + e^-z): e^-z overflows to infinity below -88 and gives 0.

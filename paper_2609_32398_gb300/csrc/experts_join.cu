@@ -17,40 +17,85 @@ __device__ __forceinline__ void add8(float (&acc)[8], uint4 v, float w) {
     }
 }
 
-// One thread per 8 columns of a token; its k rows are read as 16-byte pieces.
-// A choice that is left out adds nothing (its row is not read).
+// The pieces of a token's rows that a thread reads: up to eight choices at a time.
+struct Picks {
+    int row[8];   // -1: left out
+    float w[8];
+};
+__device__ __forceinline__ Picks read_picks(const int *pos, const float *weights, int64_t t, int k, int q0,
+                                            int limit, int *status) {
+    Picks p;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        p.row[q] = q0 + q < k ? __ldg(pos + t * k + q0 + q) : -1;
+        p.w[q] = weights && q0 + q < k ? __ldg(weights + t * k + q0 + q) : 1.0f;
+    }
+    bool bad = false;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const bool out = p.row[q] < 0 || p.row[q] >= limit;
+        bad |= out && q0 + q < k;
+        if (out) p.row[q] = -1;
+    }
+    if (bad && status) atomicOr(status, kDevBadId);
+    return p;
+}
+
+// A thread has 8 columns and walks over tokens; a token's rows are read as 16-byte
+// pieces, eight in flight, and the next token's positions and weights under them.  A
+// choice that is left out adds nothing (its row is not read).  Bound by memory: T = 16384,
+// k = 8, N = 2048 moves 604 MB.
+template <typename Y>
 __global__ void __launch_bounds__(256)
-join_kernel(const bf16 *__restrict__ Y, const int *__restrict__ pos, const float *__restrict__ weights,
-            const int *__restrict__ offsets, int64_t T, int k, int N, int E, bf16 *__restrict__ out,
+join_kernel(const Y *__restrict__ y, const int *__restrict__ pos, const float *__restrict__ weights,
+            const int *__restrict__ offsets, int64_t T, int k, int N, int E, int cx, bf16 *__restrict__ out,
             int *status) {
-    pdl_trigger();
     pdl_wait();
-    const int n8 = N / 8;
-    const int limit = offsets[E];
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < T * n8; i += (int64_t)gridDim.x * 256) {
-        const int64_t t = i / n8;
-        const int c = (int)(i - t * n8);
+    const int64_t rows = T * k;
+    const int limit = (int)min64(max(__ldg(offsets + E), 0), rows);
+    const int c = (int)blockIdx.y * 256 + (int)threadIdx.x % cx, per = 256 / cx;
+    const int64_t step = (int64_t)gridDim.x * per;
+    int64_t t = (int64_t)blockIdx.x * per + (int)threadIdx.x / cx;
+    if (c >= N / 8 || t >= T) return;
+    Picks now = read_picks(pos, weights, t, k, 0, limit, status);
+    for (; t < T; t += step) {
         float acc[8] = {};
         for (int q0 = 0; q0 < k; q0 += 8) {
-            uint4 v[8];
-            float w[8];
+            if constexpr (sizeof(Y) == 2) {
+                uint4 v[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                v[q] = make_uint4(0, 0, 0, 0);
-                w[q] = 0.0f;
-                if (q0 + q < k) {
-                    const int p = __ldg(pos + t * k + q0 + q);
-                    if (p >= 0 && p < limit && p < T * k) {
-                        v[q] = __ldg(reinterpret_cast<const uint4 *>(Y + (int64_t)p * N) + c);
-                        w[q] = weights ? __ldg(weights + t * k + q0 + q) : 1.0f;
-                    } else if (status) {
-                        atomicOr(status, kDevBadId);
+                for (int q = 0; q < 8; ++q) {
+                    v[q] = make_uint4(0, 0, 0, 0);
+                    if (now.row[q] >= 0) v[q] = __ldg(reinterpret_cast<const uint4 *>(y + (int64_t)now.row[q] * N) + c);
+                }
+                const Picks was = now;
+                if (q0 + 8 < k) now = read_picks(pos, weights, t, k, q0 + 8, limit, status);
+                else if (t + step < T) now = read_picks(pos, weights, t + step, k, 0, limit, status);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (was.row[q] >= 0) add8(acc, v[q], was.w[q]);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float4 v[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        v[q] = make_float4(0, 0, 0, 0);
+                        if (now.row[q] >= 0)
+                            v[q] = __ldg(reinterpret_cast<const float4 *>(y + (int64_t)now.row[q] * N) + 2 * c + h);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        if (now.row[q] < 0) continue;
+                        acc[4 * h] = fmaf(now.w[q], v[q].x, acc[4 * h]);
+                        acc[4 * h + 1] = fmaf(now.w[q], v[q].y, acc[4 * h + 1]);
+                        acc[4 * h + 2] = fmaf(now.w[q], v[q].z, acc[4 * h + 2]);
+                        acc[4 * h + 3] = fmaf(now.w[q], v[q].w, acc[4 * h + 3]);
                     }
                 }
+                if (q0 + 8 < k) now = read_picks(pos, weights, t, k, q0 + 8, limit, status);
+                else if (t + step < T) now = read_picks(pos, weights, t + step, k, 0, limit, status);
             }
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (q0 + q < k) add8(acc, v[q], w[q]);
         }
         reinterpret_cast<uint4 *>(out + t * N)[c] = make_uint4(pack2(acc[0], acc[1]), pack2(acc[2], acc[3]),
                                                                pack2(acc[4], acc[5]), pack2(acc[6], acc[7]));
@@ -59,7 +104,6 @@ join_kernel(const bf16 *__restrict__ Y, const int *__restrict__ pos, const float
 
 __global__ void row_weights_kernel(const float *__restrict__ combine, const int *__restrict__ pos, int64_t R,
                                    float *__restrict__ row_weight, int *status) {
-    pdl_trigger();
     pdl_wait();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= R) return;
@@ -70,13 +114,13 @@ __global__ void row_weights_kernel(const float *__restrict__ combine, const int 
 
 __global__ void strip_sums_kernel(const float *__restrict__ strips, int n, const int *__restrict__ pos,
                                   const int *__restrict__ offsets, int E, int64_t R, float *__restrict__ dcombine) {
-    pdl_trigger();
     pdl_wait();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= R) return;
     const int p = pos[i];
     float s = 0.0f;
     if (p >= 0 && p < R && p < offsets[E])
+#pragma unroll 8
         for (int j = 0; j < n; ++j) s += strips[(int64_t)j * R + p];
     dcombine[i] = s;
 }
@@ -85,7 +129,6 @@ __global__ void strip_sums_kernel(const float *__restrict__ strips, int n, const
 __global__ void __launch_bounds__(256)
 checkpoint_values_kernel(const uint4 *__restrict__ codes, const uint8_t *__restrict__ exponents, int64_t blocks,
                          uint4 *__restrict__ values) {
-    pdl_trigger();
     pdl_wait();
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < blocks; i += (int64_t)gridDim.x * 256) {
         const uint4 c = __ldg(codes + i);
@@ -107,10 +150,19 @@ unsigned blocks_of(int64_t n, int64_t most) {
 
 }  // namespace
 
-cudaError_t launch_join(const bf16 *Y, const int *pos, const float *weights, const int *offsets, int64_t T,
-                        int k, int N, int E, bf16 *out, int *status, cudaStream_t s) {
-    return launch_after(join_kernel, dim3(blocks_of(T * (N / 8), 1 << 20)), 256, 0, s, Y, pos, weights, offsets, T, k, N, E,
-                        out, status);
+cudaError_t launch_join(const void *Y, bool wide, const int *pos, const float *weights, const int *offsets,
+                        int64_t T, int k, int N, int E, bf16 *out, int *status, cudaStream_t s) {
+    int cx = 1;  // threads side by side on a token
+    while (cx < 256 && cx < N / 8) cx *= 2;
+    const int64_t need = (T + 256 / cx - 1) / (256 / cx);
+    const unsigned gy = (unsigned)((N / 8 + 255) / 256);
+    // three blocks of 80 registers a thread fit an SM
+    const unsigned gx = (unsigned)min64(need, (3 * 152 + gy - 1) / gy);
+    if (wide)
+        return launch_after(join_kernel<float>, dim3(gx, gy), 256, 0, s, static_cast<const float *>(Y), pos, weights,
+                            offsets, T, k, N, E, cx, out, status);
+    return launch_after(join_kernel<bf16>, dim3(gx, gy), 256, 0, s, static_cast<const bf16 *>(Y), pos, weights, offsets,
+                        T, k, N, E, cx, out, status);
 }
 
 cudaError_t launch_row_weights(const float *combine, const int *pos, int64_t R, float *row_weight, int *status,

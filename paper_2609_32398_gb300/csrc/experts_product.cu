@@ -115,6 +115,13 @@ __device__ __forceinline__ uint4 quantise16(const float *v, int *exponent) {
 // One routed row's values of the tile: up, 16 of the gate from column c0 on and their
 // 16 of the up side; otherwise 16 columns from c0 on.
 __device__ __forceinline__ void finish_plain(const ProductArgs &p, int64_t r, int c0, const float (&v)[16]) {
+    if (p.wide) {
+        float4 *to = reinterpret_cast<float4 *>(p.wide + r * p.N + c0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c0 + 4 * j < p.N) to[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        return;
+    }
     bf16 *dst = p.out + r * p.N + c0;
     if (c0 + 16 <= p.N) store16(dst, v);
     else if (c0 < p.N)  // N is a multiple of 8
@@ -214,7 +221,6 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         prefetch_tensormap(&amap);
     }
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
-    pdl_trigger();
     pdl_wait();
     // the first tile of each expert: a scan of ceil(n / 256) m_tiles over the experts
     int carry = 0;
@@ -420,6 +426,11 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         int done = 0;
         for (bool any = walk.find(); any; any = walk.next(), ++done) {
             const int buf = done & 1;
+            // up_grad: what the first rows want of the checkpoint comes under the products
+            const int row = lane & 15, h = lane >> 4;
+            const int cr = tl.m * 256 + (int)rank * 128 + quad * 32 + 16 * h;  // plain, up_grad: first column
+            Kept kept = {};
+            if (kMode == kProductUpGrad && 16 * part + row < tl.n) kept = read_kept(p, tl.r0 + 16 * part + row, cr);
             const bool good = pair_wait_warp(smem_u32(&acc_full[buf]), (uint32_t)(done >> 1) & 1u, p.status, abort, lane);
             if (!good) break;
             tc_fence_after();
@@ -471,13 +482,11 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 }
             } else {
                 // 16 routed rows at a time, two threads a row with 16 columns each
-                const int row = lane & 15, h = lane >> 4;
-                const int c0 = tl.m * 256 + (int)rank * 128 + quad * 32 + 16 * h;
                 for (int n0 = 16 * part; n0 < tl.n; n0 += 32) {
                     const bool in = n0 + row < tl.n;
                     const int64_t at = tl.r0 + n0 + row;
-                    Kept kept;
-                    if (kMode == kProductUpGrad && in) kept = read_kept(p, at, c0);
+                    Kept later = {};
+                    if (kMode == kProductUpGrad && n0 + 32 + row < tl.n) later = read_kept(p, at + 32, cr);
                     uint32_t r[16];
                     tmem_ld16(col + (uint32_t)n0, r);
                     tmem_wait_ld();
@@ -496,11 +505,12 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                         v[4 * j + 3] = f.w;
                     }
                     if constexpr (kMode == kProductPlain) {
-                        if (in) finish_plain(p, at, c0, v);
+                        if (in) finish_plain(p, at, cr, v);
                     } else {
-                        float sum = in ? finish_grad(p, at, c0, v, kept) : 0.0f;
+                        float sum = in ? finish_grad(p, at, cr, v, kept) : 0.0f;
                         sum += __shfl_xor_sync(kFull, sum, 16);
-                        if (in && h == 0 && c0 < p.N) p.strips[(int64_t)(c0 / 32) * p.R + at] = sum;
+                        if (in && h == 0 && cr < p.N) p.strips[(int64_t)(cr / 32) * p.R + at] = sum;
+                        kept = later;
                     }
                 }
             }
@@ -509,6 +519,7 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             if (lane == 0) mbar_arrive_cluster(empty_addr + 8u * (uint32_t)buf);
         }
     }
+    pdl_trigger();  // this CTA's work is done: the next kernel may begin to arrive
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();

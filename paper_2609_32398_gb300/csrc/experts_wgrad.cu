@@ -147,7 +147,6 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
         prefetch_tensormap(&omap);
     }
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
-    pdl_trigger();
     pdl_wait();
     tc_fence_before();
     __syncthreads();
@@ -322,6 +321,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
         if (lane == 0) bulk_wait_all<0>();
         __syncwarp();
     }
+    pdl_trigger();  // this CTA's work is done: the next kernel may begin to arrive
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();

@@ -68,6 +68,9 @@ EXPORTS = {
     "do_grouped_matmul_join_workspace_size": (["i64", "i32", "i32"], "sz"),
     "do_grouped_matmul_join": (["p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i32", "i32", "p", "p", "p",
                                 "sz", "p"], "i32"),
+    "do_expert_ffn_workspace_size": (["i64", "i32", "i32", "i32"], "sz"),
+    "do_expert_ffn": (["p", "p", "p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i32", "p", "p", "p", "sz",
+                       "p"], "i32"),
     "do_expert_up_backward_workspace_size": (["i64", "i32", "i32"], "sz"),
     "do_expert_up_backward": (["p", "p", "p", "p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i32", "p", "p",
                                "p", "p", "p", "sz", "p"], "i32"),

@@ -25,44 +25,51 @@ from . import doloss as dl
 
 _flags_lock = threading.Lock()
 _flags: dict[int, torch.Tensor] = {}
+_flag_ptrs: dict[int, int] = {}
 
 
-def _status(t: torch.Tensor) -> torch.Tensor:
-    """The device's status word, which every call on it may set (see device_status)."""
-    f = _flags.get(t.device.index)
-    if f is None:
+def _status(device: int) -> int:
+    """Address of the device's status word, which every call on it may set."""
+    p = _flag_ptrs.get(device)
+    if p is None:
         with _flags_lock:
-            f = _flags.get(t.device.index)
-            if f is None:
-                f = torch.zeros(64, dtype=torch.int32, device=t.device)
-                torch.cuda.synchronize(t.device)  # cleared for every stream
-                _flags[t.device.index] = f
-    return f
+            f = torch.zeros(64, dtype=torch.int32, device=f"cuda:{device}")
+            torch.cuda.synchronize(device)  # cleared for every stream
+            _flags.setdefault(device, f)
+            p = _flag_ptrs.setdefault(device, _flags[device].data_ptr())
+    return p
 
 
 def device_status(device="cuda") -> int:
     """Synchronizes the current stream, returns and clears what the calls of this
     module recorded on the device: 0, DO_ERR_TIMEOUT or DO_ERR_INVALID_ARG (a
     row or position outside its matrix, left out)."""
-    f = _status(torch.empty(0, device=device))
-    return int(dl.lib().do_device_status(f.data_ptr(), dl._stream(f)))
+    t = torch.empty(0, device=device)
+    return int(dl.lib().do_device_status(_status(t.get_device()), dl._stream(t)))
 
 
-def _bf16(name: str, t: torch.Tensor, dim: int) -> None:
-    if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != dim or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA bfloat16 tensor of {dim} dimensions")
+_raw_stream = torch._C._cuda_getCurrentRawStream if torch.cuda.is_available() else None
 
 
-def _index(name: str, t, n: int) -> None:
-    if t is not None and (t.dtype != torch.int32 or not t.is_cuda or t.numel() != n
-                          or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous CUDA int32 tensor of {n} values")
+def _bf16(name: str, t: torch.Tensor, dim: int, device: int) -> None:
+    if t.dtype is not torch.bfloat16 or t.dim() != dim or not t.is_contiguous() or t.get_device() != device \
+            or device < 0:
+        raise ValueError(f"{name} must be a contiguous CUDA bfloat16 tensor of {dim} dimensions, "
+                         "all tensors on one device")
 
 
-def _same_device(a: torch.Tensor, *others) -> None:
-    for t in others:
-        if t is not None and t.device != a.device:
-            raise ValueError("all tensors must be on one device")
+def _index(name: str, t, n: int, device: int) -> None:
+    if t is not None and (t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous()
+                          or t.get_device() != device):
+        raise ValueError(f"{name} must be a contiguous CUDA int32 tensor of {n} values, "
+                         "all tensors on one device")
+
+
+def _fp32(name: str, t, shape: tuple, device: int) -> None:
+    if t is not None and (t.dtype is not torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()
+                          or t.get_device() != device):
+        raise ValueError(f"{name} must be a contiguous CUDA float32 tensor of shape {list(shape)}, "
+                         "all tensors on one device")
 
 
 class Checkpoint:
@@ -76,18 +83,18 @@ class Checkpoint:
         self.codes = codes
         self.exponents = exponents
 
-    def check(self, R: int, F: int) -> None:
+    def check(self, R: int, F: int, device: int) -> None:
         c, e = self.codes, self.exponents
-        if (c.dtype != torch.int8 or e.dtype != torch.uint8 or tuple(c.shape) != (R, 2 * F)
-                or e.numel() * 16 != c.numel() or not (c.is_cuda and e.is_cuda)
-                or not (c.is_contiguous() and e.is_contiguous())):
+        if (c.dtype is not torch.int8 or e.dtype is not torch.uint8 or tuple(c.shape) != (R, 2 * F)
+                or e.numel() * 16 != c.numel() or c.get_device() != device or e.get_device() != device
+                or device < 0 or not (c.is_contiguous() and e.is_contiguous())):
             raise ValueError("a checkpoint holds contiguous CUDA codes int8 [R,2F] and exponents "
-                             "uint8 [R,2F/16]")
+                             "uint8 [R,2F/16], all tensors on one device")
 
     def values(self) -> torch.Tensor:
         """The values it stands for, bf16 [R, 2F] (7 significant bits: exact)."""
         R, n = self.codes.shape
-        self.check(R, n // 2)
+        self.check(R, n // 2, self.codes.get_device())
         out = torch.empty(R, n, dtype=torch.bfloat16, device=self.codes.device)
         if R:
             dl._check("do_checkpoint_values", dl.lib().do_checkpoint_values(
@@ -108,16 +115,16 @@ def expert_up(x: torch.Tensor, w1: torch.Tensor, offsets: torch.Tensor,
     """do_expert_up: act [R,F] bf16 = silu(z_gate) * z_up with z = x[rows] W1^T
     of each row's expert, and with `checkpoint` the Checkpoint of z (else None).
     rows [R] None: the R rows of x are in dispatch order."""
-    _bf16("x", x, 2)
-    _bf16("w1", w1, 3)
+    dev = x.get_device()
+    _bf16("x", x, 2, dev)
+    _bf16("w1", w1, 3, dev)
     T, H = x.shape
     E, F2, Hw = w1.shape
     if Hw != H or F2 % 2:
         raise ValueError("w1 must be [E, 2F, H] for x [T, H]")
-    _same_device(x, w1, offsets, rows)
     R = T if rows is None else rows.numel()
-    _index("offsets", offsets, E + 1)
-    _index("rows", rows, R)
+    _index("offsets", offsets, E + 1, dev)
+    _index("rows", rows, R, dev)
     F = F2 // 2
     act = torch.empty(R, F, dtype=torch.bfloat16, device=x.device)
     kept = None
@@ -128,7 +135,7 @@ def expert_up(x: torch.Tensor, w1: torch.Tensor, offsets: torch.Tensor,
         dl._check("do_expert_up", dl.lib().do_expert_up(
             x.data_ptr(), w1.data_ptr(), dl._ptr(rows), offsets.data_ptr(), T, H, F, E, R,
             act.data_ptr(), kept.codes.data_ptr() if kept else None,
-            kept.exponents.data_ptr() if kept else None, _status(x).data_ptr(), dl._stream(x)))
+            kept.exponents.data_ptr() if kept else None, _status(dev), _raw_stream(dev)))
     return act, kept
 
 
@@ -145,19 +152,19 @@ def grouped_matmul(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     """do_grouped_matmul: y [R,N] bf16, row r = a[rows[r]] (or a[r]) times the
     weights of its expert: w [E,N,K] (y = a w^T), or [E,K,N] where transposed
     (y = a w)."""
-    _bf16("a", a, 2)
-    _bf16("w", w, 3)
+    dev = a.get_device()
+    _bf16("a", a, 2, dev)
+    _bf16("w", w, 3, dev)
     E, N, K = _weights(a, w, transposed)
-    _same_device(a, w, offsets, rows)
     T = a.shape[0]
     R = T if rows is None else rows.numel()
-    _index("offsets", offsets, E + 1)
-    _index("rows", rows, R)
+    _index("offsets", offsets, E + 1, dev)
+    _index("rows", rows, R, dev)
     y = torch.empty(R, N, dtype=torch.bfloat16, device=a.device)
     if R:
         dl._check("do_grouped_matmul", dl.lib().do_grouped_matmul(
             a.data_ptr(), w.data_ptr(), dl._ptr(rows), offsets.data_ptr(), T, K, N, E, R,
-            int(bool(transposed)), y.data_ptr(), _status(a).data_ptr(), dl._stream(a)))
+            int(bool(transposed)), y.data_ptr(), _status(dev), _raw_stream(dev)))
     return y
 
 
@@ -166,18 +173,16 @@ def grouped_matmul_join(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     """do_grouped_matmul_join: out [T,N] bf16, the products of grouped_matmul on
     the rows a [T*k,K] in dispatch order, summed per token over its rows
     pos [T,k] with weights [T,k] fp32 (None: one each)."""
-    _bf16("a", a, 2)
-    _bf16("w", w, 3)
+    dev = a.get_device()
+    _bf16("a", a, 2, dev)
+    _bf16("w", w, 3, dev)
     E, N, K = _weights(a, w, transposed)
-    _same_device(a, w, offsets, pos, weights)
     if pos.dim() != 2 or pos.numel() != a.shape[0]:
         raise ValueError("pos must be [T, k] for a [T*k, K]")
     T, k = pos.shape
-    _index("offsets", offsets, E + 1)
-    _index("pos", pos, T * k)
-    if weights is not None and (weights.dtype != torch.float32 or weights.shape != pos.shape
-                                or not weights.is_contiguous()):
-        raise ValueError("weights must be a contiguous float32 tensor shaped like pos")
+    _index("offsets", offsets, E + 1, dev)
+    _index("pos", pos, T * k, dev)
+    _fp32("weights", weights, (T, k), dev)
     out = torch.empty(T, N, dtype=torch.bfloat16, device=a.device)
     if T:
         L = dl.lib()
@@ -185,8 +190,8 @@ def grouped_matmul_join(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
                          device=a.device)
         dl._check("do_grouped_matmul_join", L.do_grouped_matmul_join(
             a.data_ptr(), w.data_ptr(), offsets.data_ptr(), pos.data_ptr(), dl._ptr(weights), T, k,
-            K, N, E, int(bool(transposed)), out.data_ptr(), _status(a).data_ptr(), ws.data_ptr(),
-            ws.numel(), dl._stream(a)))
+            K, N, E, int(bool(transposed)), out.data_ptr(), _status(dev), ws.data_ptr(),
+            ws.numel(), _raw_stream(dev)))
     return out
 
 
@@ -197,22 +202,22 @@ def expert_up_backward(dout: torch.Tensor, w2: torch.Tensor, kept: Checkpoint,
     through the join, the down projection w2 [E,H,F] and the activation, from
     the 8-bit checkpoint.  Returns (dz [R,2F] bf16, act [R,F] bf16 times each
     row's combine weight, the operand of dW2, dcombine [T,k] fp32)."""
-    _bf16("dout", dout, 2)
-    _bf16("w2", w2, 3)
+    dev = dout.get_device()
+    _bf16("dout", dout, 2, dev)
+    _bf16("w2", w2, 3, dev)
     T, H = dout.shape
     E, Hw, F = w2.shape
     if Hw != H:
         raise ValueError("w2 must be [E, H, F] for dout [T, H]")
-    if combine.dim() != 2 or combine.shape[0] != T or combine.dtype != torch.float32 \
-            or not combine.is_contiguous():
-        raise ValueError("combine must be a contiguous float32 tensor of shape [T, k]")
+    if combine.dim() != 2:
+        raise ValueError("combine must be [T, k]")
     k = combine.shape[1]
     R = T * k
-    _same_device(dout, w2, combine, offsets, rows, pos, kept.codes, kept.exponents)
-    _index("offsets", offsets, E + 1)
-    _index("rows", rows, R)
-    _index("pos", pos, R)
-    kept.check(R, F)
+    _fp32("combine", combine, (T, k), dev)
+    _index("offsets", offsets, E + 1, dev)
+    _index("rows", rows, R, dev)
+    _index("pos", pos, R, dev)
+    kept.check(R, F, dev)
     dz = torch.empty(R, 2 * F, dtype=torch.bfloat16, device=dout.device)
     act = torch.empty(R, F, dtype=torch.bfloat16, device=dout.device)
     dcombine = torch.empty(T, k, dtype=torch.float32, device=dout.device)
@@ -223,8 +228,8 @@ def expert_up_backward(dout: torch.Tensor, w2: torch.Tensor, kept: Checkpoint,
         dl._check("do_expert_up_backward", L.do_expert_up_backward(
             dout.data_ptr(), w2.data_ptr(), kept.codes.data_ptr(), kept.exponents.data_ptr(),
             combine.data_ptr(), rows.data_ptr(), offsets.data_ptr(), pos.data_ptr(), T, k, H, F, E,
-            dz.data_ptr(), act.data_ptr(), dcombine.data_ptr(), _status(dout).data_ptr(),
-            ws.data_ptr(), ws.numel(), dl._stream(dout)))
+            dz.data_ptr(), act.data_ptr(), dcombine.data_ptr(), _status(dev), ws.data_ptr(),
+            ws.numel(), _raw_stream(dev)))
     return dz, act, dcombine
 
 
@@ -234,30 +239,29 @@ def grouped_weight_grad(p: torch.Tensor, q: torch.Tensor, offsets: torch.Tensor,
     """do_grouped_weight_grad: dw [E,M,N] fp32, dw[e] = sum over the expert's rows
     r of p[p_rows[r]]^T q[q_rows[r]] (p [.,M], q [.,N] bf16; rows None: r itself).
     With accumulate it is added to `out`."""
-    _bf16("p", p, 2)
-    _bf16("q", q, 2)
-    _same_device(p, q, offsets, p_rows, q_rows, out)
+    dev = p.get_device()
+    _bf16("p", p, 2, dev)
+    _bf16("q", q, 2, dev)
     sizes = {t.numel() for t in (p_rows, q_rows) if t is not None}
     sizes |= {t.shape[0] for t, r in ((p, p_rows), (q, q_rows)) if r is None}
     if len(sizes) != 1:
         raise ValueError("p and q must have one row (or row index) for each routed row")
     R = sizes.pop()
     E, M, N = offsets.numel() - 1, p.shape[1], q.shape[1]
-    _index("offsets", offsets, E + 1)
-    _index("p_rows", p_rows, R)
-    _index("q_rows", q_rows, R)
+    _index("offsets", offsets, E + 1, dev)
+    _index("p_rows", p_rows, R, dev)
+    _index("q_rows", q_rows, R, dev)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the out to add to")
         out = torch.empty(E, M, N, dtype=torch.float32, device=p.device)
-    if tuple(out.shape) != (E, M, N) or out.dtype != torch.float32 or not out.is_contiguous():
-        raise ValueError("out must be a contiguous float32 tensor of shape [E, M, N]")
+    _fp32("out", out, (E, M, N), dev)
     if R == 0:
         return out if accumulate else out.zero_()
     dl._check("do_grouped_weight_grad", dl.lib().do_grouped_weight_grad(
         p.data_ptr(), q.data_ptr(), dl._ptr(p_rows), dl._ptr(q_rows), offsets.data_ptr(),
         p.shape[0], q.shape[0], M, N, E, R, int(bool(accumulate)), out.data_ptr(),
-        _status(p).data_ptr(), dl._stream(p)))
+        _status(dev), _raw_stream(dev)))
     return out
 
 
@@ -305,5 +309,27 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     the weights' gradients are added to instead of being returned."""
     if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w2, combine)):
         return _ExpertFFN.apply(x, w1, w2, combine, offsets, rows, pos, main_grads)
-    act, _ = expert_up(x, w1, offsets, rows)
-    return grouped_matmul_join(act, w2, offsets, pos, combine)
+    dev = x.get_device()
+    _bf16("x", x, 2, dev)
+    _bf16("w1", w1, 3, dev)
+    _bf16("w2", w2, 3, dev)
+    T, H = x.shape
+    E, F2, Hw = w1.shape
+    F = F2 // 2
+    if Hw != H or F2 % 2 or tuple(w2.shape) != (E, H, F) or combine.dim() != 2:
+        raise ValueError("w1 must be [E, 2F, H], w2 [E, H, F] and combine [T, k] for x [T, H]")
+    k = combine.shape[1]
+    _fp32("combine", combine, (T, k), dev)
+    _index("offsets", offsets, E + 1, dev)
+    _index("rows", rows, T * k, dev)
+    _index("pos", pos, T * k, dev)
+    out = torch.empty(T, H, dtype=torch.bfloat16, device=x.device)
+    if T and k:
+        L = dl.lib()
+        n = L.do_expert_ffn_workspace_size(T, k, H, F)
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+        dl._check("do_expert_ffn", L.do_expert_ffn(
+            x.data_ptr(), w1.data_ptr(), w2.data_ptr(), combine.data_ptr(), rows.data_ptr(),
+            offsets.data_ptr(), pos.data_ptr(), T, k, H, F, E, out.data_ptr(), _status(dev),
+            ws.data_ptr(), n, _raw_stream(dev)))
+    return out
