@@ -47,7 +47,7 @@ cudaError_t launch_product(ProductMode mode, const ProductArgs &a, cudaStream_t 
 
 // The products of at most kFewRows routed rows without checkpoint, weights as they
 // are (not transposed), and the joined ones, where out is [T][N] (experts_few.cu).
-constexpr int64_t kFewRows = 32;
+constexpr int64_t kFewRows = 24;
 cudaError_t launch_few_product(ProductMode mode, const ProductArgs &a, cudaStream_t s);
 cudaError_t launch_few_join(const ProductArgs &a, const int *pos, const float *weights, int64_t T, int k,
                             cudaStream_t s);

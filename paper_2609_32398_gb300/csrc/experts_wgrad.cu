@@ -30,7 +30,7 @@ constexpr uint32_t kSide = 2 * kBlockBytes;     // a CTA's 128 columns of one op
 constexpr uint32_t kStage = 2 * kSide;
 constexpr int kStages = 6;
 constexpr uint32_t kOut = 32 * 128;             // an epilogue warp's 32 x 32 block
-constexpr uint32_t kSmem = 1024 + kStages * kStage + kEpiWarps * kOut;
+constexpr uint32_t kSmem = 1024 + kStages * kStage + kEpiWarps * 2 * kOut;
 static_assert(kSmem <= 232448 - 2048, "shared memory");
 static_assert(kStages == kLoadWarps, "a gathering warp has one stage of its own");
 
@@ -272,7 +272,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     } else {
         // ---------------------------------------------------------- epilogue
         const int quad = warp & 3, part = (warp - 2) >> 2;
-        unsigned char *mine = smem + kStages * kStage + (warp - 2) * kOut;
+        unsigned char *both = smem + kStages * kStage + (warp - 2) * 2 * kOut;
+        int block = 0;  // blocks written by this warp: two places in turn
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
         int done = 0;
         for (bool more = w.find(); more; more = w.next()) {
@@ -297,7 +298,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 32; ++i) r[i] = 0u;
                 }
-                if (lane == 0) bulk_wait_read<0>();  // the last block has left
+                unsigned char *mine = both + (block++ & 1) * kOut;
+                if (lane == 0) bulk_wait_read<1>();  // the last block but one has left
                 __syncwarp();
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
