@@ -124,15 +124,64 @@ __device__ __forceinline__ float q8_scale(int e) {
 __device__ __forceinline__ unsigned q8_code(float v, float inv) {
     return __float_as_uint(fmaf(v, inv, 12582912.0f)) & 0xffu;
 }
-// Code of byte b (0..3) of a word as a float: the byte with its sign bit turned over is
-// code + 128 in the low bits of 2^23 (the conversion instruction shares its pipe with
-// sigma's exponential and division and is four times slower).
-__device__ __forceinline__ float q8_value(unsigned word, int b) {
-    return __uint_as_float(__byte_perm(word ^ 0x80808080u, 0x4b000000u, 0x7440u + (unsigned)b)) - 8388736.0f;
+// Two fp32 values that one instruction works on (the epilogues are bound by how many
+// instructions they issue).
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair2(float lo, float hi) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split2(f32x2 v, float &lo, float &hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 
-// sigma(z) = 1 / (1 + e^-z): e^-z overflows to infinity below -88 and gives 0.
-__device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// sigma(z) = 1 / (1 + 2^(-z log2 e)) of both: 2^x overflows to infinity below z = -88
+// and gives 0.
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 z) {
+    float a, b;
+    split2(mul2(z, pair2(-1.44269504f, -1.44269504f)), a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    split2(add2(pair2(a, b), pair2(1.0f, 1.0f)), a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return pair2(a, b);
+}
+
+__device__ __forceinline__ float sigmoid_f(float z) {
+    float a, b;
+    split2(sigmoid2(pair2(z, z)), a, b);
+    return a;
+}
+
+// The codes of bytes b and b + 1 of a word, sign bits turned over beforehand (word ^
+// 0x80808080), times the block's scale: such a byte below the exponent of 2^23 is
+// 2^23 + 128 + code, and one fused multiply-add takes the rest off exactly.  (The
+// conversion instruction shares its pipe with sigma's exponential and division.)
+__device__ __forceinline__ f32x2 q8_values(unsigned word, int b, f32x2 scale, f32x2 offset) {
+    const float lo = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440u + (unsigned)b));
+    const float hi = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440u + (unsigned)b + 1u));
+    return fma2(pair2(lo, hi), scale, offset);
+}
+__device__ __forceinline__ f32x2 q8_offset(float scale) {
+    return pair2(-8388736.0f * scale, -8388736.0f * scale);
+}
 
 __device__ __forceinline__ unsigned pack2(float lo, float hi) {
     __nv_bfloat162 p = __float22bfloat162_rn(make_float2(lo, hi));

@@ -132,12 +132,16 @@ checkpoint_values_kernel(const uint4 *__restrict__ codes, const uint8_t *__restr
     pdl_wait();
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < blocks; i += (int64_t)gridDim.x * 256) {
         const uint4 c = __ldg(codes + i);
-        const float s = q8_scale(__ldg(exponents + i));
-        const unsigned u[4] = {c.x, c.y, c.z, c.w};
+        const float scale = q8_scale(__ldg(exponents + i));
+        const f32x2 s = pair2(scale, scale), off = q8_offset(scale);
+        const unsigned u[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
         unsigned o[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            o[j] = pack2(q8_value(u[j / 2], 2 * (j & 1)) * s, q8_value(u[j / 2], 2 * (j & 1) + 1) * s);
+        for (int j = 0; j < 8; ++j) {
+            float lo, hi;
+            split2(q8_values(u[j / 2], 2 * (j & 1), s, off), lo, hi);
+            o[j] = pack2(lo, hi);
+        }
         values[2 * i] = make_uint4(o[0], o[1], o[2], o[3]);
         values[2 * i + 1] = make_uint4(o[4], o[5], o[6], o[7]);
     }

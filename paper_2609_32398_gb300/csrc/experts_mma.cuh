@@ -1,6 +1,6 @@
 // PTX of the CTA-pair kernels of the expert operators: thread-block clusters of
-// two, tcgen05 with cta_group::2 (one accumulator of 256 rows over two SMs), and
-// the copies that gather rows.
+// two, tcgen05 with cta_group::2 (one accumulator of 256 rows over two SMs) and
+// row-gathering TMA loads.
 #pragma once
 
 #include "experts.cuh"
@@ -30,8 +30,8 @@ __device__ __forceinline__ uint32_t map_to_rank(const void *p, uint32_t rank) {
 // this CTA's shared memory or TMEM and has been completed and fenced by the caller
 // (a proxy fence after the copies' wait, or tcgen05.wait and its fence), and the tensor
 // core that uses it next is this SM's own, so that the arrival need not be a release
-// over the cluster: that one waits for every access in flight, and made a step of the
-// ring cost 690 ns instead of 270.
+// over the cluster: that one waits for every access of the thread in flight, and made a
+// step of a ring of copies cost 690 ns instead of 270.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
@@ -135,27 +135,42 @@ __device__ __forceinline__ void pair_load_5d(uint32_t dst, const CUtensorMap *ma
         : "memory");
 }
 
+// Four rows of a bf16 matrix (64 columns from x on) into four consecutive 128-byte rows;
+// a row outside the matrix reads as zeros.
+__device__ __forceinline__ void pair_gather4(uint32_t dst, const CUtensorMap *map, int x, int4 r, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.cta_group::2"
+        " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "r"(bar)
+        : "memory");
+}
+
 // 16 bytes global -> shared, zeros where !in (nothing is read then).
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool in) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
 }
-// Where rows are gathered, warp w of a CTA's kLoadWarps gathering warps fills the
-// steps w, w + kLoadWarps, ... of the ring alone, in 16-byte pieces, and then tells
-// the pair's first CTA: as many steps are under way as there are warps.  The ring
-// has at least kLoadWarps stages: a warp that has finished step m - kLoadWarps knows
-// step m - kLoadWarps - stages to be consumed, so that a stage's barrier is at most
-// one phase behind what it waits for, which a parity can tell.  (Rows
-// gathered by TMA, four a copy, took 85 to 100 cycles a copy of 512 bytes, five
-// times the products' time; the arrivals of 128 threads a step on one barrier took
-// twice the products' time.)
-constexpr int kLoadWarps = 6;
-
+// A warp's copies of a step are done and visible to the tensor cores: tells the pair.
 __device__ __forceinline__ void gathered(uint32_t full_addr, int lane) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive_cluster(full_addr);
 }
+
+// Where rows are gathered, warp w of a CTA's kLoadWarps gathering warps brings the steps
+// w, w + kLoadWarps, ... of the ring alone.
+//  - The products do it with TMA copies of four rows.  Such a copy takes its thread 85 to
+//    100 cycles to issue, and a step has 32: one warp took five times the products' time,
+//    six warps a step each take as long as the products do.  cp.async in 16-byte pieces
+//    takes the same where the epilogue is light, and 15% more where it stores much (105
+//    against 90 us for 103 GFLOP at K = 1024).
+//  - The weight gradients do it with cp.async: their results leave by TMA, which the
+//    four-row copies then hold up (dW1 at 16384 tokens, H = 2048: 653 us against 742; 697
+//    with plain stores).
+// The ring has at least kLoadWarps stages: a warp at step m has waited for step m -
+// kLoadWarps - stages to be consumed, so that a stage's barrier is at most one phase
+// behind what it waits for, which a parity can tell.
+constexpr int kLoadWarps = 6;
 
 __device__ __forceinline__ void tma_reduce_add_3d(const CUtensorMap *map, const void *src, int x, int y, int z) {
     asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::
@@ -215,6 +230,8 @@ __device__ __forceinline__ int divide_by(int i, uint32_t magic) {
 }
 
 // Host: the pair kernels' tensor maps (128-byte swizzle, zero outside the tensor).
+// Rows of a bf16 matrix, gathered four at a time, 64 columns each.
+bool encode_gather_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols);
 // W1 [E][2F][H] as [E][F/16][2][16][H], box 1 x 4 x 2 x 16 x 64: 64 columns of 64
 // gate rows and their 64 up rows, 16 of each in turn.
 bool encode_gate_up_map(CUtensorMap *map, const void *base, uint64_t E, uint64_t F, uint64_t H);

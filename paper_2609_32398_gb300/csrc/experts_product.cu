@@ -15,13 +15,13 @@
 // 2 x 256 TMEM columns, so that one tile's epilogue runs under the next tile's
 // products) takes tiles in a fixed order.  Per 64-wide step of k each CTA loads
 // its 128 weight rows by TMA (one box, or two where the weights are read through
-// their other side) and half of the routed rows: by TMA where they lie in dispatch
-// order, and gathered by their row ids in 16-byte pieces otherwise, so that no
+// their other side) and half of the routed rows: in one box where they lie in
+// dispatch order, and gathered four at a time by their row ids otherwise, so that no
 // permuted copy of the tokens exists.  What a tile holds past its group's end ends
 // in accumulator columns that nobody reads.
 //
 // Warps: 0 weights by TMA, 1 issues the MMAs (first CTA), then the epilogue's, then
-// six that gather rows or one that loads them by TMA.  A TMEM lane is a
+// six that gather rows or one that loads them in boxes.  A TMEM lane is a
 // weight row and a register a routed row, so each epilogue warp turns 32 x 32
 // blocks in shared memory (16-byte pieces xor-swizzled: no bank conflicts) and
 // then has 32 columns of one routed row in a thread, where the activation, the
@@ -141,15 +141,20 @@ __device__ __forceinline__ unsigned finish_up(const ProductArgs &p, int64_t r, i
         *reinterpret_cast<uint4 *>(at + F) = u;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = v[i] * sigmoid_f(v[i]) * v[16 + i];
+    for (int i = 0; i < 16; i += 2) {
+        const f32x2 g = pair2(v[i], v[i + 1]);
+        split2(mul2(mul2(g, sigmoid2(g)), pair2(v[16 + i], v[17 + i])), v[i], v[i + 1]);
+    }
     store16(p.out + r * F + c0, v);
     return (unsigned)eg | (unsigned)eu << 8;
 }
 
-// What finish_grad reads of its row, ahead of the products.
+// What finish_grad reads of its row, as it lies in memory: nothing waits for these loads
+// before finish_grad does.
 struct Kept {
     uint4 gate, up;
-    float gate_scale, up_scale, weight;
+    unsigned gate_exponent, up_exponent;
+    float weight;
 };
 __device__ __forceinline__ Kept read_kept(const ProductArgs &p, int64_t r, int c0) {
     Kept k = {};
@@ -157,34 +162,53 @@ __device__ __forceinline__ Kept read_kept(const ProductArgs &p, int64_t r, int c
         const int64_t cg = r * 2 * p.N + c0, cu = cg + p.N;
         k.gate = __ldg(reinterpret_cast<const uint4 *>(p.codes + cg));
         k.up = __ldg(reinterpret_cast<const uint4 *>(p.codes + cu));
-        k.gate_scale = q8_scale(__ldg(p.exponents + cg / kQBlock));
-        k.up_scale = q8_scale(__ldg(p.exponents + cu / kQBlock));
+        k.gate_exponent = __ldg(p.exponents + cg / kQBlock);
+        k.up_exponent = __ldg(p.exponents + cu / kQBlock);
         k.weight = __ldg(p.row_weight + r);
     }
     return k;
 }
+// The checkpoint of a tile's 128 columns on their way to the L2: up to 256 rows, two
+// lines of codes each and the exponents beside them, over 256 threads.
+__device__ __forceinline__ void prefetch_kept(const ProductArgs &p, const Tile &tl, int c0, int thread) {
+    for (int i = thread; i < 2 * tl.n; i += 256) {
+        const int64_t at = (int64_t)(tl.r0 + (i >> 1)) * 2 * p.N + (i & 1) * p.N + c0;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.codes + at));
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.exponents + at / kQBlock));
+    }
+}
+
 // Returns the sum of g act over the 16 columns.
 __device__ __forceinline__ float finish_grad(const ProductArgs &p, int64_t r, int c0, const float (&v)[16],
                                              const Kept &k) {
     const int F = p.N;
     if (c0 >= F) return 0.0f;
-    const unsigned ug[4] = {k.gate.x, k.gate.y, k.gate.z, k.gate.w}, uu[4] = {k.up.x, k.up.y, k.up.z, k.up.w};
-    float sum = 0.0f, dg[16], du[16], act[16];
+    const unsigned flip = 0x80808080u;
+    const unsigned ug[4] = {k.gate.x ^ flip, k.gate.y ^ flip, k.gate.z ^ flip, k.gate.w ^ flip};
+    const unsigned uu[4] = {k.up.x ^ flip, k.up.y ^ flip, k.up.z ^ flip, k.up.w ^ flip};
+    const float gate_scale = q8_scale((int)k.gate_exponent), up_scale = q8_scale((int)k.up_exponent);
+    const f32x2 sg = pair2(gate_scale, gate_scale), su = pair2(up_scale, up_scale);
+    const f32x2 og = q8_offset(gate_scale), ou = q8_offset(up_scale);
+    const f32x2 w = pair2(k.weight, k.weight), one = pair2(1.0f, 1.0f), minus = pair2(-1.0f, -1.0f);
+    f32x2 sum = pair2(0.0f, 0.0f);
+    float dg[16], du[16], act[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float zg = q8_value(ug[i / 4], i & 3) * k.gate_scale, zu = q8_value(uu[i / 4], i & 3) * k.up_scale;
-        const float s = sigmoid_f(zg), g = v[i];
-        const float silu = zg * s, a = silu * zu, gw = g * k.weight;
-        sum = fmaf(g, a, sum);
-        du[i] = gw * silu;
-        dg[i] = gw * zu * fmaf(silu, 1.0f - s, s);
-        act[i] = a * k.weight;
+    for (int i = 0; i < 16; i += 2) {
+        const f32x2 zg = q8_values(ug[i / 4], i & 3, sg, og), zu = q8_values(uu[i / 4], i & 3, su, ou);
+        const f32x2 s = sigmoid2(zg), g = pair2(v[i], v[i + 1]);
+        const f32x2 silu = mul2(zg, s), a = mul2(silu, zu), gw = mul2(g, w);
+        sum = fma2(g, a, sum);
+        split2(mul2(gw, silu), du[i], du[i + 1]);
+        split2(mul2(mul2(gw, zu), fma2(silu, fma2(s, minus, one), s)), dg[i], dg[i + 1]);
+        split2(mul2(a, w), act[i], act[i + 1]);
     }
     bf16 *dz = p.dz + r * 2 * F + c0, *out = p.out + r * F + c0;
     store16(dz, dg);
     store16(dz + F, du);
     store16(out, act);
-    return sum;
+    float lo, hi;
+    split2(sum, lo, hi);
+    return lo + hi;
 }
 
 template <int kMode, bool kGather, bool kTransposed>
@@ -207,7 +231,7 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < stages; ++i) {
-            mbar_init(&full[i], kGather ? 3 : 1);
+            mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -265,12 +289,12 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     if (warp == 0) {
         // ---------------------------------------------------------- weights
         if (lane == 0) {
-            const uint32_t bytes = 2u * (kABytes + (kGather ? 0u : a.b_bytes));
             Ring at{0, 0};
             bool good = true;
             int it = 0;
             for (bool any = walk.find(); good && any; any = walk.next()) {
                 const int m0 = tl.m * 256 + (int)rank * 128, mb = tl.m * 8 + (int)rank * 4;
+                const uint32_t bytes = 2u * (kABytes + (kGather ? (uint32_t)tl.width * 64u : a.b_bytes));
                 for (int k = 0; k < p.K; k += 64, ++it) {
                     good = pair_wait(empty0 + 8 * at.s, at.phase ^ 1u, p.status, abort);
                     if (!good) break;
@@ -316,63 +340,46 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         __syncwarp();
     } else if (kGather && warp >= kFirstLoader) {
         // ---------------------------------------------------------- gather
-        // Eight lanes copy the 128 bytes of a row, four rows at a time.
-        const int piece = lane & 7, row = lane >> 3;
-        const uint32_t base = ring + kABytes + (uint32_t)(row * 128);
-        const uint32_t swz[2] = {(uint32_t)((piece ^ row) << 4), (uint32_t)((piece ^ (row + 4)) << 4)};
-        int id[4];  // of this CTA's routed rows lane + 32 j; outside the matrix: recorded and -1
+        // Lane l copies this CTA's routed rows 4 l .. 4 l + 3 of the tile.
+        const int none = (int)p.a_rows;
+        int4 ids;
         auto read_ids = [&]() {
             const int half = tl.width / 2;
+            int v[4];
             bool bad = false;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int n = (int)rank * half + lane + 32 * j;
-                id[j] = lane + 32 * j < half && n < tl.n ? __ldg(p.rows + tl.r0 + n) : 0;
+                const int n = (int)rank * half + 4 * lane + j;
+                v[j] = 4 * lane < half && n < tl.n ? __ldg(p.rows + tl.r0 + n) : none;
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int n = (int)rank * half + lane + 32 * j;
-                const bool in = lane + 32 * j < half && n < tl.n, out = id[j] < 0 || id[j] >= p.a_rows;
-                bad |= in && out;
-                if (!in || out) id[j] = -1;
+                const int n = (int)rank * half + 4 * lane + j;
+                const bool out = v[j] < 0 || v[j] >= none;
+                bad |= out && 4 * lane < half && n < tl.n;
+                if (out) v[j] = none;
             }
             if (bad && p.status) atomicOr(p.status, kDevBadId);
+            ids = make_int4(v[0], v[1], v[2], v[3]);
         };
         int it = 0, mine = warp - kFirstLoader;  // steps so far, this warp's next one
         bool good = true, any = walk.find();
         if (any) read_ids();
         while (good && any) {
             const int half = tl.width / 2, end = it + steps;
-            int src[32];  // of this lane's rows row + 4 j
-#pragma unroll
-            for (int j = 0; j < 32; ++j) src[j] = __shfl_sync(kFull, id[j >> 3], (4 * j + row) & 31);
-            bool ahead = false;
             for (; mine < end; mine += kLoadWarps) {
-                const int s = mine % stages, c = 64 * (mine - it) + 8 * piece;
+                const int s = mine % stages;
                 if (mine >= stages) {
                     good = pair_wait_warp(empty0 + 8 * s, (uint32_t)(mine / stages - 1) & 1u, p.status, abort, lane);
                     if (!good) break;
                 }
-                const uint32_t dst = base + (uint32_t)s * stage_bytes;
-                const bool inside = c < p.K;
-                const bf16 *from = p.A + c;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    if (4 * j >= half) break;
-                    const bool in = inside && src[j] >= 0;
-                    cp_async16(dst + j * 512 + swz[j & 1], in ? from + (int64_t)src[j] * p.K : p.A, in);
-                }
-                if (mine + kLoadWarps >= end) {  // the next tile's ids come under these copies
-                    any = walk.next();
-                    if (any) read_ids();
-                    ahead = true;
-                }
-                gathered(full_pair + 8 * s, lane);
+                if (4 * lane < half)
+                    pair_gather4(ring + (uint32_t)s * stage_bytes + kABytes + lane * 512, &amap, 64 * (mine - it), ids,
+                                 full_pair + 8 * s);
+                __syncwarp();
             }
-            if (!ahead) {  // no step of this tile was this warp's
-                any = walk.next();
-                if (any) read_ids();
-            }
+            any = walk.next();
+            if (any) read_ids();
             it = end;
         }
         __syncwarp();
@@ -429,6 +436,13 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             // up_grad: what the first rows want of the checkpoint comes under the products
             const int row = lane & 15, h = lane >> 4;
             const int cr = tl.m * 256 + (int)rank * 128 + quad * 32 + 16 * h;  // plain, up_grad: first column
+            if (kMode == kProductUpGrad) {
+                Walk ahead = walk;
+                if (ahead.next()) {
+                    const int c = ahead.tile.m * 256 + (int)rank * 128;
+                    if (c < p.N) prefetch_kept(p, ahead.tile, c, (warp - 2) * 32 + lane);
+                }
+            }
             Kept kept = {};
             if (kMode == kProductUpGrad && 16 * part + row < tl.n) kept = read_kept(p, tl.r0 + 16 * part + row, cr);
             const bool good = pair_wait_warp(smem_u32(&acc_full[buf]), (uint32_t)(done >> 1) & 1u, p.status, abort, lane);
@@ -556,7 +570,8 @@ cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
     // (and more of it) in small calls
     const uint32_t half = (uint32_t)(p.R < kTileN ? (p.R + 15) / 16 * 16 : kTileN) / 2;
     a.b_bytes = half * 128;
-    ok = ok && encode_tensor_map_3d_bf16(&amap, p.A, 1, (uint64_t)p.a_rows, K, 64, half);
+    ok = ok && (kGather ? encode_gather_map(&amap, p.A, (uint64_t)p.a_rows, K)
+                        : encode_tensor_map_3d_bf16(&amap, p.A, 1, (uint64_t)p.a_rows, K, 64, half));
     const int sms = sm_count();
     if (!ok || sms < 2) return cudaErrorInvalidValue;
     const uint32_t fixed = 1024 + kTurnAll + table_bytes(p.E) + 2048;
