@@ -170,7 +170,7 @@ do_status do_expert_ffn(const void *X, const void *W1, const void *W2, const flo
 
 size_t do_expert_up_backward_workspace_size(int64_t T, int32_t k, int32_t F) {
     if (T < 1 || k < 1 || F < 1 || T > INT32_MAX / k) return 0;
-    return dol::round256(sizeof(float) * (size_t)T * k * (1 + (size_t)(F + 31) / 32));
+    return dol::round256(sizeof(float) * (size_t)T * k * (1 + (size_t)(F + dol::kStrip - 1) / dol::kStrip));
 }
 
 do_status do_expert_up_backward(const void *dout, const void *W2, const void *codes, const void *exponents,
@@ -200,7 +200,7 @@ do_status do_expert_up_backward(const void *dout, const void *W2, const void *co
     a.strips = row_weight + R;
     cudaError_t e = dol::launch_row_weights(combine, pos, R, row_weight, status_flags, s);
     if (e == cudaSuccess) e = dol::launch_product(dol::kProductUpGrad, a, s);
-    if (e == cudaSuccess) e = dol::launch_strip_sums(a.strips, (F + 31) / 32, pos, offsets, E, R, dcombine, s);
+    if (e == cudaSuccess) e = dol::launch_strip_sums(a.strips, (F + dol::kStrip - 1) / dol::kStrip, pos, offsets, E, R, dcombine, s);
     return dol::of(e);
 }
 

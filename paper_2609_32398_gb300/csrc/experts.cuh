@@ -18,6 +18,9 @@ typedef __nv_bfloat16 bf16;
 // Values that share one exponent byte in an 8-bit checkpoint.
 constexpr int kQBlock = 16;
 
+// Columns of a partial sum of the combine weights' gradient.
+constexpr int kStrip = 128;
+
 enum ProductMode {
     kProductPlain = 0,   // Y[r][n] = sum_k A[r][k] W[n][k]
     kProductUp = 1,      // act[r][f] = silu(z[f]) z[F + f], and z in 8 bits
@@ -39,7 +42,7 @@ struct ProductArgs {
     uint8_t *exponents;    //                                           [R][2 F / 16]
     bf16 *dz;              // up_grad: [R][2 F]
     const float *row_weight;  // up_grad: [R]
-    float *strips;         // up_grad: [ceil(F / 32)][R], sums of g act over 32 columns
+    float *strips;         // up_grad: [ceil(F / kStrip)][R], sums of g act over kStrip columns
     int *status;
 };
 

@@ -22,10 +22,14 @@
 //
 // Warps: 0 weights by TMA, 1 issues the MMAs (first CTA), then the epilogue's, then
 // six that gather rows or one that loads them in boxes.  A TMEM lane is a
-// weight row and a register a routed row, so each epilogue warp turns 32 x 32
-// blocks in shared memory (16-byte pieces xor-swizzled: no bank conflicts) and
-// then has 32 columns of one routed row in a thread, where the activation, the
-// blocks' exponents and the sums over columns need no other thread.
+// weight row and a register a routed row; the four epilogue warps of a group turn
+// blocks of 16 routed rows x 128 columns (up: 32 x 64 of the gate and their up
+// values) in shared memory and deal the rows out among them, 16 columns a thread
+// and a row's columns over neighbouring threads: whole 128-byte lines are then read
+// and written where a warp's own 32 columns would be 64 bytes of each of 16 rows
+// (four times the passes through the SM's load-store pipe, which bound the gradient's
+// epilogue), and the activation and a block's exponent need no other thread.  The
+// 16-byte pieces are xor-swizzled: no bank conflicts either way.
 //
 // Every wait is bounded; one that runs out records kDevTimeout.
 #include <cstdint>
@@ -37,9 +41,9 @@ namespace {
 
 constexpr int kTileN = 256;               // routed rows of a tile at most
 // The epilogue's blocks take 16 KB in every mode, so that the ring has six stages of
-// 32 KB: four warps with 32 routed rows each, or, where a thread can do with 16 of a
-// row's 32 columns, eight warps with 16 (the gate and up values of a column are 16
-// TMEM lanes apart and want one thread).
+// 32 KB: one group of four warps with 32 routed rows at a time, or, where a thread can
+// do with 16 of a row's 32 values, two groups with 16 (the gate and up values of a
+// column are 16 TMEM lanes apart and want one thread).
 __host__ __device__ constexpr int epi_warps(int mode) { return mode == kProductUp ? 4 : 8; }
 __host__ __device__ constexpr int first_loader(int mode) { return 2 + epi_warps(mode); }
 __host__ __device__ constexpr int threads_of(int mode, bool gather) {
@@ -60,9 +64,8 @@ struct PairArgs {
 };
 
 // Shared memory: ring [stages][weights | rows], turn blocks [16 KB], and for each
-// expert its first tile [E + 1], first row [E + 1] and the width of its tiles [E + 1];
-// then, for the up projection, a tile's exponents [256][2][4].
-__host__ __device__ inline uint32_t table_bytes(int E) { return 4u * 3u * ((uint32_t)E + 1u) + 8u * kTileN; }
+// expert its first tile [E + 1], first row [E + 1] and the width of its tiles [E + 1].
+__host__ __device__ inline uint32_t table_bytes(int E) { return 4u * 3u * ((uint32_t)E + 1u); }
 __host__ __device__ inline uint32_t off_turn(int stages, uint32_t b_bytes) { return stages * (kABytes + b_bytes); }
 
 struct Tile {
@@ -129,16 +132,17 @@ __device__ __forceinline__ void finish_plain(const ProductArgs &p, int64_t r, in
             make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
 }
 
-// Returns the two exponents (gate, then up in the second byte).
-__device__ __forceinline__ unsigned finish_up(const ProductArgs &p, int64_t r, int c0, float (&v)[32]) {
+__device__ __forceinline__ void finish_up(const ProductArgs &p, int64_t r, int c0, float (&v)[32]) {
     const int F = p.N / 2;
-    if (c0 >= F) return 0;
-    int eg = 0, eu = 0;
+    if (c0 >= F) return;
     if (p.codes) {
+        int eg, eu;
         const uint4 g = quantise16(v, &eg), u = quantise16(v + 16, &eu);
-        int8_t *at = p.codes + r * p.N + c0;
-        *reinterpret_cast<uint4 *>(at) = g;
-        *reinterpret_cast<uint4 *>(at + F) = u;
+        const int64_t at = r * p.N + c0;
+        *reinterpret_cast<uint4 *>(p.codes + at) = g;
+        *reinterpret_cast<uint4 *>(p.codes + at + F) = u;
+        p.exponents[at / kQBlock] = (uint8_t)eg;
+        p.exponents[(at + F) / kQBlock] = (uint8_t)eu;
     }
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
@@ -146,7 +150,6 @@ __device__ __forceinline__ unsigned finish_up(const ProductArgs &p, int64_t r, i
         split2(mul2(mul2(g, sigmoid2(g)), pair2(v[16 + i], v[17 + i])), v[i], v[i + 1]);
     }
     store16(p.out + r * F + c0, v);
-    return (unsigned)eg | (unsigned)eu << 8;
 }
 
 // What finish_grad reads of its row, as it lies in memory: nothing waits for these loads
@@ -209,6 +212,34 @@ __device__ __forceinline__ float finish_grad(const ProductArgs &p, int64_t r, in
     float lo, hi;
     split2(sum, lo, hi);
     return lo + hi;
+}
+
+// Named barriers of a group of four epilogue warps.
+__device__ __forceinline__ void group_sync(int id) {
+    asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory");
+}
+__device__ __forceinline__ int group_and(int id, int ok) {
+    int all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.s32 q, %1, 0;\n\t"
+        "bar.red.and.pred p, %2, 128, q;\n\t"
+        "selp.s32 %0, 1, 0, p;\n\t}"
+        : "=r"(all)
+        : "r"(ok), "r"(id)
+        : "memory");
+    return all;
+}
+
+// Where 16-byte piece j of row i of warp q's block lies in its 128 bytes.
+__device__ __forceinline__ int turn_slot(int j, int i, int q) { return (j ^ q ^ ((i & 1) << 2)) << 4; }
+
+__device__ __forceinline__ void load4(float *v, const unsigned char *from) {
+    const float4 f = *reinterpret_cast<const float4 *>(from);
+    v[0] = f.x;
+    v[1] = f.y;
+    v[2] = f.z;
+    v[3] = f.w;
 }
 
 template <int kMode, bool kGather, bool kTransposed>
@@ -426,105 +457,73 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         __syncwarp();
     } else {
         // ---------------------------------------------------------- epilogue
-        const int quad = warp & 3, part = (warp - 2) >> 2;
-        unsigned char *mine = turn + (warp - 2) * (kTurnAll / kEpiWarps);
+        constexpr int kRows = kMode == kProductUp ? 32 : 16, kGroups = kEpiWarps / 4;
+        const int quad = warp & 3, group = (warp - 2) >> 2;
+        unsigned char *blocks = turn + group * (kTurnAll / kGroups);  // [4 warps][kRows][128 B]
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
-        unsigned char *exps = reinterpret_cast<unsigned char *>(width + E + 1);  // up: [256][2][4]
+        // this lane's routed row of a block and its 16 columns
+        const int row = kMode == kProductUp ? 8 * quad + (lane >> 2) : 4 * quad + (lane >> 3);
+        const int piece = kMode == kProductUp ? lane & 3 : lane & 7;
         int done = 0;
         for (bool any = walk.find(); any; any = walk.next(), ++done) {
             const int buf = done & 1;
-            // up_grad: what the first rows want of the checkpoint comes under the products
-            const int row = lane & 15, h = lane >> 4;
-            const int cr = tl.m * 256 + (int)rank * 128 + quad * 32 + 16 * h;  // plain, up_grad: first column
-            if (kMode == kProductUpGrad) {
+            const int c0 = kMode == kProductUp ? tl.m * 128 + (int)rank * 64 + 16 * piece
+                                               : tl.m * 256 + (int)rank * 128 + 16 * piece;
+            // up_grad: what the first two rows want of the checkpoint comes under the
+            // products, and the next tile's towards the L2
+            Kept kept[2] = {};
+            if constexpr (kMode == kProductUpGrad) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (16 * group + 32 * i + row < tl.n) kept[i] = read_kept(p, tl.r0 + 16 * group + 32 * i + row, c0);
                 Walk ahead = walk;
                 if (ahead.next()) {
                     const int c = ahead.tile.m * 256 + (int)rank * 128;
                     if (c < p.N) prefetch_kept(p, ahead.tile, c, (warp - 2) * 32 + lane);
                 }
             }
-            Kept kept = {};
-            if (kMode == kProductUpGrad && 16 * part + row < tl.n) kept = read_kept(p, tl.r0 + 16 * part + row, cr);
-            const bool good = pair_wait_warp(smem_u32(&acc_full[buf]), (uint32_t)(done >> 1) & 1u, p.status, abort, lane);
-            if (!good) break;
+            int ok = pair_wait_warp(smem_u32(&acc_full[buf]), (uint32_t)(done >> 1) & 1u, p.status, abort, lane);
+            ok = group_and(1 + group, ok);  // the group's warps go on, or give up, together
+            if (!ok) break;
             tc_fence_after();
             const uint32_t col = tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)(buf * 256);
-            if constexpr (kMode == kProductUp) {
-                // 32 routed rows at a time, one a thread with its 16 gate and 16 up values
-                const int c0 = tl.m * 128 + (int)rank * 64 + quad * 16;
-                for (int n0 = 0; n0 < tl.n; n0 += 32) {
-                    uint32_t r[32];
-                    tmem_ld32(col + (uint32_t)n0, r);
-                    tmem_wait_ld();
-                    __syncwarp();
+            for (int n0 = kRows * group; n0 < tl.n; n0 += kRows * kGroups) {
+                uint32_t r[kRows];
+                if constexpr (kMode == kProductUp) tmem_ld32(col + (uint32_t)n0, r);
+                else tmem_ld16(col + (uint32_t)n0, r);
+                tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        *reinterpret_cast<uint32_t *>(mine + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) = r[i];
-                    __syncwarp();
+                for (int i = 0; i < kRows; ++i)
+                    *reinterpret_cast<uint32_t *>(blocks + (quad * kRows + i) * 128 + turn_slot(lane >> 2, i, quad) +
+                                                  (lane & 3) * 4) = r[i];
+                group_sync(1 + group);
+                const int n = n0 + row;
+                const int64_t at = tl.r0 + n;
+                if constexpr (kMode == kProductUp) {
                     float v[32];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float4 f = *reinterpret_cast<const float4 *>(mine + lane * 128 + ((j ^ (lane & 7)) << 4));
-                        v[4 * j] = f.x;
-                        v[4 * j + 1] = f.y;
-                        v[4 * j + 2] = f.z;
-                        v[4 * j + 3] = f.w;
-                    }
-                    unsigned ex = 0;
-                    if (n0 + lane < tl.n) ex = finish_up(p, tl.r0 + n0 + lane, c0, v);
-                    if (p.codes) {
-                        exps[(n0 + lane) * 8 + quad] = (unsigned char)ex;
-                        exps[(n0 + lane) * 8 + 4 + quad] = (unsigned char)(ex >> 8);
-                    }
-                }
-                // the exponents of the four warps' blocks leave together, gate and up
-                // four bytes a row where the row's place allows it
-                if (p.codes) {
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
-                    const int blocks = p.N / 32, b0 = tl.m * 8 + (int)rank * 4;  // of F, the first of this CTA's
-                    for (int i = (warp - 2) * 32 + lane; i < 2 * tl.n; i += 128) {
-                        const int row = i >> 1, side = i & 1;
-                        uint8_t *to = p.exponents + (int64_t)(tl.r0 + row) * 2 * blocks + side * blocks + b0;
-                        const unsigned w = *reinterpret_cast<const unsigned *>(exps + row * 8 + 4 * side);
-                        if (b0 + 4 <= blocks && (reinterpret_cast<uintptr_t>(to) & 3u) == 0) {
-                            *reinterpret_cast<unsigned *>(to) = w;
-                        } else {
-                            for (int j = 0; j < 4 && b0 + j < blocks; ++j) to[j] = (uint8_t)(w >> (8 * j));
-                        }
-                    }
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
-                }
-            } else {
-                // 16 routed rows at a time, two threads a row with 16 columns each
-                for (int n0 = 16 * part; n0 < tl.n; n0 += 32) {
-                    const bool in = n0 + row < tl.n;
-                    const int64_t at = tl.r0 + n0 + row;
-                    Kept later = {};
-                    if (kMode == kProductUpGrad && n0 + 32 + row < tl.n) later = read_kept(p, at + 32, cr);
-                    uint32_t r[16];
-                    tmem_ld16(col + (uint32_t)n0, r);
-                    tmem_wait_ld();
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        *reinterpret_cast<uint32_t *>(mine + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) = r[i];
-                    __syncwarp();
+                    for (int j = 0; j < 8; ++j)
+                        load4(v + 4 * j, blocks + (piece * kRows + row) * 128 + turn_slot(j, row, piece));
+                    group_sync(1 + group);  // the blocks may be written again
+                    if (n < tl.n) finish_up(p, at, c0, v);
+                } else {
                     float v[16];
+                    const int from = piece >> 1, h = piece & 1;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float4 f = *reinterpret_cast<const float4 *>(mine + row * 128 + (((4 * h + j) ^ (row & 7)) << 4));
-                        v[4 * j] = f.x;
-                        v[4 * j + 1] = f.y;
-                        v[4 * j + 2] = f.z;
-                        v[4 * j + 3] = f.w;
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        load4(v + 4 * j, blocks + (from * kRows + row) * 128 + turn_slot(4 * h + j, row, from));
+                    group_sync(1 + group);
                     if constexpr (kMode == kProductPlain) {
-                        if (in) finish_plain(p, at, cr, v);
+                        if (n < tl.n) finish_plain(p, at, c0, v);
                     } else {
-                        float sum = in ? finish_grad(p, at, cr, v, kept) : 0.0f;
-                        sum += __shfl_xor_sync(kFull, sum, 16);
-                        if (in && h == 0 && cr < p.N) p.strips[(int64_t)(cr / 32) * p.R + at] = sum;
-                        kept = later;
+                        Kept later = {};
+                        if (n + 64 < tl.n) later = read_kept(p, at + 64, c0);
+                        float sum = n < tl.n ? finish_grad(p, at, c0, v, kept[0]) : 0.0f;
+#pragma unroll
+                        for (int o = 1; o < 8; o *= 2) sum += __shfl_xor_sync(kFull, sum, o);
+                        if (n < tl.n && piece == 0 && c0 < p.N) p.strips[(int64_t)(c0 / kStrip) * p.R + at] = sum;
+                        kept[0] = kept[1];
+                        kept[1] = later;
                     }
                 }
             }
