@@ -30,14 +30,16 @@ constexpr uint32_t kSide = 2 * kBlockBytes;     // a CTA's 128 columns of one op
 constexpr uint32_t kStage = 2 * kSide;
 constexpr int kStages = 6;
 constexpr uint32_t kOut = 32 * 128;             // an epilogue warp's 32 x 32 block
-constexpr uint32_t kSmem = 1024 + kStages * kStage + kEpiWarps * 2 * kOut;
-static_assert(kSmem <= 232448 - 2048, "shared memory");
+// Shared memory: ring, the epilogue's blocks, the experts' first rows [E + 1].
+constexpr uint32_t kTable = kStages * kStage + kEpiWarps * kOut;
+constexpr uint32_t smem_bytes(int E) { return 1024 + kTable + 4u * ((uint32_t)E + 1u); }
+static_assert(smem_bytes(1024) <= 232448 - 2048, "shared memory");
 static_assert(kStages == kLoadWarps, "a gathering warp has one stage of its own");
 
 // The tiles of a pair in turn: t = pair, pair + pairs, ...
 struct Walk {
-    const int *offsets;
-    int R, E, m_tiles, per;  // per: tiles of an expert
+    const int *start;        // shared, [E + 1]
+    int E, m_tiles, per;     // per: tiles of an expert
     uint32_t m_magic;
     int step_e, step_i;      // pairs in experts and tiles
     int e, i;                // expert, and tile of it
@@ -47,8 +49,8 @@ struct Walk {
         if (e >= E) return false;
         n = divide_by(i, m_magic);
         m = i - n * m_tiles;
-        r0 = max(0, min(__ldg(offsets + e), R));
-        r1 = max(r0, min(__ldg(offsets + e + 1), R));
+        r0 = start[e];
+        r1 = max(r0, start[e + 1]);
         return true;
     }
     __device__ __forceinline__ bool next() {
@@ -148,6 +150,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     }
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
     pdl_wait();
+    int *start = reinterpret_cast<int *>(smem + kTable);
+    for (int i = threadIdx.x; i <= a.E; i += kThreads) start[i] = max(0, min(__ldg(a.offsets + i), (int)a.R));
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();
@@ -155,7 +159,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     const uint32_t tmem = tmem_slot;
     const int m_tiles = (a.M + 255) / 256, per = m_tiles * ((a.N + 255) / 256);
     const int pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1);
-    Walk w{a.offsets, (int)a.R, a.E, m_tiles, per, a.m_magic, pairs / per, pairs % per, pair / per, pair % per, 0, 0, 0, 0};
+    Walk w{start, a.E, m_tiles, per, a.m_magic, pairs / per, pairs % per, pair / per, pair % per, 0, 0, 0, 0};
     const uint32_t ring = smem_u32(smem), full0 = smem_u32(full), empty0 = smem_u32(empty);
     const uint32_t full_pair = map_to_rank(full, 0);  // the first CTA's
     if (warp == 0) {
@@ -272,8 +276,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     } else {
         // ---------------------------------------------------------- epilogue
         const int quad = warp & 3, part = (warp - 2) >> 2;
-        unsigned char *both = smem + kStages * kStage + (warp - 2) * 2 * kOut;
-        int block = 0;  // blocks written by this warp: two places in turn
+        unsigned char *mine = smem + kStages * kStage + (warp - 2) * kOut;
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
         int done = 0;
         for (bool more = w.find(); more; more = w.next()) {
@@ -298,8 +301,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 32; ++i) r[i] = 0u;
                 }
-                unsigned char *mine = both + (block++ & 1) * kOut;
-                if (lane == 0) bulk_wait_read<1>();  // the last block but one has left
+                if (lane == 0) bulk_wait_read<0>();  // the last block has left
                 __syncwarp();
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -338,7 +340,7 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s) {
     if (!encode_side(&pmap, a.P, a.p_count, a.M) || !encode_side(&qmap, a.Q, a.q_count, a.N) ||
         !encode_tensor_map_3d_f32(&omap, a.dW, (uint64_t)a.E, (uint64_t)a.M, (uint64_t)a.N, 32))
         return cudaErrorInvalidValue;
-    cudaError_t e = ensure_smem_limit<weight_grad_kernel>(kSmem);
+    cudaError_t e = ensure_smem_limit<weight_grad_kernel>(smem_bytes(1024));
     if (e != cudaSuccess) return e;
     int dev = 0, sms = 0;
     e = cudaGetDevice(&dev);
@@ -348,7 +350,7 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s) {
     b.m_magic = divide_magic((uint32_t)(a.M + 255) / 256);
     const int64_t tiles = (int64_t)a.E * ((a.M + 255) / 256) * ((a.N + 255) / 256);
     const int64_t pairs = min64(tiles, sms / 2);
-    return launch_after(weight_grad_kernel, dim3((unsigned)(2 * pairs)), kThreads, kSmem, s, pmap, qmap, omap, b);
+    return launch_after(weight_grad_kernel, dim3((unsigned)(2 * pairs)), kThreads, smem_bytes(a.E), s, pmap, qmap, omap, b);
 }
 
 }  // namespace dol
