@@ -323,8 +323,10 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     _index("offsets", offsets, E + 1, dev)
     _index("rows", rows, T * k, dev)
     _index("pos", pos, T * k, dev)
-    out = torch.empty(T, H, dtype=torch.bfloat16, device=x.device)
-    if T and k:
+    if k == 0:
+        return x.new_zeros((T, H))
+    out = x.new_empty((T, H))
+    if T:
         L = dl.lib()
         n = L.do_expert_ffn_workspace_size(T, k, H, F)
         ws = torch.empty(n, dtype=torch.uint8, device=x.device)
