@@ -71,6 +71,38 @@ __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, int *st
     return pair_wait_slow(bar, parity, status, abort);
 }
 
+// The wait of a warp that issues copies or MMAs.  Such a warp walks its loop as a whole
+// and lets one lane issue: the operands of these instructions are then in the uniform
+// registers that they are read from, where a loop of a single lane moves each of them
+// there first (a plain product of 131072 x 2048 x 1536 took 486 us with one lane, 431 with
+// the warp).  All lanes leave with the same answer.
+__device__ __forceinline__ bool pair_wait_all(uint32_t bar, uint32_t parity, int *status, volatile int *abort) {
+    unsigned long long t0 = 0;
+    for (uint32_t it = 1;; ++it) {
+        if (__all_sync(kFull, mbar_try_wait_addr(bar, parity))) return true;
+        if ((it & 1023u) == 0u) {
+            const unsigned long long t = global_ns();
+            if (t0 == 0) t0 = t;
+            if (__any_sync(kFull, *abort || t - t0 > kWaitLimitNs)) {
+                if (status) atomicOr(status, kDevTimeout);
+                *abort = 1;
+                return false;
+            }
+        }
+    }
+}
+
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(one));
+    return one != 0;
+}
+
 // The same by a whole warp: one lane polls (32 lanes polling cost the shared memory
 // that the tensor cores read from), the others follow it.
 __device__ __forceinline__ bool pair_wait_warp(uint32_t bar, uint32_t parity, int *status, volatile int *abort,
@@ -214,6 +246,11 @@ __device__ __forceinline__ void pair_commit(uint32_t bar) {
 __device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t addr, uint32_t mn_stride) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)((mn_stride >> 4) & 0x3FFFu) << 16) |
            ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+// A descriptor moved on by `off` 16-byte units: the address lies in its low word.
+__device__ __forceinline__ uint64_t desc_at(uint64_t desc, uint32_t off) {
+    return (desc & 0xffffffff00000000ull) | ((uint32_t)desc + off);
 }
 
 // kind::f16 instruction descriptor: fp32 D, bf16 A and B, M = 256 over the pair,

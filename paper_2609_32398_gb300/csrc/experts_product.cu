@@ -319,17 +319,18 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const uint32_t full_pair = map_to_rank(full, 0);  // the first CTA's
     if (warp == 0) {
         // ---------------------------------------------------------- weights
-        if (lane == 0) {
-            Ring at{0, 0};
-            bool good = true;
-            int it = 0;
-            for (bool any = walk.find(); good && any; any = walk.next()) {
-                const int m0 = tl.m * 256 + (int)rank * 128, mb = tl.m * 8 + (int)rank * 4;
-                const uint32_t bytes = 2u * (kABytes + (kGather ? (uint32_t)tl.width * 64u : a.b_bytes));
-                for (int k = 0; k < p.K; k += 64, ++it) {
-                    good = pair_wait(empty0 + 8 * at.s, at.phase ^ 1u, p.status, abort);
-                    if (!good) break;
-                    const uint32_t st = ring + at.s * stage_bytes, bar = full_pair + 8 * at.s;
+        const bool one = elect_one();
+        Ring at{0, 0};
+        bool good = true;
+        int it = 0;
+        for (bool any = walk.find(); good && any; any = walk.next()) {
+            const int m0 = tl.m * 256 + (int)rank * 128, mb = tl.m * 8 + (int)rank * 4;
+            const uint32_t bytes = 2u * (kABytes + (kGather ? (uint32_t)tl.width * 64u : a.b_bytes));
+            for (int k = 0; k < p.K; k += 64, ++it) {
+                good = pair_wait_all(empty0 + 8 * at.s, at.phase ^ 1u, p.status, abort);
+                if (!good) break;
+                const uint32_t st = ring + at.s * stage_bytes, bar = full_pair + 8 * at.s;
+                if (one) {
                     if (rank == 0) mbar_expect_tx_addr(full0 + 8 * at.s, bytes);
                     if constexpr (kMode == kProductUp) {
                         pair_load_5d(st, &wmap, k, 0, 0, mb, tl.e, bar);
@@ -341,31 +342,33 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                         pair_load_3d(st, &wmap, m0, k, tl.e, bar);
                         pair_load_3d(st + kABytes / 2, &wmap, m0 + 64, k, tl.e, bar);
                     }
-                    at.next(stages);
                 }
+                __syncwarp();
+                at.next(stages);
             }
-            // a run that gave up: the loads in flight complete before the CTA ends (in the
-            // usual case the MMAs waited for them)
-            if (!good && rank == 0)
-                for (int i = it > stages ? it - stages : 0; i < it; ++i)
-                    mbar_wait(&full[i % stages], (uint32_t)(i / stages) & 1u, p.status);
         }
+        // a run that gave up: the loads in flight complete before the CTA ends (in the
+        // usual case the MMAs waited for them)
+        if (!good && rank == 0 && lane == 0)
+            for (int i = it > stages ? it - stages : 0; i < it; ++i)
+                mbar_wait(&full[i % stages], (uint32_t)(i / stages) & 1u, p.status);
         __syncwarp();
     } else if (!kGather && warp == kFirstLoader) {
         // ---------------------------------------------------------- rows in dispatch order
         // One box as high as the widest tile's half: what it holds past this tile's half
         // is not used.
-        if (lane == 0) {
-            Ring at{0, 0};
-            bool good = true;
-            for (bool any = walk.find(); good && any; any = walk.next()) {
-                const int r = tl.r0 + (int)rank * (tl.width / 2);
-                for (int k = 0; k < p.K; k += 64) {
-                    good = pair_wait(empty0 + 8 * at.s, at.phase ^ 1u, p.status, abort);
-                    if (!good) break;
+        const bool one = elect_one();
+        Ring at{0, 0};
+        bool good = true;
+        for (bool any = walk.find(); good && any; any = walk.next()) {
+            const int r = tl.r0 + (int)rank * (tl.width / 2);
+            for (int k = 0; k < p.K; k += 64) {
+                good = pair_wait_all(empty0 + 8 * at.s, at.phase ^ 1u, p.status, abort);
+                if (!good) break;
+                if (one)
                     pair_load_3d(ring + at.s * stage_bytes + kABytes, &amap, k, r, 0, full_pair + 8 * at.s);
-                    at.next(stages);
-                }
+                __syncwarp();
+                at.next(stages);
             }
         }
         __syncwarp();
@@ -416,7 +419,8 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
-        if (rank == 0 && lane == 0) {
+        if (rank == 0) {
+            const bool one = elect_one();
             Ring at{0, 0};
             int done = 0;
             bool good = true;
@@ -428,28 +432,32 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             const uint32_t acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
             for (bool any = walk.find(); good && any; any = walk.next(), ++done) {
                 const uint32_t buf = done & 1, turns = (uint32_t)done >> 1;
-                good = pair_wait(acc_empty0 + 8 * buf, (turns & 1u) ^ 1u, p.status, abort);
+                good = pair_wait_all(acc_empty0 + 8 * buf, (turns & 1u) ^ 1u, p.status, abort);
                 if (!good) break;
                 tc_fence_after();
                 const uint32_t d = tmem + buf * 256;
                 const uint32_t idesc = pair_idesc(tl.width, kTransposed, false);
                 uint32_t more = 0;
                 for (int k = 0; k < steps; ++k) {
-                    good = pair_wait(full0 + 8 * at.s, at.phase, p.status, abort);
+                    good = pair_wait_all(full0 + 8 * at.s, at.phase, p.status, abort);
                     if (!good) break;
                     tc_fence_after();
                     const uint32_t off = at.s * (stage_bytes / 16);
+                    if (one) {
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        pair_mma(d, ad0 + off + kk * kAStep, bd0 + off + kk * kBStep, idesc, more);
-                        more = 1;
+                        for (int kk = 0; kk < 4; ++kk)
+                            pair_mma(d, desc_at(ad0, off + kk * kAStep), desc_at(bd0, off + kk * kBStep), idesc,
+                                     kk > 0 ? 1u : more);
+                        pair_commit(empty0 + 8 * at.s);
                     }
-                    pair_commit(empty0 + 8 * at.s);
+                    __syncwarp();
+                    more = 1;
                     at.next(stages);
                 }
-                if (good) pair_commit(acc_full0 + 8 * buf);
+                if (good && one) pair_commit(acc_full0 + 8 * buf);
+                __syncwarp();
             }
-            if (!good) {  // the tensor cores are done with shared memory before the CTA ends
+            if (!good && one) {  // the tensor cores are done with shared memory before the CTA ends
                 pair_commit(smem_u32(&drain));
                 mbar_wait(&drain, 0u, p.status);
             }

@@ -164,17 +164,18 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     const uint32_t full_pair = map_to_rank(full, 0);  // the first CTA's
     if (warp == 0) {
         // ---------------------------------------------------------- TMA
-        if (lane == 0) {
-            const uint32_t whole = (a.p_rows ? 0u : 2u * kSide) + (a.q_rows ? 0u : 2u * kSide);
-            Ring at{0, 0};
-            int it = 0;
-            bool good = true;
-            for (bool any = w.find(); good && any; any = w.next()) {
-                const int px = w.m * 256 + (int)rank * 128, qx = w.n * 256 + (int)rank * 128;
-                for (int r = w.r0; r < w.r1; r += kStep, ++it) {
-                    good = pair_wait(empty0 + 8 * at.s, at.phase ^ 1u, a.status, abort);
-                    if (!good) break;
-                    const bool tail = r + kStep > w.r1 || whole == 0;
+        const bool one = elect_one();
+        const uint32_t whole = (a.p_rows ? 0u : 2u * kSide) + (a.q_rows ? 0u : 2u * kSide);
+        Ring at{0, 0};
+        int it = 0;
+        bool good = true;
+        for (bool any = w.find(); good && any; any = w.next()) {
+            const int px = w.m * 256 + (int)rank * 128, qx = w.n * 256 + (int)rank * 128;
+            for (int r = w.r0; r < w.r1; r += kStep, ++it) {
+                good = pair_wait_all(empty0 + 8 * at.s, at.phase ^ 1u, a.status, abort);
+                if (!good) break;
+                const bool tail = r + kStep > w.r1 || whole == 0;
+                if (one) {
                     if (rank == 0) {
                         if (tail) mbar_arrive_addr(full0 + 8 * at.s);
                         else mbar_expect_tx_addr(full0 + 8 * at.s, whole);
@@ -184,13 +185,14 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
                         if (!a.p_rows) load_side(st, &pmap, a.M, px, r, bar);
                         if (!a.q_rows) load_side(st + kSide, &qmap, a.N, qx, r, bar);
                     }
-                    at.next(kStages);
                 }
+                __syncwarp();
+                at.next(kStages);
             }
-            if (!good && rank == 0)
-                for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
-                    mbar_wait(&full[i % kStages], (uint32_t)(i / kStages) & 1u, a.status);
         }
+        if (!good && rank == 0 && lane == 0)
+            for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
+                mbar_wait(&full[i % kStages], (uint32_t)(i / kStages) & 1u, a.status);
         __syncwarp();
     } else if (warp >= kFirstLoader) {
         // ---------------------------------------------------------- gather
@@ -236,7 +238,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------- MMA issuer
-        if (rank == 0 && lane == 0) {
+        if (rank == 0) {
+            const bool one = elect_one();
             constexpr uint32_t idesc = pair_idesc(256, true, true);
             const uint64_t pd0 = desc_mn_sw128(ring, kBlockBytes), qd0 = desc_mn_sw128(ring + kSide, kBlockBytes);
             const uint32_t acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
@@ -246,28 +249,32 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
             for (bool any = w.find(); good && any; any = w.next()) {
                 if (w.r0 == w.r1) continue;
                 const uint32_t buf = done & 1, turns = (uint32_t)done >> 1;
-                good = pair_wait(acc_empty0 + 8 * buf, (turns & 1u) ^ 1u, a.status, abort);
+                good = pair_wait_all(acc_empty0 + 8 * buf, (turns & 1u) ^ 1u, a.status, abort);
                 if (!good) break;
                 tc_fence_after();
                 const uint32_t d = tmem + buf * 256;
                 uint32_t more = 0;
                 for (int r = w.r0; r < w.r1; r += kStep) {
-                    good = pair_wait(full0 + 8 * at.s, at.phase, a.status, abort);
+                    good = pair_wait_all(full0 + 8 * at.s, at.phase, a.status, abort);
                     if (!good) break;
                     tc_fence_after();
                     const uint32_t off = at.s * (kStage / 16);
+                    if (one) {
 #pragma unroll
-                    for (int kk = 0; kk < kStep / 16; ++kk) {
-                        pair_mma(d, pd0 + off + kk * (2048 / 16), qd0 + off + kk * (2048 / 16), idesc, more);
-                        more = 1;
+                        for (int kk = 0; kk < kStep / 16; ++kk)
+                            pair_mma(d, desc_at(pd0, off + kk * (2048 / 16)), desc_at(qd0, off + kk * (2048 / 16)), idesc,
+                                     kk > 0 ? 1u : more);
+                        pair_commit(empty0 + 8 * at.s);
                     }
-                    pair_commit(empty0 + 8 * at.s);
+                    __syncwarp();
+                    more = 1;
                     at.next(kStages);
                 }
-                if (good) pair_commit(acc_full0 + 8 * buf);
+                if (good && one) pair_commit(acc_full0 + 8 * buf);
+                __syncwarp();
                 ++done;
             }
-            if (!good) {  // the tensor cores are done with shared memory before the CTA ends
+            if (!good && one) {  // the tensor cores are done with shared memory before the CTA ends
                 pair_commit(smem_u32(&drain));
                 mbar_wait(&drain, 0u, a.status);
             }
