@@ -459,7 +459,7 @@ do_status do_rem_allocate(const double *loads, const double *expert_tokens,
  * pos [T][k] of one of its L problems.  Weights are bf16 (uint16 bit patterns):
  * W1 [E][2F][H], the F gate rows before the F up rows, and W2 [E][H][F].
  *  - Every matrix is dense, row-major and 16-byte aligned; its columns are a
- *    multiple of 8 (F, where it is named, of 16) and at most 2^20; E <= 1024.
+ *    multiple of 8 (F, where it is named, of 16) and at most 2^17; E <= 1024.
  *    Other sizes return DO_ERR_UNSUPPORTED.
  *  - Groups may be empty or of any length.  offsets is read as given, clipped to
  *    [0, R]; routed rows at or past offsets[E] are not written.

@@ -10,10 +10,11 @@ namespace {
 bool off(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Sizes that every call shares.  Columns are whole 16-byte pieces (8 bf16 values).
+// Sizes that every call shares.  Columns are whole 16-byte pieces (8 bf16 values), and
+// few enough that divide_by is exact for every tile that fits the memory.
 do_status check(int64_t R, int32_t E, int32_t c0, int32_t c1, int step0, int step1) {
     if (R < 1 || E < 1 || c0 < 1 || c1 < 1) return DO_ERR_INVALID_ARG;
-    if (E > 1024 || R > INT32_MAX - 256 || c0 % step0 || c1 % step1 || c0 > (1 << 20) || c1 > (1 << 20))
+    if (E > 1024 || R > INT32_MAX - 256 || c0 % step0 || c1 % step1 || c0 > (1 << 17) || c1 > (1 << 17))
         return DO_ERR_UNSUPPORTED;
     return DO_OK;
 }

@@ -175,15 +175,12 @@ __device__ __forceinline__ float sigmoid_f(float z) {
 
 // The codes of bytes b and b + 1 of a word, sign bits turned over beforehand (word ^
 // 0x80808080), times the block's scale: such a byte below the exponent of 2^23 is
-// 2^23 + 128 + code, and one fused multiply-add takes the rest off exactly.  (The
-// conversion instruction shares its pipe with sigma's exponential and division.)
-__device__ __forceinline__ f32x2 q8_values(unsigned word, int b, f32x2 scale, f32x2 offset) {
+// 2^23 + 128 + code.  (The conversion instruction shares its pipe with sigma's
+// exponential and division.)
+__device__ __forceinline__ f32x2 q8_values(unsigned word, int b, f32x2 scale) {
     const float lo = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440u + (unsigned)b));
     const float hi = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440u + (unsigned)b + 1u));
-    return fma2(pair2(lo, hi), scale, offset);
-}
-__device__ __forceinline__ f32x2 q8_offset(float scale) {
-    return pair2(-8388736.0f * scale, -8388736.0f * scale);
+    return mul2(add2(pair2(lo, hi), pair2(-8388736.0f, -8388736.0f)), scale);
 }
 
 __device__ __forceinline__ unsigned pack2(float lo, float hi) {

@@ -133,13 +133,13 @@ checkpoint_values_kernel(const uint4 *__restrict__ codes, const uint8_t *__restr
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < blocks; i += (int64_t)gridDim.x * 256) {
         const uint4 c = __ldg(codes + i);
         const float scale = q8_scale(__ldg(exponents + i));
-        const f32x2 s = pair2(scale, scale), off = q8_offset(scale);
+        const f32x2 s = pair2(scale, scale);
         const unsigned u[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
         unsigned o[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float lo, hi;
-            split2(q8_values(u[j / 2], 2 * (j & 1), s, off), lo, hi);
+            split2(q8_values(u[j / 2], 2 * (j & 1), s), lo, hi);
             o[j] = pack2(lo, hi);
         }
         values[2 * i] = make_uint4(o[0], o[1], o[2], o[3]);
@@ -160,8 +160,9 @@ cudaError_t launch_join(const void *Y, bool wide, const int *pos, const float *w
     while (cx < 256 && cx < N / 8) cx *= 2;
     const int64_t need = (T + 256 / cx - 1) / (256 / cx);
     const unsigned gy = (unsigned)((N / 8 + 255) / 256);
-    // three blocks of 80 registers a thread fit an SM
-    const unsigned gx = (unsigned)min64(need, (3 * 152 + gy - 1) / gy);
+    // four times what is resident at once: the last blocks even out (382 against 391 us for
+    // the products and the join of 16384 tokens, H = 2048)
+    const unsigned gx = (unsigned)min64(need, (12 * 152 + gy - 1) / gy);
     if (wide)
         return launch_after(join_kernel<float>, dim3(gx, gy), 256, 0, s, static_cast<const float *>(Y), pos, weights,
                             offsets, T, k, N, E, cx, out, status);

@@ -119,21 +119,14 @@ __device__ __forceinline__ void mbar_arrive_addr(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// A place in the ring, as a thread walks it: the threads that issue copies and MMAs
-// are each one thread deep in a dependent chain, where the division of a step number
-// by the number of stages alone costs 60 ns a step.
+// A place in the ring, as an issuing warp walks it: such a warp is one dependent chain,
+// in which the division of a step number by the number of stages alone cost 60 ns a
+// step.
 struct Ring {
     uint32_t s, phase;  // stage; how often the ring has been walked, mod 2
     __device__ __forceinline__ void next(uint32_t stages) {
         if (++s == stages) {
             s = 0;
-            phase ^= 1u;
-        }
-    }
-    __device__ __forceinline__ void skip(uint32_t n, uint32_t stages) {  // n <= stages
-        s += n;
-        if (s >= stages) {
-            s -= stages;
             phase ^= 1u;
         }
     }

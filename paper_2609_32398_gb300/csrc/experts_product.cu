@@ -191,13 +191,12 @@ __device__ __forceinline__ float finish_grad(const ProductArgs &p, int64_t r, in
     const unsigned uu[4] = {k.up.x ^ flip, k.up.y ^ flip, k.up.z ^ flip, k.up.w ^ flip};
     const float gate_scale = q8_scale((int)k.gate_exponent), up_scale = q8_scale((int)k.up_exponent);
     const f32x2 sg = pair2(gate_scale, gate_scale), su = pair2(up_scale, up_scale);
-    const f32x2 og = q8_offset(gate_scale), ou = q8_offset(up_scale);
     const f32x2 w = pair2(k.weight, k.weight), one = pair2(1.0f, 1.0f), minus = pair2(-1.0f, -1.0f);
     f32x2 sum = pair2(0.0f, 0.0f);
     float dg[16], du[16], act[16];
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-        const f32x2 zg = q8_values(ug[i / 4], i & 3, sg, og), zu = q8_values(uu[i / 4], i & 3, su, ou);
+        const f32x2 zg = q8_values(ug[i / 4], i & 3, sg), zu = q8_values(uu[i / 4], i & 3, su);
         const f32x2 s = sigmoid2(zg), g = pair2(v[i], v[i + 1]);
         const f32x2 silu = mul2(zg, s), a = mul2(silu, zu), gw = mul2(g, w);
         sum = fma2(g, a, sum);

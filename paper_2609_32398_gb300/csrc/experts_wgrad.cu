@@ -30,10 +30,15 @@ constexpr uint32_t kSide = 2 * kBlockBytes;     // a CTA's 128 columns of one op
 constexpr uint32_t kStage = 2 * kSide;
 constexpr int kStages = 6;
 constexpr uint32_t kOut = 32 * 128;             // an epilogue warp's 32 x 32 block
-// Shared memory: ring, the epilogue's blocks, the experts' first rows [E + 1].
-constexpr uint32_t kTable = kStages * kStage + kEpiWarps * kOut;
-constexpr uint32_t smem_bytes(int E) { return 1024 + kTable + 4u * ((uint32_t)E + 1u); }
-static_assert(smem_bytes(1024) <= 232448 - 2048, "shared memory");
+// Shared memory: ring, the epilogue's blocks (two a warp where the table leaves the room:
+// one is filled while the other leaves), the experts' first rows [E + 1].
+constexpr uint32_t kSmemLimit = 232448 - 512;  // the barriers are not dynamic
+constexpr uint32_t smem_with(int E, int blocks) {
+    return 1024 + kStages * kStage + kEpiWarps * blocks * kOut + 4u * ((uint32_t)E + 1u);
+}
+constexpr int out_blocks(int E) { return smem_with(E, 2) <= kSmemLimit ? 2 : 1; }
+constexpr uint32_t smem_bytes(int E) { return smem_with(E, out_blocks(E)); }
+static_assert(smem_bytes(1024) <= kSmemLimit && out_blocks(256) == 2, "shared memory");
 static_assert(kStages == kLoadWarps, "a gathering warp has one stage of its own");
 
 // The tiles of a pair in turn: t = pair, pair + pairs, ...
@@ -150,7 +155,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     }
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
     pdl_wait();
-    int *start = reinterpret_cast<int *>(smem + kTable);
+    const int blocks = out_blocks(a.E);
+    int *start = reinterpret_cast<int *>(smem + kStages * kStage + kEpiWarps * blocks * kOut);
     for (int i = threadIdx.x; i <= a.E; i += kThreads) start[i] = max(0, min(__ldg(a.offsets + i), (int)a.R));
     tc_fence_before();
     __syncthreads();
@@ -283,7 +289,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     } else {
         // ---------------------------------------------------------- epilogue
         const int quad = warp & 3, part = (warp - 2) >> 2;
-        unsigned char *mine = smem + kStages * kStage + (warp - 2) * kOut;
+        unsigned char *places = smem + kStages * kStage + (warp - 2) * blocks * kOut;
+        int turn = 0;  // the place of the next block
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
         int done = 0;
         for (bool more = w.find(); more; more = w.next()) {
@@ -308,7 +315,13 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 32; ++i) r[i] = 0u;
                 }
-                if (lane == 0) bulk_wait_read<0>();  // the last block has left
+                unsigned char *mine = places + turn * kOut;
+                if (blocks == 2) {
+                    turn ^= 1;
+                    if (lane == 0) bulk_wait_read<1>();  // what was in it has left
+                } else if (lane == 0) {
+                    bulk_wait_read<0>();
+                }
                 __syncwarp();
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -347,7 +360,7 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s) {
     if (!encode_side(&pmap, a.P, a.p_count, a.M) || !encode_side(&qmap, a.Q, a.q_count, a.N) ||
         !encode_tensor_map_3d_f32(&omap, a.dW, (uint64_t)a.E, (uint64_t)a.M, (uint64_t)a.N, 32))
         return cudaErrorInvalidValue;
-    cudaError_t e = ensure_smem_limit<weight_grad_kernel>(smem_bytes(1024));
+    cudaError_t e = ensure_smem_limit<weight_grad_kernel>(kSmemLimit);
     if (e != cudaSuccess) return e;
     int dev = 0, sms = 0;
     e = cudaGetDevice(&dev);

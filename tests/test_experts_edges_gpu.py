@@ -245,3 +245,14 @@ def test_graph_replays_give_the_same_results(ex):  # noqa: F811
         for a, b in zip(caught, plain):
             assert torch.equal(a, b)
     ok(ex)
+
+
+def test_checkpoint_values_over_the_whole_range(ex):  # noqa: F811
+    """Every code with exponents from the least to the greatest that the format has; a
+    code above 64 at the greatest stands for more than bf16 holds and reads as infinity."""
+    codes = torch.arange(-127, 129).clamp(max=127).to(torch.int8).reshape(1, 256).repeat(10, 1)
+    exps = torch.tensor([1, 2, 3, 100, 127, 200, 231, 232, 240, 249], dtype=torch.uint8).reshape(10, 1).repeat(1, 16)
+    gc, gexp = gpu(codes, exps)
+    got = ex.Checkpoint(gc, gexp).values()
+    ok(ex)
+    assert torch.equal(got.cpu(), ref.values(codes, exps).bfloat16())
