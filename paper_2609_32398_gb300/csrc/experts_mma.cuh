@@ -115,10 +115,6 @@ __device__ __forceinline__ bool pair_wait_warp(uint32_t bar, uint32_t parity, in
 __device__ __forceinline__ void mbar_expect_tx_addr(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void mbar_arrive_addr(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
 // A place in the ring, as an issuing warp walks it: such a warp is one dependent chain,
 // in which the division of a step number by the number of stages alone cost 60 ns a
 // step.
@@ -182,20 +178,22 @@ __device__ __forceinline__ void gathered(uint32_t full_addr, int lane) {
     if (lane == 0) mbar_arrive_cluster(full_addr);
 }
 
-// Where rows are gathered, warp w of a CTA's kLoadWarps gathering warps brings the steps
-// w, w + kLoadWarps, ... of the ring alone.
-//  - The products do it with TMA copies of four rows.  Such a copy takes its thread 85 to
-//    100 cycles to issue, and a step has 32: one warp took five times the products' time,
-//    six warps a step each take as long as the products do.  cp.async in 16-byte pieces
-//    takes the same where the epilogue is light, and 15% more where it stores much (105
-//    against 90 us for 103 GFLOP at K = 1024).
-//  - The weight gradients do it with cp.async: their results leave by TMA, which the
-//    four-row copies then hold up (dW1 at 16384 tokens, H = 2048: 653 us against 742; 697
-//    with plain stores).
-// The ring has at least kLoadWarps stages: a warp at step m has waited for step m -
-// kLoadWarps - stages to be consumed, so that a stage's barrier is at most one phase
-// behind what it waits for, which a parity can tell.
-constexpr int kLoadWarps = 6;
+// Gathering.  The products bring rows by TMA copies of four (pair_gather4).  Such a copy
+// takes its lane 85 to 100 cycles to issue and a step has up to 32, so that what bounds
+// the ring is how long a step's copies take to leave: with one warp a step they took 1.4
+// of the 2.8 us that a stage is on its way (up projection of 16384 tokens, H = 2048: 550
+// us with six warps of a step each, 508 with three pairs, 486 with three times four, 707
+// with all six on one step; the same rows in dispatch order 465).  cp.async in 16-byte
+// pieces took as long as six warps, and half of the rows each way no less.  The weight
+// gradients bring theirs by cp.async, a warp a step: their results leave by TMA, which
+// the copies of four rows then hold up (dW1 of 16384 tokens: 627 us against 679).
+//
+// The rings' barriers are waited for by parity, which can tell one phase from the next
+// only.  So every warp that waits for a stage is one that the stage's next phase waits
+// for: each arrives on every step that it takes part in, whether it had copies to issue
+// or not; and no warp is ahead by more than the ring: it waits at each of its steps, and
+// its last one was fewer than `stages` steps before.
+constexpr int kLoadWarps = 6;  // of the weight gradients, one for each stage of the ring
 
 __device__ __forceinline__ void tma_reduce_add_3d(const CUtensorMap *map, const void *src, int x, int y, int z) {
     asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::

@@ -139,7 +139,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(&full[i], 3);
+            mbar_init(&full[i], 4);  // each CTA's TMA warp and its gathering warp of the step
             mbar_init(&empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -182,10 +182,10 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
                 if (!good) break;
                 const bool tail = r + kStep > w.r1 || whole == 0;
                 if (one) {
-                    if (rank == 0) {
-                        if (tail) mbar_arrive_addr(full0 + 8 * at.s);
-                        else mbar_expect_tx_addr(full0 + 8 * at.s, whole);
-                    }
+                    // the second CTA's warp arrives too: a step that has nothing to load by
+                    // TMA must not leave it a phase behind, which its parity could not tell
+                    if (rank == 0 && !tail) mbar_expect_tx_addr(full0 + 8 * at.s, whole);
+                    else mbar_arrive_cluster(full_pair + 8 * at.s);
                     if (!tail) {
                         const uint32_t st = ring + at.s * kStage, bar = full_pair + 8 * at.s;
                         if (!a.p_rows) load_side(st, &pmap, a.M, px, r, bar);

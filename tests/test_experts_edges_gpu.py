@@ -256,3 +256,30 @@ def test_checkpoint_values_over_the_whole_range(ex):  # noqa: F811
     got = ex.Checkpoint(gc, gexp).values()
     ok(ex)
     assert torch.equal(got.cpu(), ref.values(codes, exps).bfloat16())
+
+
+@pytest.mark.parametrize("gather", [False, True])
+def test_short_steps_leave_no_warp_behind(ex, gather):  # noqa: F811
+    """Many experts of one to three rows: steps in which most loading warps have nothing
+    to load.  The same results, and no wait that runs out, over many runs."""
+    E, K, N = 500, 512, 1024
+    g = torch.Generator().manual_seed(5)
+    counts = torch.randint(0, 4, (E,), generator=g).tolist()
+    off = ref.groups(counts)
+    R = sum(counts)
+    a, q, w = rnd(1, 40 if gather else R, K), rnd(2, R, N), rnd(3, E, N, K, scale=0.1)
+    rows = torch.randint(0, 40, (R,), generator=g) if gather else None
+    ga, gq, gw, go, gr = gpu(a, q, w, off, rows)
+    dw = ex.grouped_weight_grad(ga, gq, go, gr, None)
+    y = ex.grouped_matmul(ga, gw, go, gr)
+    ok(ex)
+    want, m = ref.product(a, w, off, rows)
+    within(y, want, 2 * K * U * m + BF * want.abs())
+    ad = (a if rows is None else a[rows]).double()
+    for e in range(0, E, 37):
+        i, j = int(off[e]), int(off[e + 1])
+        within(dw[e], ad[i:j].T @ q[i:j].double(), 2 * max(j - i, 1) * U * (ad[i:j].abs().T @ q[i:j].double().abs()))
+    for _ in range(100):
+        assert torch.equal(ex.grouped_weight_grad(ga, gq, go, gr, None), dw)
+        assert torch.equal(ex.grouped_matmul(ga, gw, go, gr), y)
+    ok(ex)
