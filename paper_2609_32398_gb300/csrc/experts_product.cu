@@ -46,8 +46,13 @@ constexpr int kTileN = 256;               // routed rows of a tile at most
 // column are 16 TMEM lanes apart and want one thread).
 __host__ __device__ constexpr int epi_warps(int mode) { return mode == kProductUp ? 4 : 8; }
 __host__ __device__ constexpr int first_loader(int mode) { return 2 + epi_warps(mode); }
+// Gathering warps: load_split of them share a step, kLoadSteps steps are filled at a time
+// (see pair_gather4).  The gradient's epilogue leaves registers for six.
+constexpr int kLoadSteps = 3;
+__host__ __device__ constexpr int load_split(int mode) { return mode == kProductUpGrad ? 2 : 4; }
+__host__ __device__ constexpr int load_warps(int mode) { return kLoadSteps * load_split(mode); }
 __host__ __device__ constexpr int threads_of(int mode, bool gather) {
-    return (first_loader(mode) + (gather ? kLoadWarps : 1)) * 32;
+    return (first_loader(mode) + (gather ? load_warps(mode) : 1)) * 32;
 }
 constexpr uint32_t kTurnAll = 16384;
 constexpr uint32_t kABytes = 128 * 128;   // a CTA's weight rows of one step
@@ -261,7 +266,7 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < stages; ++i) {
-            mbar_init(&full[i], 1);
+            mbar_init(&full[i], kGather ? 1 + 2 * load_split(kMode) : 1);
             mbar_init(&empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -373,7 +378,10 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         __syncwarp();
     } else if (kGather && warp >= kFirstLoader) {
         // ---------------------------------------------------------- gather
-        // Lane l copies this CTA's routed rows 4 l .. 4 l + 3 of the tile.
+        // Of the kSplit warps that share a step, lane l of the w-th copies this CTA's
+        // routed rows 4 (l kSplit + w) .. + 3 of the tile.
+        constexpr int kSplit = load_split(kMode);
+        const int loader = warp - kFirstLoader, mine4 = 4 * (lane * kSplit + loader % kSplit);
         const int none = (int)p.a_rows;
         int4 ids;
         auto read_ids = [&]() {
@@ -382,34 +390,37 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             bool bad = false;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int n = (int)rank * half + 4 * lane + j;
-                v[j] = 4 * lane < half && n < tl.n ? __ldg(p.rows + tl.r0 + n) : none;
+                const int n = (int)rank * half + mine4 + j;
+                v[j] = mine4 < half && n < tl.n ? __ldg(p.rows + tl.r0 + n) : none;
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int n = (int)rank * half + 4 * lane + j;
+                const int n = (int)rank * half + mine4 + j;
                 const bool out = v[j] < 0 || v[j] >= none;
-                bad |= out && 4 * lane < half && n < tl.n;
+                bad |= out && mine4 < half && n < tl.n;
                 if (out) v[j] = none;
             }
             if (bad && p.status) atomicOr(p.status, kDevBadId);
             ids = make_int4(v[0], v[1], v[2], v[3]);
         };
-        int it = 0, mine = warp - kFirstLoader;  // steps so far, this warp's next one
+        int it = 0, mine = loader / kSplit;  // steps so far, this warp's next one
         bool good = true, any = walk.find();
         if (any) read_ids();
         while (good && any) {
             const int half = tl.width / 2, end = it + steps;
-            for (; mine < end; mine += kLoadWarps) {
+            for (; mine < end; mine += kLoadSteps) {
                 const int s = mine % stages;
                 if (mine >= stages) {
                     good = pair_wait_warp(empty0 + 8 * s, (uint32_t)(mine / stages - 1) & 1u, p.status, abort, lane);
                     if (!good) break;
                 }
-                if (4 * lane < half)
-                    pair_gather4(ring + (uint32_t)s * stage_bytes + kABytes + lane * 512, &amap, 64 * (mine - it), ids,
+                if (mine4 < half)
+                    pair_gather4(ring + (uint32_t)s * stage_bytes + kABytes + mine4 * 128, &amap, 64 * (mine - it), ids,
                                  full_pair + 8 * s);
                 __syncwarp();
+                // a step waits for each of its warps, with copies or (a narrow tile) without:
+                // none may fall a phase behind
+                if (lane == 0) mbar_arrive_cluster(full_pair + 8 * s);
             }
             any = walk.next();
             if (any) read_ids();
@@ -583,7 +594,7 @@ cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
     const uint32_t fixed = 1024 + kTurnAll + table_bytes(p.E) + 2048;
     a.stages = (int)((kSmemLimit - fixed) / (kABytes + a.b_bytes));
     if (a.stages > kMaxStages) a.stages = kMaxStages;
-    if (a.stages < kLoadWarps) return cudaErrorInvalidConfiguration;
+    if (a.stages < kLoadSteps + 1) return cudaErrorInvalidConfiguration;
     const uint32_t smem = 1024 + off_turn(a.stages, a.b_bytes) + kTurnAll + table_bytes(p.E);
     constexpr auto kernel = product_kernel<kMode, kGather, kTransposed>;
     cudaError_t e = ensure_smem_limit<kernel>(kSmemLimit - 2048);
