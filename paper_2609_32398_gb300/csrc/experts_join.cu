@@ -42,11 +42,12 @@ __device__ __forceinline__ Picks read_picks(const int *pos, const float *weights
 }
 
 // A thread has 8 columns and walks over tokens; a token's rows are read as 16-byte
-// pieces, eight in flight, and the next token's positions and weights under them.  A
-// choice that is left out adds nothing (its row is not read).  Bound by memory: T = 16384,
-// k = 8, N = 2048 moves 604 MB.
+// pieces, eight in flight a thread and 24 warps an SM.  A choice that is left out adds
+// nothing (its row is not read).  Bound by memory: T = 16384, k = 8, N = 2048 moves 604 MB
+// in about 110 us.  (The next token's positions read ahead cost the third block an SM:
+// 383 against 376 us for the products and the join.)
 template <typename Y>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, sizeof(Y) == 2 ? 3 : 2)
 join_kernel(const Y *__restrict__ y, const int *__restrict__ pos, const float *__restrict__ weights,
             const int *__restrict__ offsets, int64_t T, int k, int N, int E, int cx, bf16 *__restrict__ out,
             int *status) {
@@ -68,12 +69,9 @@ join_kernel(const Y *__restrict__ y, const int *__restrict__ pos, const float *_
                     v[q] = make_uint4(0, 0, 0, 0);
                     if (now.row[q] >= 0) v[q] = __ldg(reinterpret_cast<const uint4 *>(y + (int64_t)now.row[q] * N) + c);
                 }
-                const Picks was = now;
-                if (q0 + 8 < k) now = read_picks(pos, weights, t, k, q0 + 8, limit, status);
-                else if (t + step < T) now = read_picks(pos, weights, t + step, k, 0, limit, status);
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    if (was.row[q] >= 0) add8(acc, v[q], was.w[q]);
+                    if (now.row[q] >= 0) add8(acc, v[q], now.w[q]);
             } else {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -93,9 +91,9 @@ join_kernel(const Y *__restrict__ y, const int *__restrict__ pos, const float *_
                         acc[4 * h + 3] = fmaf(now.w[q], v[q].w, acc[4 * h + 3]);
                     }
                 }
-                if (q0 + 8 < k) now = read_picks(pos, weights, t, k, q0 + 8, limit, status);
-                else if (t + step < T) now = read_picks(pos, weights, t + step, k, 0, limit, status);
             }
+            if (q0 + 8 < k) now = read_picks(pos, weights, t, k, q0 + 8, limit, status);
+            else if (t + step < T) now = read_picks(pos, weights, t + step, k, 0, limit, status);
         }
         reinterpret_cast<uint4 *>(out + t * N)[c] = make_uint4(pack2(acc[0], acc[1]), pack2(acc[2], acc[3]),
                                                                pack2(acc[4], acc[5]), pack2(acc[6], acc[7]));
@@ -125,31 +123,34 @@ __global__ void strip_sums_kernel(const float *__restrict__ strips, int n, const
     dcombine[i] = s;
 }
 
-// One thread per block of 16 codes: 16 bytes and an exponent in, 32 bytes out.
+// A thread takes two blocks of 16 codes, their loads in flight together: 16 bytes and an
+// exponent in, 32 bytes out each.  131072 x 1536 values: 90.5 us, 6.8 TB/s (one block a
+// thread 104.5, four 90.5).
 __global__ void __launch_bounds__(256)
 checkpoint_values_kernel(const uint4 *__restrict__ codes, const uint8_t *__restrict__ exponents, int64_t blocks,
                          uint4 *__restrict__ values) {
     pdl_wait();
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < blocks; i += (int64_t)gridDim.x * 256) {
-        const uint4 c = __ldg(codes + i);
-        const float scale = q8_scale(__ldg(exponents + i));
-        const f32x2 s = pair2(scale, scale);
-        const unsigned u[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
-        unsigned o[8];
+    const int64_t i0 = (int64_t)blockIdx.x * 512 + threadIdx.x;
+    uint4 c[2];
+    int e[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float lo, hi;
-            split2(q8_values(u[j / 2], 2 * (j & 1), s), lo, hi);
-            o[j] = pack2(lo, hi);
-        }
-        values[2 * i] = make_uint4(o[0], o[1], o[2], o[3]);
-        values[2 * i + 1] = make_uint4(o[4], o[5], o[6], o[7]);
+    for (int u = 0; u < 2; ++u) {
+        const int64_t i = i0 + 256 * u;
+        c[u] = i < blocks ? __ldg(codes + i) : make_uint4(0, 0, 0, 0);
+        e[u] = i < blocks ? __ldg(exponents + i) : 1;
     }
-}
-
-unsigned blocks_of(int64_t n, int64_t most) {
-    const int64_t b = (n + 255) / 256;
-    return (unsigned)(b < most ? b : most);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int64_t i = i0 + 256 * u;
+        if (i >= blocks) break;
+        const float scale = q8_scale(e[u]);
+        const f32x2 s = pair2(scale, scale);
+        const unsigned w[4] = {c[u].x ^ 0x80808080u, c[u].y ^ 0x80808080u, c[u].z ^ 0x80808080u, c[u].w ^ 0x80808080u};
+        float v[16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) split2(q8_values(w[j / 2], 2 * (j & 1), s), v[2 * j], v[2 * j + 1]);
+        store16(reinterpret_cast<bf16 *>(values + 2 * i), v);
+    }
 }
 
 }  // namespace
@@ -185,7 +186,7 @@ cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos,
 cudaError_t launch_checkpoint_values(const int8_t *codes, const uint8_t *exponents, int64_t rows, int cols,
                                      bf16 *values, cudaStream_t s) {
     const int64_t n = rows * (cols / kQBlock);
-    return launch_after(checkpoint_values_kernel, dim3(blocks_of(n, 1 << 20)), 256, 0, s,
+    return launch_after(checkpoint_values_kernel, dim3((unsigned)((n + 511) / 512)), 256, 0, s,
                         reinterpret_cast<const uint4 *>(codes), exponents, n, reinterpret_cast<uint4 *>(values));
 }
 
