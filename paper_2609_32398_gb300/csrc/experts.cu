@@ -37,7 +37,7 @@ size_t join_bytes(int64_t R, int32_t N) {
 // a.out: [T][N]; workspace: join_bytes (not used by the few-row kernel).
 cudaError_t product_join(ProductArgs a, const int *pos, const float *weights, int64_t T, int k, void *workspace,
                          cudaStream_t s) {
-    if (a.R <= kFewRows && !a.transposed) return launch_few_join(a, pos, weights, T, k, s);
+    if (a.R <= kFewRows && T <= kFewTokens && !a.transposed) return launch_few_join(a, pos, weights, T, k, s);
     bf16 *out = a.out;
     const bool wide = join_wide(a.R, a.N);
     a.wide = wide ? static_cast<float *>(workspace) : nullptr;

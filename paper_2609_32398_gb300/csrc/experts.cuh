@@ -49,8 +49,14 @@ struct ProductArgs {
 cudaError_t launch_product(ProductMode mode, const ProductArgs &a, cudaStream_t s);
 
 // The products of at most kFewRows routed rows without checkpoint, weights as they
-// are (not transposed), and the joined ones, where out is [T][N] (experts_few.cu).
-constexpr int64_t kFewRows = 24;
+// are (not transposed), and the joined ones of at most kFewTokens tokens of them, where
+// out is [T][N] (experts_few.cu).  Measured on both sides (us in a graph; H = 2048, F =
+// 768, k = 8 of 128 experts; few rows against tensor cores): up R = 8 10.5 and 15.5, 16
+// 17.1 and 25.4, 24 23.5 and 27.3, 32 39 and 36; down 7.0 and 9.9, 11.3 and 13.8, 19.3 and
+// 17.0, 25 and 19; joined T = 1 9.5 and 12.3, 2 17.4 and 16.6 (H = 512: 3.5 and 6.9), 16
+// tokens of one row 15.5 and 10.6.
+constexpr int64_t kFewRows = 16;
+constexpr int64_t kFewTokens = 2;
 cudaError_t launch_few_product(ProductMode mode, const ProductArgs &a, cudaStream_t s);
 cudaError_t launch_few_join(const ProductArgs &a, const int *pos, const float *weights, int64_t T, int k,
                             cudaStream_t s);

@@ -5,7 +5,9 @@
 // spread evenly over the GPU; the tensor-core kernels' tiles of 256 weight rows
 // leave a part of it idle then (8 routed rows of E = 128 experts, H = 2048, F = 768:
 // 96 CTAs of 152).  Rows that share an expert read its weights again, from the L2:
-// kFewRows is where that starts to cost more than the idle part saves.
+// kFewRows is where that starts to cost more than the idle part saves.  Bound by memory
+// and the latency of two dependent loads (the group ends, then the weights): the up
+// projection of those 8 rows takes 10.5 us for 50 MB, 7.4 at the copy rate.
 //
 // Sums are fp32, lane by lane in order and then over the lanes.
 #include "experts.cuh"

@@ -41,7 +41,7 @@ def test_group_sizes_at_the_tiles_edges(ex, n, gather):  # noqa: F811
         within(dw[e], ad[i:j].T @ q[i:j].double(), 2 * (j - i) * U * (ad[i:j].abs().T @ q[i:j].double().abs()))
 
 
-@pytest.mark.parametrize("R", [24, 25, 900])
+@pytest.mark.parametrize("R", [16, 17, 24, 25, 900])
 @pytest.mark.parametrize("gather", [False, True])
 def test_many_experts_and_both_sides_of_the_few_row_line(ex, R, gather):  # noqa: F811
     E, K, N = 1024, 136, 72
@@ -72,7 +72,7 @@ def test_many_experts_and_both_sides_of_the_few_row_line(ex, R, gather):  # noqa
     within(dw[e], ad[i:j].T @ ud[i:j], 2 * (j - i) * U * (ad[i:j].abs().T @ ud[i:j].abs()))
 
 
-@pytest.mark.parametrize("T,k", [(1, 16), (2, 12), (24, 1), (25, 1), (3, 5)])
+@pytest.mark.parametrize("T,k", [(1, 16), (2, 12), (24, 1), (25, 1), (3, 5), (2, 8), (3, 4), (1, 17)])
 def test_join_of_few_rows(ex, T, k):  # noqa: F811
     E, K, N = 40, 776, 136
     g = torch.Generator().manual_seed(T + k)
