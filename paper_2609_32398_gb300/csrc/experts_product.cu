@@ -34,7 +34,7 @@
 // What bounds it: the tensor cores, once a tile has a few tens of steps.  131072 rows of
 // one expert, 2048 x 1536: 429 us, 1.92 PFLOP/s (of 1.94 measured); the up projection of
 // 16384 tokens over 128 experts (H = 2048, F = 768) 479 us, 1.72 PFLOP/s, with its
-// checkpoint 505; the gradient through W2 and the activation 372 us, of which the
+// checkpoint 505; the gradient through W2 and the activation 362 us, of which the
 // products alone 280: its epilogue moves 820 MB.  Short contractions (768 to 1024) pay
 // one to two microseconds a tile, few tiles the rounding up to whole rounds of 76 pairs,
 // few rows the reading of the weights (16 tokens: 76 us of 81).
@@ -184,16 +184,6 @@ __device__ __forceinline__ Kept read_kept(const ProductArgs &p, int64_t r, int c
     }
     return k;
 }
-// The checkpoint of a tile's 128 columns on their way to the L2: up to 256 rows, two
-// lines of codes each and the exponents beside them, over 256 threads.
-__device__ __forceinline__ void prefetch_kept(const ProductArgs &p, const Tile &tl, int c0, int thread) {
-    for (int i = thread; i < 2 * tl.n; i += 256) {
-        const int64_t at = (int64_t)(tl.r0 + (i >> 1)) * 2 * p.N + (i & 1) * p.N + c0;
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.codes + at));
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.exponents + at / kQBlock));
-    }
-}
-
 // Returns the sum of g act over the 16 columns.
 __device__ __forceinline__ float finish_grad(const ProductArgs &p, int64_t r, int c0, const float (&v)[16],
                                              const Kept &k) {
@@ -496,17 +486,13 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             const int c0 = kMode == kProductUp ? tl.m * 128 + (int)rank * 64 + 16 * piece
                                                : tl.m * 256 + (int)rank * 128 + 16 * piece;
             // up_grad: what the first two rows want of the checkpoint comes under the
-            // products, and the next tile's towards the L2
+            // products (fetching the next tile's whole checkpoint to the L2 here read a
+            // part of it twice: 372 us against 362)
             Kept kept[2] = {};
             if constexpr (kMode == kProductUpGrad) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     if (16 * group + 32 * i + row < tl.n) kept[i] = read_kept(p, tl.r0 + 16 * group + 32 * i + row, c0);
-                Walk ahead = walk;
-                if (ahead.next()) {
-                    const int c = ahead.tile.m * 256 + (int)rank * 128;
-                    if (c < p.N) prefetch_kept(p, ahead.tile, c, (warp - 2) * 32 + lane);
-                }
             }
             int ok = pair_wait_warp(smem_u32(&acc_full[buf]), (uint32_t)(done >> 1) & 1u, p.status, abort, lane);
             ok = group_and(1 + group, ok);  // the group's warps go on, or give up, together
