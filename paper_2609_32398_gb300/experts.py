@@ -66,7 +66,7 @@ def _index(name: str, t, n: int, device: int) -> None:
 
 
 def _fp32(name: str, t, shape: tuple, device: int) -> None:
-    if t is not None and (t.dtype is not torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()
+    if t is not None and (t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous()
                           or t.get_device() != device):
         raise ValueError(f"{name} must be a contiguous CUDA float32 tensor of shape {list(shape)}, "
                          "all tensors on one device")
@@ -85,7 +85,7 @@ class Checkpoint:
 
     def check(self, R: int, F: int, device: int) -> None:
         c, e = self.codes, self.exponents
-        if (c.dtype is not torch.int8 or e.dtype is not torch.uint8 or tuple(c.shape) != (R, 2 * F)
+        if (c.dtype is not torch.int8 or e.dtype is not torch.uint8 or c.shape != (R, 2 * F)
                 or e.numel() * 16 != c.numel() or c.get_device() != device or e.get_device() != device
                 or device < 0 or not (c.is_contiguous() and e.is_contiguous())):
             raise ValueError("a checkpoint holds contiguous CUDA codes int8 [R,2F] and exponents "
@@ -93,13 +93,14 @@ class Checkpoint:
 
     def values(self) -> torch.Tensor:
         """The values it stands for, bf16 [R, 2F] (7 significant bits: exact)."""
-        R, n = self.codes.shape
-        self.check(R, n // 2, self.codes.get_device())
-        out = torch.empty(R, n, dtype=torch.bfloat16, device=self.codes.device)
+        codes = self.codes
+        R, n = codes.shape
+        dev = codes.get_device()
+        self.check(R, n // 2, dev)
+        out = codes.new_empty((R, n), dtype=torch.bfloat16)
         if R:
             dl._check("do_checkpoint_values", dl.lib().do_checkpoint_values(
-                self.codes.data_ptr(), self.exponents.data_ptr(), R, n, out.data_ptr(),
-                dl._stream(out)))
+                codes.data_ptr(), self.exponents.data_ptr(), R, n, out.data_ptr(), _raw_stream(dev)))
         return out
 
 
@@ -126,11 +127,11 @@ def expert_up(x: torch.Tensor, w1: torch.Tensor, offsets: torch.Tensor,
     _index("offsets", offsets, E + 1, dev)
     _index("rows", rows, R, dev)
     F = F2 // 2
-    act = torch.empty(R, F, dtype=torch.bfloat16, device=x.device)
+    act = x.new_empty((R, F))
     kept = None
     if checkpoint:
-        kept = Checkpoint(torch.empty(R, F2, dtype=torch.int8, device=x.device),
-                          torch.empty(R, F2 // 16, dtype=torch.uint8, device=x.device))
+        kept = Checkpoint(x.new_empty((R, F2), dtype=torch.int8),
+                          x.new_empty((R, F2 // 16), dtype=torch.uint8))
     if R:
         dl._check("do_expert_up", dl.lib().do_expert_up(
             x.data_ptr(), w1.data_ptr(), dl._ptr(rows), offsets.data_ptr(), T, H, F, E, R,
@@ -160,7 +161,7 @@ def grouped_matmul(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     R = T if rows is None else rows.numel()
     _index("offsets", offsets, E + 1, dev)
     _index("rows", rows, R, dev)
-    y = torch.empty(R, N, dtype=torch.bfloat16, device=a.device)
+    y = a.new_empty((R, N))
     if R:
         dl._check("do_grouped_matmul", dl.lib().do_grouped_matmul(
             a.data_ptr(), w.data_ptr(), dl._ptr(rows), offsets.data_ptr(), T, K, N, E, R,
@@ -183,15 +184,15 @@ def grouped_matmul_join(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     _index("offsets", offsets, E + 1, dev)
     _index("pos", pos, T * k, dev)
     _fp32("weights", weights, (T, k), dev)
-    out = torch.empty(T, N, dtype=torch.bfloat16, device=a.device)
+    out = a.new_empty((T, N))
     if T:
         L = dl.lib()
-        ws = torch.empty(int(L.do_grouped_matmul_join_workspace_size(T, k, N)), dtype=torch.uint8,
-                         device=a.device)
+        n = L.do_grouped_matmul_join_workspace_size(T, k, N)
+        ws = a.new_empty(n, dtype=torch.uint8)
         dl._check("do_grouped_matmul_join", L.do_grouped_matmul_join(
             a.data_ptr(), w.data_ptr(), offsets.data_ptr(), pos.data_ptr(), dl._ptr(weights), T, k,
             K, N, E, int(bool(transposed)), out.data_ptr(), _status(dev), ws.data_ptr(),
-            ws.numel(), _raw_stream(dev)))
+            n, _raw_stream(dev)))
     return out
 
 
@@ -218,18 +219,18 @@ def expert_up_backward(dout: torch.Tensor, w2: torch.Tensor, kept: Checkpoint,
     _index("rows", rows, R, dev)
     _index("pos", pos, R, dev)
     kept.check(R, F, dev)
-    dz = torch.empty(R, 2 * F, dtype=torch.bfloat16, device=dout.device)
-    act = torch.empty(R, F, dtype=torch.bfloat16, device=dout.device)
-    dcombine = torch.empty(T, k, dtype=torch.float32, device=dout.device)
+    dz = dout.new_empty((R, 2 * F))
+    act = dout.new_empty((R, F))
+    dcombine = combine.new_empty((T, k))
     if R:
         L = dl.lib()
-        ws = torch.empty(int(L.do_expert_up_backward_workspace_size(T, k, F)), dtype=torch.uint8,
-                         device=dout.device)
+        n = L.do_expert_up_backward_workspace_size(T, k, F)
+        ws = dout.new_empty(n, dtype=torch.uint8)
         dl._check("do_expert_up_backward", L.do_expert_up_backward(
             dout.data_ptr(), w2.data_ptr(), kept.codes.data_ptr(), kept.exponents.data_ptr(),
             combine.data_ptr(), rows.data_ptr(), offsets.data_ptr(), pos.data_ptr(), T, k, H, F, E,
             dz.data_ptr(), act.data_ptr(), dcombine.data_ptr(), _status(dev), ws.data_ptr(),
-            ws.numel(), _raw_stream(dev)))
+            n, _raw_stream(dev)))
     return dz, act, dcombine
 
 
@@ -254,7 +255,7 @@ def grouped_weight_grad(p: torch.Tensor, q: torch.Tensor, offsets: torch.Tensor,
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the out to add to")
-        out = torch.empty(E, M, N, dtype=torch.float32, device=p.device)
+        out = p.new_empty((E, M, N), dtype=torch.float32)
     _fp32("out", out, (E, M, N), dev)
     if R == 0:
         return out if accumulate else out.zero_()
@@ -316,7 +317,7 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     T, H = x.shape
     E, F2, Hw = w1.shape
     F = F2 // 2
-    if Hw != H or F2 % 2 or tuple(w2.shape) != (E, H, F) or combine.dim() != 2:
+    if Hw != H or F2 % 2 or w2.shape != (E, H, F) or combine.dim() != 2:
         raise ValueError("w1 must be [E, 2F, H], w2 [E, H, F] and combine [T, k] for x [T, H]")
     k = combine.shape[1]
     _fp32("combine", combine, (T, k), dev)
@@ -329,7 +330,7 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     if T:
         L = dl.lib()
         n = L.do_expert_ffn_workspace_size(T, k, H, F)
-        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+        ws = x.new_empty(n, dtype=torch.uint8)
         dl._check("do_expert_ffn", L.do_expert_ffn(
             x.data_ptr(), w1.data_ptr(), w2.data_ptr(), combine.data_ptr(), rows.data_ptr(),
             offsets.data_ptr(), pos.data_ptr(), T, k, H, F, E, out.data_ptr(), _status(dev),
