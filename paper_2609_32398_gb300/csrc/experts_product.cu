@@ -9,7 +9,8 @@
 // is the N side, whose width may be any multiple of 16.  An expert's n rows are
 // ceil(n / 256) tiles of equal width, so that a ragged group wastes at most 15
 // columns a tile (a fixed 256-row tile would waste 128 rows an expert on average)
-// and a decode step's groups of one or two rows take tiles 16 wide.
+// and a decode step's groups of one or two rows take tiles 16 wide.  Where that is too
+// few tiles for half of the pairs, 128 or 64 rows are the most instead.
 //
 // A persistent CTA pair (cta_group::2, 256 weight rows x up to 256 routed rows in
 // 2 x 256 TMEM columns, so that one tile's epilogue runs under the next tile's
@@ -279,34 +280,44 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     }
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
     pdl_wait();
-    // the first tile of each expert: a scan of ceil(n / 256) m_tiles over the experts
-    int carry = 0;
-    for (int base = 0; base <= E; base += kThreads) {
-        const int e = base + (int)threadIdx.x;
-        int c = 0;
-        if (e <= E) start[e] = max(0, min(__ldg(p.offsets + e), (int)p.R));
-        if (e < E) {
-            const int n = max(0, max(0, min(__ldg(p.offsets + e + 1), (int)p.R)) - start[e]);
-            const int nt = (n + kTileN - 1) / kTileN;
-            width[e] = nt > 0 ? ((n + nt - 1) / nt + 15) & ~15 : 0;
-            c = nt * a.m_tiles;
-        }
-        int x = c;
+    // The first tile of each expert: a scan of ceil(n / cap) m_tiles over the experts.  Tiles
+    // are 256 rows at most, or 128 or 64 while that leaves half of the pairs without one:
+    // a tile's time is mostly its epilogue then, which narrower tiles divide.  T = 1000, H = 512,
+    // F = 256, E = 8, k = 2, against 256 always: the gradient 17.9 to 13.4 us, up 9.7 to 8.4, a
+    // plain product 8.8 to 8.4; T = 1000, H = 2048, F = 768 (48 tiles, not divided) 20.6 either way.
+    const int pairs = (int)(gridDim.x >> 1);
+    int carry;
+    for (int cap = kTileN;; cap /= 2) {
+        carry = 0;
+        int wide = 0;  // some group could be divided further
+        for (int base = 0; base <= E; base += kThreads) {
+            const int e = base + (int)threadIdx.x;
+            int c = 0, n = 0;
+            if (e <= E) start[e] = max(0, min(__ldg(p.offsets + e), (int)p.R));
+            if (e < E) {
+                n = max(0, max(0, min(__ldg(p.offsets + e + 1), (int)p.R)) - start[e]);
+                const int nt = (n + cap - 1) / cap;
+                width[e] = nt > 0 ? ((n + nt - 1) / nt + 15) & ~15 : 0;
+                c = nt * a.m_tiles;
+            }
+            int x = c;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(kFull, x, o);
-            if (lane >= o) x += y;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(kFull, x, o);
+                if (lane >= o) x += y;
+            }
+            if (lane == 31) s_part[warp] = x;
+            wide |= __syncthreads_or(n > cap / 2);
+            int before = carry, all = 0;
+            for (int i = 0; i < kThreads / 32; ++i) {
+                if (i < warp) before += s_part[i];
+                all += s_part[i];
+            }
+            if (e < E) first[e] = before + x - c;
+            carry += all;
+            __syncthreads();
         }
-        if (lane == 31) s_part[warp] = x;
-        __syncthreads();
-        int before = carry, all = 0;
-        for (int i = 0; i < kThreads / 32; ++i) {
-            if (i < warp) before += s_part[i];
-            all += s_part[i];
-        }
-        if (e < E) first[e] = before + x - c;
-        carry += all;
-        __syncthreads();
+        if (!wide || cap == 64 || 2 * carry > pairs) break;
     }
     if (threadIdx.x == 0) first[E] = carry;
     tc_fence_before();
@@ -315,7 +326,7 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     const int steps = (p.K + 63) / 64;
-    Walk walk{first, start, width, carry, (int)(gridDim.x >> 1), a.m_tiles, a.m_magic, (int)(blockIdx.x >> 1), 0, {}};
+    Walk walk{first, start, width, carry, pairs, a.m_tiles, a.m_magic, (int)(blockIdx.x >> 1), 0, {}};
     const Tile &tl = walk.tile;
     const uint32_t ring = smem_u32(smem), full0 = smem_u32(full), empty0 = smem_u32(empty);
     const uint32_t full_pair = map_to_rank(full, 0);  // the first CTA's
@@ -593,8 +604,8 @@ cudaError_t launch(const ProductArgs &p, cudaStream_t s) {
     constexpr auto kernel = product_kernel<kMode, kGather, kTransposed>;
     cudaError_t e = ensure_smem_limit<kernel>(kSmemLimit - 2048);
     if (e != cudaSuccess) return e;
-    // at most R groups have rows, and a group of n rows has n / 256 + 1 tiles at most
-    const int64_t most = (p.R / kTileN + min64(p.R, p.E)) * a.m_tiles;
+    // at most R groups have rows, and a group of n rows has n / 64 + 1 tiles at most
+    const int64_t most = (p.R / 64 + min64(p.R, p.E)) * a.m_tiles;
     const int64_t pairs = min64(most, sms / 2);
     return launch_after(kernel, dim3((unsigned)(2 * pairs)), threads_of(kMode, kGather), smem, s, wmap, amap, a);
 }

@@ -283,3 +283,51 @@ def test_short_steps_leave_no_warp_behind(ex, gather):  # noqa: F811
         assert torch.equal(ex.grouped_weight_grad(ga, gq, go, gr, None), dw)
         assert torch.equal(ex.grouped_matmul(ga, gw, go, gr), y)
     ok(ex)
+
+
+@pytest.mark.parametrize("n", [63, 65, 128, 129, 255, 256, 257, 513])
+@pytest.mark.parametrize("blocks", [1, 9, 20, 40])
+def test_tile_widths_follow_the_number_of_tiles(ex, n, blocks):  # noqa: F811
+    """Few tiles are divided and many are not: group sizes at the edges of each width, with
+    one to forty tiles of weights, through every epilogue."""
+    counts, K, F, T = [n, 0, 1, n + 1], 72, 128 * blocks - 16, 31
+    off, R = ref.groups(counts), 2 * n + 2
+    rows = torch.randint(0, T, (R,), generator=torch.Generator().manual_seed(n))
+    a, w = rnd(n, T, K), rnd(n + blocks, 4, 2 * F, K, scale=0.2)
+    z, mz = ref.product(a, w, off, rows)
+    act = ref.swiglu(z)
+    ga, gw, go, gr = gpu(a, w, off, rows)
+    got = ex.grouped_matmul(ga, gw, go, gr)
+    up, kept = ex.expert_up(ga, gw, go, gr, checkpoint=True)
+    ok(ex)
+    within(got, z, 2 * K * U * mz + BF * z.abs())
+    d = 2 * K * U * mz
+    dg, du, gate, u = d[:, :F], d[:, F:], z[:, :F].abs(), z[:, F:].abs()
+    within(up, act, 1.1 * dg * u + gate * du + 2 * dg * du + (BF + FN) * act.abs())
+    top = (z.abs() + d).reshape(R, -1, 16).amax(-1, keepdim=True).expand(R, F // 8, 16).reshape(R, 2 * F)
+    within(kept.values(), z, top / 127 + d)
+
+
+@pytest.mark.parametrize("T,E", [(63, 2), (128, 1), (129, 3), (515, 2)])
+@pytest.mark.parametrize("F", [48, 1296, 5120])
+def test_tile_widths_of_the_gradient(ex, T, E, F):  # noqa: F811
+    H, k, g = 72, 1, torch.Generator().manual_seed(T + F)
+    ids = torch.randint(0, E, (T, k), generator=g)
+    off, rows, pos = ref.dispatch(ids, E)
+    dout, w2 = rnd(1, T, H, scale=0.1), rnd(2, E, H, F, scale=0.1)
+    combine = torch.rand(T, k, generator=g)
+    codes, exps = ref.quantise(torch.randn(T * k, 2 * F, generator=g) * 2)
+    z = ref.values(codes, exps)
+    dz, act, dc, gr, gm, w, a1 = ref.up_backward(dout, w2, z, combine, off, rows, pos)
+    gd, gw, gc, go, grw, gp, gco, gex = gpu(dout, w2, combine, off, rows, pos, codes, exps)
+    got_z, got_a, got_c = ex.expert_up_backward(gd, gw, ex.Checkpoint(gco, gex), gc, go, grw, gp)
+    ok(ex)
+    d = 2 * H * U * gm
+    gate, up = z[:, :F], z[:, F:].abs()
+    s = torch.sigmoid(gate)
+    slope = torch.cat([w * up * s * (1 + gate.abs() * (1 - s)), w * gate.abs() * s], 1)
+    gg = torch.cat([gr, gr], 1).abs()
+    within(got_z, dz, slope * torch.cat([d, d], 1) * 1.01 + 4 * FN * slope * gg + BF * dz.abs())
+    within(got_a, act, (BF + 2 * FN) * act.abs())
+    bound = ((d * a1.abs()) * 1.01 + (2 * F * U + 2 * FN) * (gr * a1).abs()).sum(1)[pos]
+    within(got_c, dc, bound)
