@@ -461,8 +461,10 @@ do_status do_rem_allocate(const double *loads, const double *expert_tokens,
  *  - Every matrix is dense, row-major and 16-byte aligned; its columns are a
  *    multiple of 8 (F, where it is named, of 16) and at most 2^17; E <= 1024.
  *    Other sizes return DO_ERR_UNSUPPORTED.
- *  - Groups may be empty or of any length.  offsets is read as given, clipped to
- *    [0, R]; routed rows at or past offsets[E] are not written.
+ *  - Groups may be empty or of any length.  offsets ascends; it is clipped to
+ *    [0, R] and may begin above zero (a slice of the experts).  Routed rows before
+ *    offsets[0] and at or past offsets[E] are not written, and a choice whose pos
+ *    names one is left out.
  *  - Products run on the tensor cores or the ALU with bf16 operands, fp32
  *    accumulation and one rounding of the result; results are identical run to run.
  *  - A NaN or an infinity in a row of one expert, or in an expert without rows,
@@ -502,7 +504,7 @@ do_status do_grouped_matmul(const void *A, const void *W, const int32_t *rows,
 /* do_grouped_matmul on rows A [T k][K] in dispatch order, and the sum of each
  * token's k rows: out [T][N] bf16 = sum_q weights[t][q] Y[pos[t][q]] in fp32
  * (weights [T][k] fp32; NULL: one each, as the gradient of a layer's input
- * wants).  A pos outside [0, offsets[E]) is left out.  workspace:
+ * wants).  A pos outside [offsets[0], offsets[E]) is left out.  workspace:
  * do_grouped_matmul_join_workspace_size bytes, 256-byte aligned, of any content
  * (it holds Y); none of it is read by a later call. */
 do_status do_grouped_matmul_join(const void *A, const void *W, const int32_t *offsets,

@@ -78,14 +78,15 @@ struct WeightGradArgs {
 cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s);
 
 // out[t][n] = sum_q weights[t][q] Y[pos[t][q]][n] (weights null: all one) in fp32,
-// rounded once.  A pos outside [0, offsets[E]) is left out and recorded.
+// rounded once.  A pos outside [offsets[0], offsets[E]) is left out and recorded.
 // Y is fp32 where `wide`, else bf16.
 cudaError_t launch_join(const void *Y, bool wide, const int *pos, const float *weights, const int *offsets,
                         int64_t T, int k, int N, int E, bf16 *out, int *status, cudaStream_t s);
-// row_weight[pos[t][q]] = combine[t][q]
-cudaError_t launch_row_weights(const float *combine, const int *pos, int64_t R, float *row_weight,
-                               int *status, cudaStream_t s);
-// dcombine[t][q] = sum over the strips of strips[.][pos[t][q]], in order
+// row_weight[pos[t][q]] = combine[t][q].  A pos outside [offsets[0], offsets[E]) is recorded.
+cudaError_t launch_row_weights(const float *combine, const int *pos, const int *offsets, int E, int64_t R,
+                               float *row_weight, int *status, cudaStream_t s);
+// dcombine[t][q] = sum over the strips of strips[.][pos[t][q]], in order; 0 for a pos
+// outside [offsets[0], offsets[E])
 cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos, const int *offsets,
                               int E, int64_t R, float *dcombine, cudaStream_t s);
 cudaError_t launch_checkpoint_values(const int8_t *codes, const uint8_t *exponents, int64_t rows,
@@ -109,6 +110,13 @@ inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, si
 }
 
 // ---------------------------------------------------------------- device helpers
+
+// The routed rows that groups hold, offsets[0] .. offsets[E] clipped to [0, R]: the others
+// are written by no product, so that nothing may read what their places hold.
+__device__ __forceinline__ int2 rows_of_groups(const int *offsets, int E, int64_t R) {
+    const int lo = __ldg(offsets), hi = __ldg(offsets + E);
+    return make_int2(max(lo, 0), (int)min64(max(hi, 0), R));
+}
 
 // 8-bit checkpoint of a block of 16 values: codes in [-127, 127] times 2^(e - 127),
 // e the exponent byte.  e is the least in [1, 250] with max |v| <= 127 * 2^(e - 127):

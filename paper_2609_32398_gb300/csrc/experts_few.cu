@@ -29,9 +29,11 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
 }
 
 // How many of the E groups end at or before each of n routed rows: the rows' experts
-// (E: none has it).  Four loads of 32 group ends at a time.
+// (E: none has it; nor has any a row before the first group).  Four loads of 32 group ends
+// at a time.
 template <int n>
 __device__ __forceinline__ void experts_of(const int *offsets, int E, const int (&row)[n], int lane, int (&e)[n]) {
+    const int lo = __ldg(offsets);
 #pragma unroll
     for (int q = 0; q < n; ++q) e[q] = 0;
     for (int base = 0; base < E; base += 128) {
@@ -46,6 +48,9 @@ __device__ __forceinline__ void experts_of(const int *offsets, int E, const int 
 #pragma unroll
             for (int q = 0; q < n; ++q) e[q] += __popc(__ballot_sync(kFull, end[j] <= row[q] && end[j] != 0x7fffffff));
     }
+#pragma unroll
+    for (int q = 0; q < n; ++q)
+        if (row[q] < lo) e[q] = E;
 }
 
 // A warp takes kCols result columns of one routed row at a time, kPieces 16-byte

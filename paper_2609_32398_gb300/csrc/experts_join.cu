@@ -23,7 +23,7 @@ struct Picks {
     float w[8];
 };
 __device__ __forceinline__ Picks read_picks(const int *pos, const float *weights, int64_t t, int k, int q0,
-                                            int limit, int *status) {
+                                            int2 in, int *status) {
     Picks p;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
@@ -33,7 +33,7 @@ __device__ __forceinline__ Picks read_picks(const int *pos, const float *weights
     bool bad = false;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-        const bool out = p.row[q] < 0 || p.row[q] >= limit;
+        const bool out = p.row[q] < in.x || p.row[q] >= in.y;
         bad |= out && q0 + q < k;
         if (out) p.row[q] = -1;
     }
@@ -52,13 +52,12 @@ join_kernel(const Y *__restrict__ y, const int *__restrict__ pos, const float *_
             const int *__restrict__ offsets, int64_t T, int k, int N, int E, int cx, bf16 *__restrict__ out,
             int *status) {
     pdl_wait();
-    const int64_t rows = T * k;
-    const int limit = (int)min64(max(__ldg(offsets + E), 0), rows);
+    const int2 in = rows_of_groups(offsets, E, T * k);
     const int c = (int)blockIdx.y * 256 + (int)threadIdx.x % cx, per = 256 / cx;
     const int64_t step = (int64_t)gridDim.x * per;
     int64_t t = (int64_t)blockIdx.x * per + (int)threadIdx.x / cx;
     if (c >= N / 8 || t >= T) return;
-    Picks now = read_picks(pos, weights, t, k, 0, limit, status);
+    Picks now = read_picks(pos, weights, t, k, 0, in, status);
     for (; t < T; t += step) {
         float acc[8] = {};
         for (int q0 = 0; q0 < k; q0 += 8) {
@@ -92,21 +91,23 @@ join_kernel(const Y *__restrict__ y, const int *__restrict__ pos, const float *_
                     }
                 }
             }
-            if (q0 + 8 < k) now = read_picks(pos, weights, t, k, q0 + 8, limit, status);
-            else if (t + step < T) now = read_picks(pos, weights, t + step, k, 0, limit, status);
+            if (q0 + 8 < k) now = read_picks(pos, weights, t, k, q0 + 8, in, status);
+            else if (t + step < T) now = read_picks(pos, weights, t + step, k, 0, in, status);
         }
         reinterpret_cast<uint4 *>(out + t * N)[c] = make_uint4(pack2(acc[0], acc[1]), pack2(acc[2], acc[3]),
                                                                pack2(acc[4], acc[5]), pack2(acc[6], acc[7]));
     }
 }
 
-__global__ void row_weights_kernel(const float *__restrict__ combine, const int *__restrict__ pos, int64_t R,
-                                   float *__restrict__ row_weight, int *status) {
+__global__ void row_weights_kernel(const float *__restrict__ combine, const int *__restrict__ pos,
+                                   const int *__restrict__ offsets, int E, int64_t R, float *__restrict__ row_weight,
+                                   int *status) {
     pdl_wait();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= R) return;
     const int p = pos[i];
-    if (p >= 0 && p < R) row_weight[p] = combine[i];
+    const int2 in = rows_of_groups(offsets, E, R);
+    if (p >= in.x && p < in.y) row_weight[p] = combine[i];
     else if (status) atomicOr(status, kDevBadId);
 }
 
@@ -116,8 +117,9 @@ __global__ void strip_sums_kernel(const float *__restrict__ strips, int n, const
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= R) return;
     const int p = pos[i];
+    const int2 in = rows_of_groups(offsets, E, R);
     float s = 0.0f;
-    if (p >= 0 && p < R && p < offsets[E])
+    if (p >= in.x && p < in.y)
 #pragma unroll 8
         for (int j = 0; j < n; ++j) s += strips[(int64_t)j * R + p];
     dcombine[i] = s;
@@ -171,10 +173,10 @@ cudaError_t launch_join(const void *Y, bool wide, const int *pos, const float *w
                         T, k, N, E, cx, out, status);
 }
 
-cudaError_t launch_row_weights(const float *combine, const int *pos, int64_t R, float *row_weight, int *status,
-                               cudaStream_t s) {
-    return launch_after(row_weights_kernel, dim3((unsigned)((R + 255) / 256)), 256, 0, s, combine, pos, R, row_weight,
-                        status);
+cudaError_t launch_row_weights(const float *combine, const int *pos, const int *offsets, int E, int64_t R,
+                               float *row_weight, int *status, cudaStream_t s) {
+    return launch_after(row_weights_kernel, dim3((unsigned)((R + 255) / 256)), 256, 0, s, combine, pos, offsets, E, R,
+                        row_weight, status);
 }
 
 cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos, const int *offsets, int E,

@@ -1,0 +1,129 @@
+"""What the expert operators promise beside their formulas: routed rows and choices
+that are left out, with the workspace of any content; gradients that are whole or
+refused; checks of shapes; captures.  Bounds as in test_experts_gpu.py."""
+import pytest
+import torch
+
+import experts_ref as ref
+from test_experts_gpu import BF, FN, U, ex, gpu, layer, ok, rnd, within  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def raw(name, *args):
+    """A call of the C ABI on the current stream: tensors by their address, a NULL for None."""
+    from paper_2609_32398_gb300 import doloss as dl
+
+    st = getattr(dl.lib(), name)(*[a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args],
+                                 torch.cuda.current_stream().cuda_stream)
+    assert st == 0, dl.status_string(st)
+
+
+def of_nans(name, *sizes):
+    """A workspace of that call that holds NaNs, and its size."""
+    from paper_2609_32398_gb300 import doloss as dl
+
+    n = getattr(dl.lib(), name)(*sizes)
+    return torch.full((n,), 255, dtype=torch.uint8, device="cuda"), n
+
+
+def recorded(status):
+    from paper_2609_32398_gb300 import doloss as dl
+
+    return dl.lib().do_device_status(status.data_ptr(), torch.cuda.current_stream().cuda_stream)
+
+
+def word():
+    return torch.zeros(64, dtype=torch.int32, device="cuda")
+
+
+def chosen(seed, T, k, E):
+    g = torch.Generator().manual_seed(seed)
+    return torch.stack([torch.randperm(E, generator=g)[:k] for _ in range(T)])
+
+
+def gradient_bounds(one, z, w2, F, H):
+    """Bounds of dz, w act and dcombine by row, from ref.up_backward's results."""
+    dz, act, _, g, gm, w, a = one
+    d = 2 * H * U * gm
+    gate, up = z[:, :F], z[:, F:].abs()
+    s = torch.sigmoid(gate)
+    slope = torch.cat([w * up * s * (1 + gate.abs() * (1 - s)), w * gate.abs() * s], 1)
+    gg = torch.cat([g, g], 1).abs()
+    return (slope * torch.cat([d, d], 1) * 1.01 + 4 * FN * slope * gg + BF * dz.abs(), (BF + 2 * FN) * act.abs(),
+            ((d * a.abs()) * 1.01 + (2 * F * U + 2 * FN) * (g * a).abs()).sum(1))
+
+
+@pytest.mark.parametrize("T,k", [(1, 8), (2, 8), (40, 3)])
+@pytest.mark.parametrize("first", [5, 9])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_join_with_the_offsets_of_a_slice(ex, T, k, first, transposed):  # noqa: F811
+    """Offsets that begin above zero: choices before them are left out and recorded, whatever
+    the workspace held."""
+    E, K, N = 12, 72, 136
+    off, _, pos = ref.dispatch(chosen(T + first, T, k, E), E)
+    a, w = rnd(T, T * k, K), rnd(2, E, *((K, N) if transposed else (N, K)), scale=0.1)
+    c = torch.rand(T, k, generator=torch.Generator().manual_seed(first))
+    lo = int(off[first])
+    assert lo > 0
+    y, m = ref.product(a, w, off, None, transposed)
+    cw = (c.double() * (pos >= lo)).unsqueeze(-1)
+    out = (y[pos] * cw).sum(1)
+    ga, gw, go, gp, gc = gpu(a, w[first:], off[first:], pos, c)
+    ws, n = of_nans("do_grouped_matmul_join_workspace_size", T, k, N)
+    got, status = torch.empty(T, N, dtype=torch.bfloat16, device="cuda"), word()
+    raw("do_grouped_matmul_join", ga, gw, go, gp, gc, T, k, K, N, E - first, int(transposed), got, status, ws, n)
+    assert recorded(status) == 1
+    within(got, out, ((2 * (K + 2 * k) * U * m[pos]) * cw).sum(1) + BF * out.abs())
+
+
+@pytest.mark.parametrize("R", [9, 16, 17, 90])
+@pytest.mark.parametrize("gather", [False, True])
+def test_products_with_the_offsets_of_a_slice(ex, R, gather):  # noqa: F811
+    """Rows before offsets[0] are not written."""
+    E, first, K, N, F, T = 6, 2, 72, 40, 48, 11
+    g = torch.Generator().manual_seed(R)
+    off = ref.groups(torch.bincount(torch.randint(0, E, (R,), generator=g), minlength=E).tolist())
+    lo = int(off[first])
+    assert 0 < lo < R
+    a, w, w1 = rnd(1, T if gather else R, K), rnd(2, E, N, K, scale=0.2), rnd(3, E, 2 * F, K, scale=0.2)
+    rows = torch.randint(0, T, (R,), generator=g) if gather else None
+    y, m = ref.product(a, w, off, rows)
+    z, mz = ref.product(a, w1, off, rows)
+    act = ref.swiglu(z)
+    ga, gw, gw1, go, gr = gpu(a, w[first:], w1[first:], off[first:], rows)
+    got = torch.full((R, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    up = torch.full((R, F), 7.0, dtype=torch.bfloat16, device="cuda")
+    raw("do_grouped_matmul", ga, gw, gr, go, a.shape[0], K, N, E - first, R, 0, got, None)
+    raw("do_expert_up", ga, gw1, gr, go, a.shape[0], K, F, E - first, R, up, None, None, None)
+    assert (got[:lo] == 7).all() and (up[:lo] == 7).all()
+    within(got[lo:], y[lo:], (2 * K * U * m + BF * y.abs())[lo:])
+    d = 2 * K * U * mz
+    dg, du, gate, u = d[:, :F], d[:, F:], z[:, :F].abs(), z[:, F:].abs()
+    within(up[lo:], act[lo:], (1.1 * dg * u + gate * du + 2 * dg * du + (BF + FN) * act.abs())[lo:])
+
+
+@pytest.mark.parametrize("T,k,F", [(1, 8, 48), (40, 3, 208)])
+def test_gradient_with_the_offsets_of_a_slice(ex, T, k, F):  # noqa: F811
+    E, first, H = 12, 6, 72
+    off, rows, pos = ref.dispatch(chosen(T, T, k, E), E)
+    R, lo = T * k, int(off[first])
+    assert 0 < lo < R
+    dout, w2 = rnd(1, T, H, scale=0.1), rnd(2, E, H, F, scale=0.1)
+    c = torch.rand(T, k, generator=torch.Generator().manual_seed(k))
+    codes, exps = ref.quantise(torch.randn(R, 2 * F, generator=torch.Generator().manual_seed(F)) * 2)
+    z = ref.values(codes, exps)
+    one = ref.up_backward(dout, w2, z, c, off, rows, pos)
+    bz, ba, bc = gradient_bounds(one, z, w2, F, H)
+    gd, gw, gco, gex, gc, grw, go, gp = gpu(dout, w2[first:], codes, exps, c, rows, off[first:], pos)
+    ws, n = of_nans("do_expert_up_backward_workspace_size", T, k, F)
+    dz = torch.full((R, 2 * F), 7.0, dtype=torch.bfloat16, device="cuda")
+    act = torch.full((R, F), 7.0, dtype=torch.bfloat16, device="cuda")
+    dc, status = torch.empty(T, k, device="cuda"), word()
+    raw("do_expert_up_backward", gd, gw, gco, gex, gc, grw, go, gp, T, k, H, F, E - first, dz, act, dc, status, ws, n)
+    assert recorded(status) == 1
+    assert (dz[:lo] == 7).all() and (act[:lo] == 7).all()
+    within(dz[lo:], one[0][lo:], bz[lo:])
+    within(act[lo:], one[1][lo:], ba[lo:])
+    kept = pos >= lo
+    within(dc, torch.where(kept, one[2], 0.0), torch.where(kept, bc[pos], 0.0))
