@@ -537,6 +537,8 @@ size_t do_expert_ffn_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F);
  *   act [R][F] bf16     w a, the operand of dW2 beside dout (so that neither the
  *                       layer's rows of output nor their gradient are ever kept)
  *   dcombine [T][k] fp32  sum_f g_r[f] a_r[f]
+ * A choice whose pos is outside [offsets[0], offsets[E]) is left out: its dcombine
+ * is 0, and a routed row that no choice names has w = 0.
  * workspace: do_expert_up_backward_workspace_size bytes, 256-byte aligned, of
  * any content. */
 do_status do_expert_up_backward(const void *dout, const void *W2, const void *codes,

@@ -199,7 +199,7 @@ do_status do_expert_up_backward(const void *dout, const void *W2, const void *co
     a.dz = static_cast<dol::bf16 *>(dz);
     a.row_weight = row_weight;
     a.strips = row_weight + R;
-    cudaError_t e = dol::launch_row_weights(combine, pos, offsets, E, R, row_weight, status_flags, s);
+    cudaError_t e = dol::launch_row_weights(combine, rows, pos, offsets, E, T, k, row_weight, status_flags, s);
     if (e == cudaSuccess) e = dol::launch_product(dol::kProductUpGrad, a, s);
     if (e == cudaSuccess) e = dol::launch_strip_sums(a.strips, (F + dol::kStrip - 1) / dol::kStrip, pos, offsets, E, R, dcombine, s);
     return dol::of(e);

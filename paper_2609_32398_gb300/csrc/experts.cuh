@@ -82,9 +82,10 @@ cudaError_t launch_weight_grad(const WeightGradArgs &a, cudaStream_t s);
 // Y is fp32 where `wide`, else bf16.
 cudaError_t launch_join(const void *Y, bool wide, const int *pos, const float *weights, const int *offsets,
                         int64_t T, int k, int N, int E, bf16 *out, int *status, cudaStream_t s);
-// row_weight[pos[t][q]] = combine[t][q].  A pos outside [offsets[0], offsets[E]) is recorded.
-cudaError_t launch_row_weights(const float *combine, const int *pos, const int *offsets, int E, int64_t R,
-                               float *row_weight, int *status, cudaStream_t s);
+// row_weight[r] = combine[t][q] with t = rows[r] and pos[t][q] = r; 0 for a row that no
+// choice of its token names.  A pos outside [offsets[0], offsets[E]) is recorded.
+cudaError_t launch_row_weights(const float *combine, const int *rows, const int *pos, const int *offsets, int E,
+                               int64_t T, int k, float *row_weight, int *status, cudaStream_t s);
 // dcombine[t][q] = sum over the strips of strips[.][pos[t][q]], in order; 0 for a pos
 // outside [offsets[0], offsets[E])
 cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos, const int *offsets,

@@ -99,16 +99,34 @@ join_kernel(const Y *__restrict__ y, const int *__restrict__ pos, const float *_
     }
 }
 
-__global__ void row_weights_kernel(const float *__restrict__ combine, const int *__restrict__ pos,
-                                   const int *__restrict__ offsets, int E, int64_t R, float *__restrict__ row_weight,
-                                   int *status) {
+// A routed row looks its choice up among its token's k (and is not told by the choice): every
+// row then has a weight, also one that no choice names.
+__global__ void row_weights_kernel(const float *__restrict__ combine, const int *__restrict__ rows,
+                                   const int *__restrict__ pos, const int *__restrict__ offsets, int E, int64_t T,
+                                   int k, float *__restrict__ row_weight, int *status) {
     pdl_wait();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= R) return;
-    const int p = pos[i];
+    const int64_t R = T * k, r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (r >= R) return;
+    const int t = __ldg(rows + r), p = __ldg(pos + r);
     const int2 in = rows_of_groups(offsets, E, R);
-    if (p >= in.x && p < in.y) row_weight[p] = combine[i];
-    else if (status) atomicOr(status, kDevBadId);
+    float w = 0.0f;
+    if (t >= 0 && t < T) {
+        const int64_t at = (int64_t)t * k;
+        for (int q0 = 0; q0 < k; q0 += 8) {  // positions and weights in flight together
+            int named[8];
+            float c[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                named[q] = q0 + q < k ? __ldg(pos + at + q0 + q) : -1;
+                c[q] = q0 + q < k ? __ldg(combine + at + q0 + q) : 0.0f;
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (named[q] == r) w = c[q];
+        }
+    }
+    row_weight[r] = w;
+    if ((p < in.x || p >= in.y) && status) atomicOr(status, kDevBadId);
 }
 
 __global__ void strip_sums_kernel(const float *__restrict__ strips, int n, const int *__restrict__ pos,
@@ -173,10 +191,10 @@ cudaError_t launch_join(const void *Y, bool wide, const int *pos, const float *w
                         T, k, N, E, cx, out, status);
 }
 
-cudaError_t launch_row_weights(const float *combine, const int *pos, const int *offsets, int E, int64_t R,
-                               float *row_weight, int *status, cudaStream_t s) {
-    return launch_after(row_weights_kernel, dim3((unsigned)((R + 255) / 256)), 256, 0, s, combine, pos, offsets, E, R,
-                        row_weight, status);
+cudaError_t launch_row_weights(const float *combine, const int *rows, const int *pos, const int *offsets, int E,
+                               int64_t T, int k, float *row_weight, int *status, cudaStream_t s) {
+    return launch_after(row_weights_kernel, dim3((unsigned)((T * k + 255) / 256)), 256, 0, s, combine, rows, pos, offsets,
+                        E, T, k, row_weight, status);
 }
 
 cudaError_t launch_strip_sums(const float *strips, int n_strips, const int *pos, const int *offsets, int E,

@@ -127,3 +127,41 @@ def test_gradient_with_the_offsets_of_a_slice(ex, T, k, F):  # noqa: F811
     within(act[lo:], one[1][lo:], ba[lo:])
     kept = pos >= lo
     within(dc, torch.where(kept, one[2], 0.0), torch.where(kept, bc[pos], 0.0))
+
+
+def test_a_choice_left_out_of_the_gradient(ex):  # noqa: F811
+    """A position outside the rows: the routed row that it should have named has no weight, so
+    that its dz and act are zeros, and nothing else changes."""
+    T, k, E, H, F = 40, 3, 5, 72, 208
+    off, rows, pos = ref.dispatch(chosen(1, T, k, E), E)
+    R = T * k
+    dout, w2, x = rnd(1, T, H, scale=0.1), rnd(2, E, H, F, scale=0.1), rnd(3, T, H)
+    c = torch.rand(T, k, generator=torch.Generator().manual_seed(k))
+    codes, exps = ref.quantise(torch.randn(R, 2 * F, generator=torch.Generator().manual_seed(F)) * 2)
+    bad = pos.clone()
+    gone = [int(pos[0, 1]), int(pos[31, 0])]
+    bad[0, 1], bad[31, 0] = -5, 2 ** 31 - 1
+    gd, gw, gco, gex, gc, grw, go, gp, gb, gx = gpu(dout, w2, codes, exps, c, rows, off, pos, bad, x)
+
+    def run(p, status):
+        ws, n = of_nans("do_expert_up_backward_workspace_size", T, k, F)
+        dz = torch.full((R, 2 * F), 7.0, dtype=torch.bfloat16, device="cuda")
+        act, dc = torch.full((R, F), 7.0, dtype=torch.bfloat16, device="cuda"), torch.empty(T, k, device="cuda")
+        raw("do_expert_up_backward", gd, gw, gco, gex, gc, grw, go, p, T, k, H, F, E, dz, act, dc, status, ws, n)
+        return dz, act, dc
+
+    status = word()
+    dz, act, dc = run(gp, status)
+    assert recorded(status) == 0
+    want = [t.clone() for t in (dz, act, dc)]
+    want[0][gone] = 0
+    want[1][gone] = 0
+    want[2][0, 1] = want[2][31, 0] = 0
+    got = run(gb, status)
+    assert recorded(status) == 1
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for grad in (lambda z, a: ex.grouped_weight_grad(z, gx, go, None, grw),
+                 lambda z, a: ex.grouped_weight_grad(gd, a, go, grw, None)):
+        assert torch.equal(grad(*got[:2]), grad(*want[:2]))
+    ok(ex)
