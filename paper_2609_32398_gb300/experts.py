@@ -281,23 +281,40 @@ class _ExpertFFN(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dout):
-        x, w1, w2, combine, offsets, rows, pos, codes, exponents = ctx.saved_tensors
-        dout = dout.contiguous()
-        dz, act, dcombine = expert_up_backward(dout, w2, Checkpoint(codes, exponents), combine,
-                                               offsets, rows, pos)
-        need = ctx.needs_input_grad
-        dw1 = dw2 = dx = None
-        if ctx.main_grads is not None:
-            grouped_weight_grad(dz, x, offsets, None, rows, out=ctx.main_grads[0], accumulate=True)
-            grouped_weight_grad(dout, act, offsets, rows, None, out=ctx.main_grads[1], accumulate=True)
-        else:
-            if need[1]:
-                dw1 = grouped_weight_grad(dz, x, offsets, None, rows)
-            if need[2]:
-                dw2 = grouped_weight_grad(dout, act, offsets, rows, None)
-        if need[0]:
-            dx = grouped_matmul_join(dz, w1, offsets, pos, None, transposed=True)
-        return dx, dw1, dw2, dcombine, None, None, None, None
+        args = (dout.contiguous(), *ctx.saved_tensors, ctx.main_grads, ctx.needs_input_grad)
+        # under create_graph the gradients get a graph too, whose only node raises
+        grads = (_ExpertFFNGrad.apply if torch.is_grad_enabled() else _expert_ffn_grad)(*args)
+        return (*grads, None, None, None, None)
+
+
+def _expert_ffn_grad(dout, x, w1, w2, combine, offsets, rows, pos, codes, exponents, main_grads, need):
+    """(dx, dw1, dw2, dcombine) of the layer, None where not needed."""
+    dz, act, dcombine = expert_up_backward(dout, w2, Checkpoint(codes, exponents), combine, offsets, rows, pos)
+    dw1 = dw2 = dx = None
+    if main_grads is not None:
+        grouped_weight_grad(dz, x, offsets, None, rows, out=main_grads[0], accumulate=True)
+        grouped_weight_grad(dout, act, offsets, rows, None, out=main_grads[1], accumulate=True)
+    else:
+        if need[1]:
+            dw1 = grouped_weight_grad(dz, x, offsets, None, rows)
+        if need[2]:
+            dw2 = grouped_weight_grad(dout, act, offsets, rows, None)
+    if need[0]:
+        dx = grouped_matmul_join(dz, w1, offsets, pos, None, transposed=True)
+    return dx, dw1, dw2, dcombine
+
+
+class _ExpertFFNGrad(torch.autograd.Function):
+    """The layer's gradients as a node without a derivative: the kernels leave no graph, so
+    that second-order terms through x, the weights, combine or dout would be left out."""
+
+    @staticmethod
+    def forward(ctx, *args):
+        return _expert_ffn_grad(*args)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("expert_ffn has no second derivative")
 
 
 def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: torch.Tensor,
@@ -305,9 +322,10 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
                main_grads: tuple[torch.Tensor, torch.Tensor] | None = None) -> torch.Tensor:
     """The experts of one MoE layer: out[t] = sum_q combine[t,q] W2_e (silu(g) * u)
     with (g, u) = W1_e x[t], e the q-th expert of token t; out [T,H] bf16.
-    Differentiable in x, w1, w2 and combine; the backward pass works from 8-bit
-    pre-activations.  main_grads: (dw1 [E,2F,H], dw2 [E,H,F]) fp32 buffers that
-    the weights' gradients are added to instead of being returned."""
+    Differentiable once in x, w1, w2 and combine (a second derivative raises); the
+    backward pass works from 8-bit pre-activations.  main_grads: (dw1 [E,2F,H],
+    dw2 [E,H,F]) fp32 buffers that the weights' gradients are added to instead of
+    being returned."""
     if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w2, combine)):
         return _ExpertFFN.apply(x, w1, w2, combine, offsets, rows, pos, main_grads)
     dev = x.get_device()

@@ -165,3 +165,16 @@ def test_a_choice_left_out_of_the_gradient(ex):  # noqa: F811
                  lambda z, a: ex.grouped_weight_grad(gd, a, go, grw, None)):
         assert torch.equal(grad(*got[:2]), grad(*want[:2]))
     ok(ex)
+
+
+def test_a_second_derivative_is_refused(ex):  # noqa: F811
+    """The layer has no second derivative: a graph through its gradient raises instead of
+    leaving its terms out."""
+    x, w1, w2, c, off, rows, pos = layer(3, 20, 2, 4, 64, 32)
+    gx, gw1, gw2, gc, go, gr, gp = gpu(x, w1, w2, c, off, rows, pos)
+    leaves = [t.requires_grad_() for t in (gx, gw1, gw2, gc)]
+    out = ex.expert_ffn(*leaves, go, gr, gp).float().sum()
+    (dx,) = torch.autograd.grad(out, gx, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivative"):
+        (out + dx.float().square().sum()).backward()
+    ok(ex)
