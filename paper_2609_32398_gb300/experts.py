@@ -14,6 +14,9 @@ combine [T,k] fp32 as `doloss.routing()` writes them for one layer
     ids, combine, route = dl.route(z, k)
     offsets, rows, pos = dispatch_of(route)
     out = expert_ffn(x, w1, w2, combine, offsets, rows, pos)    # differentiable
+
+The other calls are the pieces of its forward and backward pass and leave no graph:
+the forward ones raise where an operand requires a gradient and one is recorded.
 """
 from __future__ import annotations
 
@@ -63,6 +66,14 @@ def _index(name: str, t, n: int, device: int) -> None:
                           or t.get_device() != device):
         raise ValueError(f"{name} must be a contiguous CUDA int32 tensor of {n} values, "
                          "all tensors on one device")
+
+
+def _no_graph(name: str, *tensors) -> None:
+    """The pieces of the layer are no autograd nodes: where a graph is being recorded,
+    operands that want one are refused instead of being detached."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise RuntimeError(f"{name} is not differentiable: call it under torch.no_grad(), or take expert_ffn, "
+                           "whose gradients are")
 
 
 def _fp32(name: str, t, shape: tuple, device: int) -> None:
@@ -115,7 +126,8 @@ def expert_up(x: torch.Tensor, w1: torch.Tensor, offsets: torch.Tensor,
               rows: torch.Tensor | None = None, checkpoint: bool = False):
     """do_expert_up: act [R,F] bf16 = silu(z_gate) * z_up with z = x[rows] W1^T
     of each row's expert, and with `checkpoint` the Checkpoint of z (else None).
-    rows [R] None: the R rows of x are in dispatch order."""
+    rows [R] None: the R rows of x are in dispatch order.  Not differentiable."""
+    _no_graph("expert_up", x, w1)
     dev = x.get_device()
     _bf16("x", x, 2, dev)
     _bf16("w1", w1, 3, dev)
@@ -152,7 +164,8 @@ def grouped_matmul(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
                    rows: torch.Tensor | None = None, transposed: bool = False) -> torch.Tensor:
     """do_grouped_matmul: y [R,N] bf16, row r = a[rows[r]] (or a[r]) times the
     weights of its expert: w [E,N,K] (y = a w^T), or [E,K,N] where transposed
-    (y = a w)."""
+    (y = a w).  Not differentiable."""
+    _no_graph("grouped_matmul", a, w)
     dev = a.get_device()
     _bf16("a", a, 2, dev)
     _bf16("w", w, 3, dev)
@@ -173,7 +186,8 @@ def grouped_matmul_join(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
                         weights: torch.Tensor | None = None, transposed: bool = False) -> torch.Tensor:
     """do_grouped_matmul_join: out [T,N] bf16, the products of grouped_matmul on
     the rows a [T*k,K] in dispatch order, summed per token over its rows
-    pos [T,k] with weights [T,k] fp32 (None: one each)."""
+    pos [T,k] with weights [T,k] fp32 (None: one each).  Not differentiable."""
+    _no_graph("grouped_matmul_join", a, w, weights)
     dev = a.get_device()
     _bf16("a", a, 2, dev)
     _bf16("w", w, 3, dev)

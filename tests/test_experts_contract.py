@@ -1,0 +1,42 @@
+"""What the expert operators' binding refuses on the host, before it touches a tensor's
+memory or a device."""
+import pytest
+import torch
+
+from paper_2609_32398_gb300 import experts as ex
+
+T, k, E, H, F = 4, 1, 2, 64, 16
+
+
+def operands():
+    """One of each operand, on the CPU: a call that gets past the checks tested here is
+    refused as not being on a GPU, by a ValueError."""
+    return dict(x=torch.zeros(T, H).bfloat16(), w1=torch.zeros(E, 2 * F, H).bfloat16(),
+                w2=torch.zeros(E, H, F).bfloat16(), a=torch.zeros(T * k, F).bfloat16(), combine=torch.zeros(T, k),
+                offsets=torch.zeros(E + 1, dtype=torch.int32), rows=torch.zeros(T * k, dtype=torch.int32),
+                pos=torch.zeros(T, k, dtype=torch.int32))
+
+
+# the layer's forward pieces, and their operands that have derivatives
+CALLS = {
+    "expert_up": (lambda o: ex.expert_up(o["x"], o["w1"], o["offsets"], o["rows"]), ("x", "w1")),
+    "grouped_matmul": (lambda o: ex.grouped_matmul(o["a"], o["w2"], o["offsets"]), ("a", "w2")),
+    "grouped_matmul_join": (lambda o: ex.grouped_matmul_join(o["a"], o["w2"], o["offsets"], o["pos"], o["combine"]),
+                            ("a", "w2", "combine")),
+}
+EACH = [(name, operand) for name, (_, has) in CALLS.items() for operand in has]
+
+
+@pytest.mark.parametrize("name,operand", EACH)
+def test_a_call_that_leaves_no_graph_refuses_operands_that_want_one(name, operand):
+    """Of the forward calls only expert_ffn is an autograd node: the others raise where a
+    gradient would be lost."""
+    o = operands()
+    o[operand].requires_grad_()
+    with pytest.raises(RuntimeError, match="expert_ffn"):
+        CALLS[name][0](o)
+    with torch.no_grad(), pytest.raises(ValueError):    # as without a gradient: not on a GPU
+        CALLS[name][0](o)
+    o[operand] = o[operand].detach()
+    with pytest.raises(ValueError):
+        CALLS[name][0](o)
