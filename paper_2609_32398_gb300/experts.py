@@ -23,6 +23,7 @@ from __future__ import annotations
 import threading
 
 import torch
+import torch.autograd.forward_ad as fwd
 
 from . import doloss as dl
 
@@ -68,9 +69,16 @@ def _index(name: str, t, n: int, device: int) -> None:
                          "all tensors on one device")
 
 
+def _no_tangent(name: str, *tensors) -> None:
+    """Forward-mode derivatives are refused: a kernel would drop the tangent."""
+    if fwd._current_level >= 0 and any(t is not None and fwd.unpack_dual(t).tangent is not None for t in tensors):
+        raise RuntimeError(f"{name} has no forward-mode derivative")
+
+
 def _no_graph(name: str, *tensors) -> None:
     """The pieces of the layer are no autograd nodes: where a graph is being recorded,
     operands that want one are refused instead of being detached."""
+    _no_tangent(name, *tensors)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         raise RuntimeError(f"{name} is not differentiable: call it under torch.no_grad(), or take expert_ffn, "
                            "whose gradients are")
@@ -340,6 +348,7 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     backward pass works from 8-bit pre-activations.  main_grads: (dw1 [E,2F,H],
     dw2 [E,H,F]) fp32 buffers that the weights' gradients are added to instead of
     being returned."""
+    _no_tangent("expert_ffn", x, w1, w2, combine)
     if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w2, combine)):
         return _ExpertFFN.apply(x, w1, w2, combine, offsets, rows, pos, main_grads)
     dev = x.get_device()

@@ -2,6 +2,7 @@
 memory or a device."""
 import pytest
 import torch
+import torch.autograd.forward_ad as fwd
 
 from paper_2609_32398_gb300 import experts as ex
 
@@ -40,3 +41,22 @@ def test_a_call_that_leaves_no_graph_refuses_operands_that_want_one(name, operan
     o[operand] = o[operand].detach()
     with pytest.raises(ValueError):
         CALLS[name][0](o)
+
+
+LAYER = {**CALLS, "expert_ffn": (lambda o: ex.expert_ffn(o["x"], o["w1"], o["w2"], o["combine"], o["offsets"],
+                                                         o["rows"], o["pos"]), ("x", "w1", "w2", "combine"))}
+
+
+@pytest.mark.parametrize("name,operand", [(name, operand) for name, (_, has) in LAYER.items() for operand in has])
+def test_forward_mode_derivatives_are_refused(name, operand):
+    """A dual tensor needs no requires_grad: its tangent would be lost."""
+    with fwd.dual_level():
+        o = operands()
+        o[operand] = fwd.make_dual(o[operand], torch.ones_like(o[operand]))
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            LAYER[name][0](o)
+        with torch.no_grad(), pytest.raises(RuntimeError, match="forward-mode"):   # which does not turn it off
+            LAYER[name][0](o)
+        o[operand] = fwd.unpack_dual(o[operand]).primal
+        with pytest.raises(ValueError):
+            LAYER[name][0](o)
