@@ -3,7 +3,8 @@ with ragged groups, the SwiGLU up projection with its 8-bit activation
 checkpoint, the gradients, and the layer as one autograd node.
 
 Argument marshalling over libdoloss.so (include/doloss.h); torch supplies
-device memory and the current stream.  There is no CPU fallback.
+device memory and the current stream.  There is no CPU fallback, and the tensors
+of a call are on the current device.
 
 Layouts: tokens x [T,H], expert weights w1 [E,2F,H] (gate rows, then up rows)
 and w2 [E,H,F], all bf16; offsets [E+1], rows [T*k] and pos [T,k] int32 and
@@ -49,7 +50,16 @@ def device_status(device="cuda") -> int:
     module recorded on the device: 0, DO_ERR_TIMEOUT or DO_ERR_INVALID_ARG (a
     row or position outside its matrix, left out)."""
     t = torch.empty(0, device=device)
-    return int(dl.lib().do_device_status(_status(t.get_device()), dl._stream(t)))
+    return int(dl.lib().do_device_status(_status(_device(t)), dl._stream(t)))
+
+
+def _device(t: torch.Tensor) -> int:
+    """The device of a call's tensors (-1: the CPU), which has to be the current one: streams
+    and launches are the current device's."""
+    dev = t.get_device()
+    if dev >= 0 and dev != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{dev}, which is not the current device")
+    return dev
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream if torch.cuda.is_available() else None
@@ -113,8 +123,8 @@ class Checkpoint:
     def values(self) -> torch.Tensor:
         """The values it stands for, bf16 [R, 2F] (7 significant bits: exact)."""
         codes = self.codes
+        dev = _device(codes)
         R, n = codes.shape
-        dev = codes.get_device()
         self.check(R, n // 2, dev)
         out = codes.new_empty((R, n), dtype=torch.bfloat16)
         if R:
@@ -136,7 +146,7 @@ def expert_up(x: torch.Tensor, w1: torch.Tensor, offsets: torch.Tensor,
     of each row's expert, and with `checkpoint` the Checkpoint of z (else None).
     rows [R] None: the R rows of x are in dispatch order.  Not differentiable."""
     _no_graph("expert_up", x, w1)
-    dev = x.get_device()
+    dev = _device(x)
     _bf16("x", x, 2, dev)
     _bf16("w1", w1, 3, dev)
     T, H = x.shape
@@ -174,7 +184,7 @@ def grouped_matmul(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     weights of its expert: w [E,N,K] (y = a w^T), or [E,K,N] where transposed
     (y = a w).  Not differentiable."""
     _no_graph("grouped_matmul", a, w)
-    dev = a.get_device()
+    dev = _device(a)
     _bf16("a", a, 2, dev)
     _bf16("w", w, 3, dev)
     E, N, K = _weights(a, w, transposed)
@@ -196,7 +206,7 @@ def grouped_matmul_join(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     the rows a [T*k,K] in dispatch order, summed per token over its rows
     pos [T,k] with weights [T,k] fp32 (None: one each).  Not differentiable."""
     _no_graph("grouped_matmul_join", a, w, weights)
-    dev = a.get_device()
+    dev = _device(a)
     _bf16("a", a, 2, dev)
     _bf16("w", w, 3, dev)
     E, N, K = _weights(a, w, transposed)
@@ -225,7 +235,7 @@ def expert_up_backward(dout: torch.Tensor, w2: torch.Tensor, kept: Checkpoint,
     through the join, the down projection w2 [E,H,F] and the activation, from
     the 8-bit checkpoint.  Returns (dz [R,2F] bf16, act [R,F] bf16 times each
     row's combine weight, the operand of dW2, dcombine [T,k] fp32)."""
-    dev = dout.get_device()
+    dev = _device(dout)
     _bf16("dout", dout, 2, dev)
     _bf16("w2", w2, 3, dev)
     T, H = dout.shape
@@ -262,7 +272,7 @@ def grouped_weight_grad(p: torch.Tensor, q: torch.Tensor, offsets: torch.Tensor,
     """do_grouped_weight_grad: dw [E,M,N] fp32, dw[e] = sum over the expert's rows
     r of p[p_rows[r]]^T q[q_rows[r]] (p [.,M], q [.,N] bf16; rows None: r itself).
     With accumulate it is added to `out`."""
-    dev = p.get_device()
+    dev = _device(p)
     _bf16("p", p, 2, dev)
     _bf16("q", q, 2, dev)
     sizes = {t.numel() for t in (p_rows, q_rows) if t is not None}
@@ -349,9 +359,9 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     dw2 [E,H,F]) fp32 buffers that the weights' gradients are added to instead of
     being returned."""
     _no_tangent("expert_ffn", x, w1, w2, combine)
+    dev = _device(x)
     if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w2, combine)):
         return _ExpertFFN.apply(x, w1, w2, combine, offsets, rows, pos, main_grads)
-    dev = x.get_device()
     _bf16("x", x, 2, dev)
     _bf16("w1", w1, 3, dev)
     _bf16("w2", w2, 3, dev)

@@ -60,3 +60,26 @@ def test_forward_mode_derivatives_are_refused(name, operand):
         o[operand] = fwd.unpack_dual(o[operand]).primal
         with pytest.raises(ValueError):
             LAYER[name][0](o)
+
+
+class Elsewhere:
+    """Stands for a tensor of device 1: all that may be asked of it before it is refused."""
+
+    requires_grad = False
+
+    def get_device(self):
+        return 1
+
+
+def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
+    """The streams and kernels of a call are the current device's: a tensor of another one is
+    refused before anything is launched or read of it."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    t = Elsewhere()
+    kept = ex.Checkpoint(t, t)
+    for call in (lambda: ex.expert_up(t, t, t, t), lambda: ex.grouped_matmul(t, t, t),
+                 lambda: ex.grouped_matmul_join(t, t, t, t, t), lambda: kept.values(),
+                 lambda: ex.expert_up_backward(t, t, kept, t, t, t, t), lambda: ex.grouped_weight_grad(t, t, t),
+                 lambda: ex.expert_ffn(t, t, t, t, t, t, t)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
