@@ -116,6 +116,10 @@ def _check(fn: str, status: int):
 
 
 def _stream(t: torch.Tensor) -> int:
+    """The current stream of a call on t, whose device has to be the current one: the handle of
+    a default stream is the same for all devices and stands for the current device's."""
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {t.device}, which is not the current device")
     return torch.cuda.current_stream(t.device).cuda_stream
 
 
@@ -504,7 +508,7 @@ def forward_backward_host(h_logits: torch.Tensor, k, gate=GATE_SIGMOID_NORM, gra
     _check("do_forward_backward_host", lib().do_forward_backward_host(
         z.data_ptr(), T, E, k, L, gate, grad_scale, h_loss.data_ptr(), _ptr(h_dlogits),
         _ptr(h_counts), _ptr(h_D), device_buffer.data_ptr(), device_buffer.numel(),
-        torch.cuda.current_stream(device_buffer.device).cuda_stream))
+        _stream(device_buffer)))
     return h_loss
 
 
@@ -521,10 +525,12 @@ def forward_backward_host_async(h_logits: torch.Tensor, k, h_result: torch.Tenso
     L, T, E = z.shape
     if h_result.is_cuda or h_result.numel() * h_result.element_size() < 4 * (L + 1):
         raise ValueError("h_result must be a CPU tensor of at least 4 (L + 1) bytes")
-    st = stream if stream is not None else torch.cuda.current_stream(device_buffer.device)
+    st = _stream(device_buffer)  # checks the buffer's device also where a stream is given
+    if stream is not None:
+        st = stream.cuda_stream
     _check("do_forward_backward_host_async", lib().do_forward_backward_host_async(
         z.data_ptr(), T, E, k, L, gate, grad_scale, h_result.data_ptr(), device_buffer.data_ptr(),
-        device_buffer.numel(), st.cuda_stream))
+        device_buffer.numel(), st))
 
 
 def host_result(h_result: torch.Tensor, L: int):
