@@ -62,7 +62,9 @@ def _device(t: torch.Tensor) -> int:
     return dev
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream if torch.cuda.is_available() else None
+# (not torch.cuda.is_available(): asking the driver here would leave the children of a later
+# fork without their GPU)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _bf16(name: str, t: torch.Tensor, dim: int, device: int) -> None:

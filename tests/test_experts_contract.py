@@ -83,3 +83,19 @@ def test_tensors_of_a_device_that_is_not_current_are_refused(monkeypatch):
                  lambda: ex.expert_ffn(t, t, t, t, t, t, t)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_importing_the_module_leaves_forked_children_their_gpu():
+    """Nothing asks the driver for devices at import: a process may fork workers after it."""
+    import os
+    import subprocess
+    import sys
+
+    code = ("import os, torch, paper_2609_32398_gb300.experts\n"
+            "pid = os.fork()\n"
+            "if pid == 0:\n"
+            "    os._exit(3 if torch.cuda._is_in_bad_fork() else 0)\n"
+            "sys_exit = os.waitstatus_to_exitcode(os.waitpid(pid, 0)[1])\n"
+            "raise SystemExit(sys_exit)\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    assert subprocess.run([sys.executable, "-c", code], cwd=root, timeout=300).returncode == 0
