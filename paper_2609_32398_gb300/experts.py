@@ -103,6 +103,14 @@ def _fp32(name: str, t, shape: tuple, device: int) -> None:
                          "all tensors on one device")
 
 
+def _positions(pos: torch.Tensor, T: int, k: int, device: int) -> torch.Tensor:
+    """pos as [T, k], which a flat one of T*k values is too."""
+    _index("pos", pos, T * k, device)
+    if pos.dim() != 1 and pos.shape != (T, k):
+        raise ValueError(f"pos must be [T, k], here {[T, k]}")
+    return pos.view(T, k)
+
+
 class Checkpoint:
     """Pre-activations [R, 2F] kept in 8 bits: codes int8 [R, 2F] and exponents
     uint8 [R, 2F/16]; the value of a code is code * 2^(e - 127), e the exponent
@@ -251,7 +259,7 @@ def expert_up_backward(dout: torch.Tensor, w2: torch.Tensor, kept: Checkpoint,
     _fp32("combine", combine, (T, k), dev)
     _index("offsets", offsets, E + 1, dev)
     _index("rows", rows, R, dev)
-    _index("pos", pos, R, dev)
+    pos = _positions(pos, T, k, dev)
     kept.check(R, F, dev)
     dz = dout.new_empty((R, 2 * F))
     act = dout.new_empty((R, F))
@@ -362,8 +370,6 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     being returned."""
     _no_tangent("expert_ffn", x, w1, w2, combine)
     dev = _device(x)
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w2, combine)):
-        return _ExpertFFN.apply(x, w1, w2, combine, offsets, rows, pos, main_grads)
     _bf16("x", x, 2, dev)
     _bf16("w1", w1, 3, dev)
     _bf16("w2", w2, 3, dev)
@@ -376,7 +382,9 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     _fp32("combine", combine, (T, k), dev)
     _index("offsets", offsets, E + 1, dev)
     _index("rows", rows, T * k, dev)
-    _index("pos", pos, T * k, dev)
+    pos = _positions(pos, T, k, dev)
+    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w2, combine)):
+        return _ExpertFFN.apply(x, w1, w2, combine, offsets, rows, pos, main_grads)
     if k == 0:
         return x.new_zeros((T, H))
     out = x.new_empty((T, H))

@@ -178,3 +178,30 @@ def test_a_second_derivative_is_refused(ex):  # noqa: F811
     with pytest.raises(RuntimeError, match="second derivative"):
         (out + dx.float().square().sum()).backward()
     ok(ex)
+
+
+def test_shapes_are_checked_alike_with_and_without_gradients(ex):  # noqa: F811
+    T, k, E, H, F = 20, 2, 4, 64, 32
+    x, w1, w2, c, off, rows, pos = layer(5, T, k, E, H, F)
+    gx, gw1, gw2, gc, go, gr, gp = gpu(x, w1, w2, c, off, rows, pos)
+    good = dict(x=gx, w1=gw1, w2=gw2, combine=gc, offsets=go, rows=gr, pos=gp)
+    bad = [dict(pos=gp.T.contiguous()), dict(combine=gc.T.contiguous()), dict(combine=gc.reshape(-1)),
+           dict(w2=rnd(1, E, H + 8, F).cuda()), dict(w2=rnd(1, E + 1, H, F).cuda()), dict(w1=rnd(1, E, 2 * F, H + 8).cuda()),
+           dict(x=rnd(1, T + 1, H).cuda()), dict(rows=gr[:-1])]
+    for train in (False, True):
+        for t in (gx, gw1, gw2, gc):
+            t.requires_grad_(train)
+        for change in bad:
+            with pytest.raises(ValueError):
+                ex.expert_ffn(**{**good, **change})
+    # the positions in one dimension are the same memory
+    flat = {**good, "pos": gp.reshape(-1)}
+    want = ex.expert_ffn(**good)
+    assert torch.equal(ex.expert_ffn(**flat), want)
+    with torch.no_grad():
+        assert torch.equal(ex.expert_ffn(**flat), ex.expert_ffn(**good))
+    codes, exps = ref.quantise(torch.randn(T * k, 2 * F, generator=torch.Generator().manual_seed(1)))
+    kept = ex.Checkpoint(*gpu(codes, exps))
+    with torch.no_grad(), pytest.raises(ValueError):
+        ex.expert_up_backward(gx, gw2, kept, gc, go, gr, gp.T.contiguous())
+    ok(ex)
