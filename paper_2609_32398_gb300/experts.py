@@ -383,6 +383,11 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     _index("offsets", offsets, E + 1, dev)
     _index("rows", rows, T * k, dev)
     pos = _positions(pos, T, k, dev)
+    if main_grads is not None:
+        if len(main_grads) != 2 or any(b is None for b in main_grads):
+            raise ValueError("main_grads must be a pair of buffers, of w1 and of w2")
+        _fp32("main_grads[0]", main_grads[0], w1.shape, dev)
+        _fp32("main_grads[1]", main_grads[1], w2.shape, dev)
     if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w2, combine)):
         return _ExpertFFN.apply(x, w1, w2, combine, offsets, rows, pos, main_grads)
     if k == 0:

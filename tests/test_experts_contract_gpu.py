@@ -205,3 +205,19 @@ def test_shapes_are_checked_alike_with_and_without_gradients(ex):  # noqa: F811
     with torch.no_grad(), pytest.raises(ValueError):
         ex.expert_up_backward(gx, gw2, kept, gc, go, gr, gp.T.contiguous())
     ok(ex)
+
+
+def test_buffers_of_the_weights_gradients_are_checked_in_the_forward_call(ex):  # noqa: F811
+    T, k, E, H, F = 20, 2, 4, 64, 32
+    x, w1, w2, c, off, rows, pos = layer(5, T, k, E, H, F)
+    args = gpu(x, w1, w2, c, off, rows, pos)
+    bufs = (torch.zeros(E, 2 * F, H, device="cuda"), torch.zeros(E, H, F, device="cuda"))
+    for train in (False, True):
+        for t in args[:4]:
+            t.requires_grad_(train)
+        for bad in (bufs[::-1], (bufs[0], bufs[1].half()), bufs[:1], (bufs[0], bufs[1].cpu()), (None, bufs[1]),
+                    (bufs[0].transpose(1, 2).contiguous().transpose(1, 2), bufs[1])):
+            with pytest.raises(ValueError):
+                ex.expert_ffn(*args, main_grads=bad)
+        ex.expert_ffn(*args, main_grads=bufs)
+    ok(ex)
