@@ -226,6 +226,8 @@ def grouped_matmul_join(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
     _index("offsets", offsets, E + 1, dev)
     _index("pos", pos, T * k, dev)
     _fp32("weights", weights, (T, k), dev)
+    if k == 0:
+        return a.new_zeros((T, N))
     out = a.new_empty((T, N))
     if T:
         L = dl.lib()

@@ -221,3 +221,18 @@ def test_buffers_of_the_weights_gradients_are_checked_in_the_forward_call(ex):  
                 ex.expert_ffn(*args, main_grads=bad)
         ex.expert_ffn(*args, main_grads=bufs)
     ok(ex)
+
+
+def test_a_layer_without_choices_has_gradients(ex):  # noqa: F811
+    """k = 0: zeros, and zeros for gradients."""
+    T, E, H, F = 6, 4, 64, 32
+    x, w1, w2 = rnd(1, T, H), rnd(2, E, 2 * F, H), rnd(3, E, H, F)
+    none = torch.zeros(T, 0, dtype=torch.int64)
+    gx, gw1, gw2, gc, go, gr, gp = gpu(x, w1, w2, torch.zeros(T, 0), torch.zeros(E + 1, dtype=torch.int64),
+                                       none.reshape(-1), none)
+    leaves = [t.requires_grad_() for t in (gx, gw1, gw2, gc)]
+    out = ex.expert_ffn(*leaves, go, gr, gp)
+    assert out.shape == (T, H) and (out == 0).all()
+    for g, t in zip(torch.autograd.grad(out, leaves, torch.ones_like(out)), leaves):
+        assert g.shape == t.shape and (g == 0).all()
+    ok(ex)
