@@ -335,14 +335,14 @@ def _expert_ffn_grad(dout, x, w1, w2, combine, offsets, rows, pos, codes, expone
     """(dx, dw1, dw2, dcombine) of the layer, None where not needed."""
     dz, act, dcombine = expert_up_backward(dout, w2, Checkpoint(codes, exponents), combine, offsets, rows, pos)
     dw1 = dw2 = dx = None
-    if main_grads is not None:
-        grouped_weight_grad(dz, x, offsets, None, rows, out=main_grads[0], accumulate=True)
-        grouped_weight_grad(dout, act, offsets, rows, None, out=main_grads[1], accumulate=True)
-    else:
-        if need[1]:
-            dw1 = grouped_weight_grad(dz, x, offsets, None, rows)
-        if need[2]:
-            dw2 = grouped_weight_grad(dout, act, offsets, rows, None)
+    add = main_grads is not None
+    to1, to2 = main_grads if add else (None, None)
+    if need[1]:
+        dw1 = grouped_weight_grad(dz, x, offsets, None, rows, out=to1, accumulate=add)
+    if need[2]:
+        dw2 = grouped_weight_grad(dout, act, offsets, rows, None, out=to2, accumulate=add)
+    if add:  # nothing else is returned for them
+        dw1 = dw2 = None
     if need[0]:
         dx = grouped_matmul_join(dz, w1, offsets, pos, None, transposed=True)
     return dx, dw1, dw2, dcombine
@@ -368,8 +368,8 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     with (g, u) = W1_e x[t], e the q-th expert of token t; out [T,H] bf16.
     Differentiable once in x, w1, w2 and combine (a second derivative raises); the
     backward pass works from 8-bit pre-activations.  main_grads: (dw1 [E,2F,H],
-    dw2 [E,H,F]) fp32 buffers that the weights' gradients are added to instead of
-    being returned."""
+    dw2 [E,H,F]) fp32 buffers that the gradients of the weights that require one are
+    added to instead of being returned."""
     _no_tangent("expert_ffn", x, w1, w2, combine)
     dev = _device(x)
     _bf16("x", x, 2, dev)

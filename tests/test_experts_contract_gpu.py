@@ -236,3 +236,20 @@ def test_a_layer_without_choices_has_gradients(ex):  # noqa: F811
     for g, t in zip(torch.autograd.grad(out, leaves, torch.ones_like(out)), leaves):
         assert g.shape == t.shape and (g == 0).all()
     ok(ex)
+
+
+@pytest.mark.parametrize("frozen", [0, 1])
+def test_a_frozen_weight_takes_no_gradient(ex, frozen):  # noqa: F811
+    """Weights that require no gradient leave their buffer of main_grads as it was."""
+    x, w1, w2, c, off, rows, pos = layer(7, 30, 2, 4, 64, 32)
+    gx, gw1, gw2, gc, go, gr, gp = gpu(x, w1, w2, c, off, rows, pos)
+    for t in (gx, gw1, gw2, gc):
+        t.requires_grad_()
+    full = [torch.full(w.shape, 2.0, device="cuda") for w in (gw1, gw2)]
+    ex.expert_ffn(gx, gw1, gw2, gc, go, gr, gp, main_grads=tuple(full)).float().sum().backward()
+    (gw1, gw2)[frozen].requires_grad_(False)
+    bufs = [torch.full(w.shape, 2.0, device="cuda") for w in (gw1, gw2)]
+    ex.expert_ffn(gx, gw1, gw2, gc, go, gr, gp, main_grads=tuple(bufs)).float().sum().backward()
+    assert (bufs[frozen] == 2.0).all()
+    assert torch.equal(bufs[1 - frozen], full[1 - frozen]) and not (full[1 - frozen] == 2.0).all()
+    ok(ex)
