@@ -34,9 +34,13 @@ _flag_ptrs: dict[int, int] = {}
 
 
 def _status(device: int) -> int:
-    """Address of the device's status word, which every call on it may set."""
+    """Address of the device's status word, which every call on it may set.  It is made by the
+    first call, which therefore cannot be captured."""
     p = _flag_ptrs.get(device)
     if p is None:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the first call of this module on a device makes its status word, outside of a graph "
+                               "capture: call device_status() before the capture")
         with _flags_lock:
             f = torch.zeros(64, dtype=torch.int32, device=f"cuda:{device}")
             torch.cuda.synchronize(device)  # cleared for every stream
@@ -47,8 +51,11 @@ def _status(device: int) -> int:
 
 def device_status(device="cuda") -> int:
     """Synchronizes the current stream, returns and clears what the calls of this
-    module recorded on the device: 0, DO_ERR_TIMEOUT or DO_ERR_INVALID_ARG (a
-    row or position outside its matrix, left out)."""
+    module recorded on the device, on any stream: 0, DO_ERR_TIMEOUT (a bounded
+    wait ran out: results of calls since the last poll may be wrong) or
+    DO_ERR_INVALID_ARG (a row or position outside its matrix, left out).  There is
+    one word a device, which a poll clears for everybody.  A call before the first
+    graph capture makes it."""
     t = torch.empty(0, device=device)
     return int(dl.lib().do_device_status(_status(_device(t)), dl._stream(t)))
 

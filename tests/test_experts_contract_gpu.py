@@ -253,3 +253,30 @@ def test_a_frozen_weight_takes_no_gradient(ex, frozen):  # noqa: F811
     assert (bufs[frozen] == 2.0).all()
     assert torch.equal(bufs[1 - frozen], full[1 - frozen]) and not (full[1 - frozen] == 2.0).all()
     ok(ex)
+
+
+def test_the_first_call_of_a_capture_is_refused_in_words(ex, monkeypatch):  # noqa: F811
+    """The device's status word is made by the first call, which a capture cannot hold: it is
+    refused before anything is captured, and the capture goes on."""
+    x, w = rnd(1, 20, 64), rnd(2, 1, 40, 64)
+    gx, gw, go = gpu(x, w, ref.groups([20]))
+    want = ex.grouped_matmul(gx, gw, go)
+    ok(ex)
+    with monkeypatch.context() as m:
+        m.setattr(ex, "_flags", {})
+        m.setattr(ex, "_flag_ptrs", {})
+        graph, other = torch.cuda.CUDAGraph(), torch.zeros(8, device="cuda")
+        with torch.cuda.graph(graph):
+            with pytest.raises(RuntimeError, match="capture"):
+                ex.grouped_matmul(gx, gw, go)
+            other += 1
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (other == 1).all()
+        assert ex.device_status() == 0        # makes the word
+        with torch.cuda.graph(graph := torch.cuda.CUDAGraph()):
+            got = ex.grouped_matmul(gx, gw, go)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        ok(ex)
