@@ -278,8 +278,9 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         prefetch_tensormap(&wmap);
         prefetch_tensormap(&amap);
     }
-    if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
     pdl_wait();
+    // not before: the kernel before may share this SM and still have to take its own
+    if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
     // The first tile of each expert: a scan of ceil(n / cap) m_tiles over the experts.  Tiles
     // are 256 rows at most, or 128 or 64 while that leaves half of the pairs without one:
     // a tile's time is mostly its epilogue then, which narrower tiles divide.  T = 1000, H = 512,

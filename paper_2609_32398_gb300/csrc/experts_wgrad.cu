@@ -158,8 +158,9 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
         prefetch_tensormap(&qmap);
         prefetch_tensormap(&omap);
     }
-    if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
     pdl_wait();
+    // not before: the kernel before may share this SM and still have to take its own
+    if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
     const int blocks = out_blocks(a.E);
     int *start = reinterpret_cast<int *>(smem + kStages * kStage + kEpiWarps * blocks * kOut);
     for (int i = threadIdx.x; i <= a.E; i += kThreads) start[i] = max(0, min(__ldg(a.offsets + i), (int)a.R));
