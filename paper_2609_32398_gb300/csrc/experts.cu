@@ -2,7 +2,7 @@
 #include <climits>
 
 #include "doloss.h"
-#include "experts.cuh"
+#include "experts_mma.cuh"
 
 namespace dol {
 namespace {
@@ -10,13 +10,20 @@ namespace {
 bool off(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Sizes that every call shares.  Columns are whole 16-byte pieces (8 bf16 values), and
-// few enough that divide_by is exact for every tile that fits the memory.
+// Sizes that every call shares.  Columns are whole 16-byte pieces (8 bf16 values).
 do_status check(int64_t R, int32_t E, int32_t c0, int32_t c1, int step0, int step1) {
     if (R < 1 || E < 1 || c0 < 1 || c1 < 1) return DO_ERR_INVALID_ARG;
     if (E > 1024 || R > INT32_MAX - 256 || c0 % step0 || c1 % step1 || c0 > (1 << 17) || c1 > (1 << 17))
         return DO_ERR_UNSUPPORTED;
     return DO_OK;
+}
+
+// Whether the up projection's tiles of one expert (at most 256 rows each; narrower ones only
+// where there are few) are divided exactly by its weight tiles of 128 columns.  Of the
+// other products, with at most 512 weight tiles, all that fit the memory are.
+do_status check_up_tiles(int64_t R, int32_t F) {
+    const int tiles = (F + 127) / 128;
+    return (uint64_t)((R + 255) / 256) * tiles > divide_limit((uint32_t)tiles) ? DO_ERR_UNSUPPORTED : DO_OK;
 }
 
 // The rows that a join adds are kept in fp32 where they stay in the L2 anyway: the sum
@@ -82,6 +89,8 @@ do_status do_expert_up(const void *X, const void *W1, const int32_t *rows, const
         off(status_flags, 4))
         return DO_ERR_INVALID_ARG;
     if (T > INT32_MAX - 256) return DO_ERR_UNSUPPORTED;
+    st = dol::check_up_tiles(R, F);
+    if (st != DO_OK) return st;
     dol::ProductArgs a = dol::product_args(X, T, rows, W1, offsets, R, H, 2 * F, E, false, act, status_flags);
     a.codes = static_cast<int8_t *>(codes);
     a.exponents = static_cast<uint8_t *>(exponents);
@@ -156,6 +165,8 @@ do_status do_expert_ffn(const void *X, const void *W1, const void *W2, const flo
     if (off(X, 16) || off(W1, 16) || off(W2, 16) || off(out, 16) || off(combine, 4) || off(rows, 4) ||
         off(offsets, 4) || off(pos, 4) || off(status_flags, 4))
         return DO_ERR_INVALID_ARG;
+    st = dol::check_up_tiles(R, F);
+    if (st != DO_OK) return st;
     if (!workspace || off(workspace, 256) || workspace_bytes < do_expert_ffn_workspace_size(T, k, H, F))
         return DO_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -251,8 +251,13 @@ __host__ __device__ constexpr uint32_t pair_idesc(int n, bool a_mn, bool b_mn) {
            ((uint32_t)(n / 8) << 17) | ((uint32_t)(256 / 16) << 24);
 }
 
-// i / d for i d < 2^32, by the product with ceil(2^32 / d) (0 stands for d = 1).
+// i / d for i up to divide_limit(d), by the product with m = ceil(2^32 / d) (0 stands for d
+// = 1): exact while i (m d - 2^32) < 2^32.
 __host__ __device__ inline uint32_t divide_magic(uint32_t d) { return d == 1 ? 0u : 0xffffffffu / d + 1u; }
+inline uint64_t divide_limit(uint32_t d) {
+    const uint64_t over = (uint64_t)divide_magic(d) * d - (1ull << 32);  // below d; 0 for a power of two
+    return d == 1 || over == 0 ? UINT32_MAX : UINT32_MAX / over;
+}
 __device__ __forceinline__ int divide_by(int i, uint32_t magic) {
     return magic ? (int)__umulhi((uint32_t)i, magic) : i;
 }

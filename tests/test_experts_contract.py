@@ -99,3 +99,22 @@ def test_importing_the_module_leaves_forked_children_their_gpu():
             "raise SystemExit(sys_exit)\n")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     assert subprocess.run([sys.executable, "-c", code], cwd=root, timeout=300).returncode == 0
+
+
+@pytest.mark.parametrize("d", [1000, 1021, 1023])
+def test_tiles_that_a_reciprocal_cannot_divide_are_refused(d):
+    """An expert's tiles are divided by its d weight tiles with ceil(2^32 / d), which is exact
+    while a tile's number times (that d - 2^32) stays below 2^32.  Calls that could reach past it
+    (1023 weight tiles, 1,055,232 rows, 276 GB of results) are refused before any launch."""
+    from paper_2609_32398_gb300 import build, doloss as dl
+
+    build.build()
+    magic = 0xffffffff // d + 1
+    last = (2 ** 32 - 1) // (magic * d - 2 ** 32)
+    assert all(i * magic >> 32 == i // d for i in range(last - 3 * d, last + 1))
+    assert any(i * magic >> 32 != i // d for i in range(last + 1, last + 3 * d))
+    R, F = 256 * (last // d + 2), 128 * d
+    fake = 0x10000
+    assert dl.lib().do_expert_up(fake, fake, fake, fake, 1, 8, F, 1, R, fake, None, None, None, None) == 2
+    n = dl.lib().do_expert_ffn_workspace_size(R, 1, 8, F)
+    assert dl.lib().do_expert_ffn(*[fake] * 7, R, 1, 8, F, 1, fake, None, fake, n, None) == 2
