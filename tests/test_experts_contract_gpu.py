@@ -1,6 +1,7 @@
 """What the expert operators promise beside their formulas: routed rows and choices
 that are left out, with the workspace of any content; gradients that are whole or
-refused; checks of shapes; captures.  Bounds as in test_experts_gpu.py."""
+refused; checks of shapes; captures; the variants of every size; the layer entry by entry.
+Bounds as in test_experts_gpu.py."""
 import pytest
 import torch
 
@@ -280,3 +281,130 @@ def test_the_first_call_of_a_capture_is_refused_in_words(ex, monkeypatch):  # no
         torch.cuda.synchronize()
         assert torch.equal(got, want)
         ok(ex)
+
+
+@pytest.mark.parametrize("T,k,N", [(3100, 8, 1032), (2100, 12, 1032), (1600, 4, 4104), (3100, 4, 2056), (300, 4, 4104),
+                                   (90, 9, 2056)])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_wide_and_long_joins(ex, T, k, N, weighted):  # noqa: F811
+    """Both sides of the 25,165,824 values up to which joined rows are kept in fp32, columns
+    past 2048 and more than eight choices."""
+    E, K = 24, 16
+    off, _, pos = ref.dispatch(chosen(T + N, T, k, E), E)
+    a, w = rnd(T, T * k, K), rnd(N, E, N, K, scale=0.3)
+    c = torch.rand(T, k, generator=torch.Generator().manual_seed(T)) if weighted else None
+    y, m = ref.product(a, w, off)
+    cw = (c if weighted else torch.ones(T, k)).double()
+    out, bound = torch.zeros(T, N, dtype=torch.float64), torch.zeros(T, N, dtype=torch.float64)
+    rounded = BF if T * k * N > (96 << 20) // 4 else 0.0     # of each row, before the sum
+    for q in range(k):
+        out += y[pos[:, q]] * cw[:, q:q + 1]
+        bound += (2 * (K + 2 * k) * U * m[pos[:, q]] + rounded * y[pos[:, q]].abs()) * cw[:, q:q + 1]
+    ga, gw, go, gp, gc = gpu(a, w, off, pos, c)
+    got = ex.grouped_matmul_join(ga, gw, go, gp, gc)
+    ok(ex)
+    within(got, out, bound * (1 + BF) + BF * out.abs())
+
+
+@pytest.mark.parametrize("K", [8, 264, 512, 520, 776, 1024, 1032, 2048, 2056, 4104])
+@pytest.mark.parametrize("R", [1, 7, 16])
+@pytest.mark.parametrize("gather", [False, True])
+def test_products_of_few_rows(ex, K, R, gather):  # noqa: F811
+    """Few rows with contractions at the edges of every variant, and odd numbers of columns."""
+    E, N, F, T = 5, 104, 112, 6
+    g = torch.Generator().manual_seed(K + R)
+    off = ref.groups(torch.bincount(torch.randint(0, E, (R,), generator=g), minlength=E).tolist())
+    a, w, w1 = rnd(K, T if gather else R, K), rnd(R, E, N, K, scale=0.1), rnd(R + 1, E, 2 * F, K, scale=1 / K ** 0.5)
+    rows = torch.randint(0, T, (R,), generator=g) if gather else None
+    y, m = ref.product(a, w, off, rows)
+    z, mz = ref.product(a, w1, off, rows)
+    act = ref.swiglu(z)
+    ga, gw, gw1, go, gr = gpu(a, w, w1, off, rows)
+    got = ex.grouped_matmul(ga, gw, go, gr)
+    up, _ = ex.expert_up(ga, gw1, go, gr)
+    ok(ex)
+    within(got, y, 2 * K * U * m + BF * y.abs())
+    d = 2 * K * U * mz
+    dg, du, gate, u = d[:, :F], d[:, F:], z[:, :F].abs(), z[:, F:].abs()
+    within(up, act, 1.1 * dg * u + gate * du + 2 * dg * du + (BF + FN) * act.abs())
+
+
+@pytest.mark.parametrize("K", [768, 776, 1536, 4104])
+@pytest.mark.parametrize("T,k", [(1, 1), (1, 5), (2, 8), (1, 16)])
+def test_joins_of_few_rows_over_long_contractions(ex, K, T, k):  # noqa: F811
+    E, N = 20, 72
+    off, _, pos = ref.dispatch(chosen(K, T, k, E), E)
+    a, w, c = rnd(T, T * k, K), rnd(2, E, N, K, scale=0.1), torch.rand(T, k, generator=torch.Generator().manual_seed(K))
+    y, m = ref.product(a, w, off)
+    cw = c.double().unsqueeze(-1)
+    out = (y[pos] * cw).sum(1)
+    ga, gw, go, gp, gc = gpu(a, w, off, pos, c)
+    got = ex.grouped_matmul_join(ga, gw, go, gp, gc)
+    ok(ex)
+    within(got, out, ((2 * (K + 2 * k) * U * m[pos]) * cw).sum(1) + BF * out.abs())
+
+
+@pytest.mark.parametrize("T,k,E,H,F", [(60, 3, 8, 136, 80), (300, 2, 5, 72, 208), (2, 8, 16, 264, 48)])
+def test_every_entry_of_the_layers_gradients(ex, T, k, E, H, F):  # noqa: F811
+    """The layer's output and gradients entry by entry, in 64 bits from its own checkpoint: which
+    operand goes into which product, with which rounding.  dz and w act are bf16, dW and the
+    joined rows (few here) fp32, dx is rounded once."""
+    x, w1, w2, c, off, rows, pos = layer(T + F, T, k, E, H, F)
+    dout = rnd(T, T, H)
+    gx, gw1, gw2, gc, go, gr, gp, gd = gpu(x, w1, w2, c, off, rows, pos, dout)
+    _, kept = ex.expert_up(gx, gw1, go, gr, checkpoint=True)
+    zk = ref.values(kept.codes.cpu(), kept.exponents.cpu())
+    leaves = [t.requires_grad_() for t in (gx, gw1, gw2, gc)]
+    out = ex.expert_ffn(*leaves, go, gr, gp)
+    dx, dw1, dw2, dc = torch.autograd.grad(out, leaves, gd)
+    ok(ex)
+    # the output: act from the exact z, rounded to bf16
+    z, mz = ref.product(x, w1, off, rows)
+    act = ref.swiglu(z)
+    d = 2 * H * U * mz
+    dg, du, gate, u = d[:, :F], d[:, F:], z[:, :F].abs(), z[:, F:].abs()
+    ba = 1.1 * dg * u + gate * du + 2 * dg * du + (BF + FN) * act.abs()
+    cw = c.double().unsqueeze(-1)
+    y = ref.each(off, H, T * k, lambda e, i, j: act[i:j] @ w2[e].double().T)
+    by = ref.each(off, H, T * k, lambda e, i, j: (ba[i:j] + 2 * (F + 2 * k) * U * act[i:j].abs()) * 1.01
+                  @ w2[e].double().abs().T)
+    want = (y[pos] * cw).sum(1)
+    within(out.detach(), want, (by[pos] * cw).sum(1) + BF * want.abs())
+    # the gradients, from the checkpoint's z
+    one = ref.up_backward(dout, w2, zk, c, off, rows, pos)
+    dz, wact = one[0], one[1]
+    bz, bw, bc = gradient_bounds(one, zk, w2, F, H)
+    within(dc, one[2], bc[pos])
+    xr, dr = x[rows].double(), dout[rows].double()
+    w1d = w1.double()
+    for e in range(E):
+        i, j = int(off[e]), int(off[e + 1])
+        n = max(j - i, 1)
+        # the returned gradients have the leaves' type: one more rounding to bf16
+        g1, g2 = dz[i:j].T @ xr[i:j], dr[i:j].T @ wact[i:j]
+        e1 = (bz[i:j] + 2 * n * U * dz[i:j].abs()).T * 1.01 @ xr[i:j].abs()
+        e2 = dr[i:j].abs().T @ (bw[i:j] + 2 * n * U * wact[i:j].abs()) * 1.01
+        within(dw1[e], g1, e1 * (1 + BF) + BF * g1.abs())
+        within(dw2[e], g2, e2 * (1 + BF) + BF * g2.abs())
+    v = ref.each(off, H, T * k, lambda e, i, j: dz[i:j] @ w1d[e])
+    bv = ref.each(off, H, T * k, lambda e, i, j: (bz[i:j] + 2 * (2 * F + 2 * k) * U * dz[i:j].abs()) * 1.01
+                  @ w1d[e].abs())
+    want = v[pos].sum(1)
+    within(dx, want, bv[pos].sum(1) * (1 + BF) + BF * want.abs())
+
+
+def test_weight_gradient_of_a_collapsed_router(ex):  # noqa: F811
+    """131072 rows of one expert.  A step of 16 rows is one addition to the fp32 accumulator:
+    each of its 17 terms loses at most a unit in the last of 24 bits of the largest, so 2 * 17 U of
+    the partial sum's and the step's magnitudes (the running error bound)."""
+    n, M, N = 131072, 64, 48
+    p, q = rnd(1, n, M), rnd(2, n, N)
+    gp, gq, go = gpu(p, q, ref.groups([n, 0]))
+    dw = ex.grouped_weight_grad(gp, gq, go)
+    ok(ex)
+    ps, qs = p.double().reshape(-1, 16, M), q.double().reshape(-1, 16, N)
+    steps = torch.bmm(ps.transpose(1, 2), qs)
+    mags = torch.bmm(ps.abs().transpose(1, 2), qs.abs())
+    sums = torch.cumsum(steps, 0)
+    within(dw[0], sums[-1], 34 * U * (sums.abs() + mags).sum(0))
+    assert (dw[1] == 0).all()
