@@ -115,12 +115,23 @@ def _check(fn: str, status: int):
         raise DoLossError(fn, status)
 
 
+_only_device = False  # device 0 is the only one, and so the current one
+
+
+def _check_current(index: int) -> None:
+    global _only_device
+    if index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{index}, which is not the current device")
+    _only_device = torch.cuda.device_count() == 1
+
+
 def _stream(t: torch.Tensor) -> int:
     """The current stream of a call on t, whose device has to be the current one: the handle of
     a default stream is the same for all devices and stands for the current device's."""
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {t.device}, which is not the current device")
-    return torch.cuda.current_stream(t.device).cuda_stream
+    device = t.device
+    if not _only_device or device.index != 0:
+        _check_current(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _ptr(t):

@@ -64,8 +64,8 @@ def _device(t: torch.Tensor) -> int:
     """The device of a call's tensors (-1: the CPU), which has to be the current one: streams
     and launches are the current device's."""
     dev = t.get_device()
-    if dev >= 0 and dev != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on cuda:{dev}, which is not the current device")
+    if dev > 0 or (dev == 0 and not dl._only_device):
+        dl._check_current(dev)
     return dev
 
 
@@ -90,15 +90,17 @@ def _index(name: str, t, n: int, device: int) -> None:
 
 def _no_tangent(name: str, *tensors) -> None:
     """Forward-mode derivatives are refused: a kernel would drop the tangent."""
-    if fwd._current_level >= 0 and any(t is not None and fwd.unpack_dual(t).tangent is not None for t in tensors):
+    if any(t is not None and fwd.unpack_dual(t).tangent is not None for t in tensors):
         raise RuntimeError(f"{name} has no forward-mode derivative")
 
 
-def _no_graph(name: str, *tensors) -> None:
+def _no_graph(name: str, a: torch.Tensor, w: torch.Tensor, weights=None) -> None:
     """The pieces of the layer are no autograd nodes: where a graph is being recorded,
     operands that want one are refused instead of being detached."""
-    _no_tangent(name, *tensors)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+    if fwd._current_level >= 0:
+        _no_tangent(name, a, w, weights)
+    if ((a.requires_grad or w.requires_grad or (weights is not None and weights.requires_grad))
+            and torch.is_grad_enabled()):
         raise RuntimeError(f"{name} is not differentiable: call it under torch.no_grad(), or take expert_ffn, "
                            "whose gradients are")
 
@@ -113,7 +115,9 @@ def _fp32(name: str, t, shape: tuple, device: int) -> None:
 def _positions(pos: torch.Tensor, T: int, k: int, device: int) -> torch.Tensor:
     """pos as [T, k], which a flat one of T*k values is too."""
     _index("pos", pos, T * k, device)
-    if pos.dim() != 1 and pos.shape != (T, k):
+    if pos.shape == (T, k):
+        return pos
+    if pos.dim() != 1:
         raise ValueError(f"pos must be [T, k], here {[T, k]}")
     return pos.view(T, k)
 
@@ -377,7 +381,8 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     backward pass works from 8-bit pre-activations.  main_grads: (dw1 [E,2F,H],
     dw2 [E,H,F]) fp32 buffers that the gradients of the weights that require one are
     added to instead of being returned."""
-    _no_tangent("expert_ffn", x, w1, w2, combine)
+    if fwd._current_level >= 0:
+        _no_tangent("expert_ffn", x, w1, w2, combine)
     dev = _device(x)
     _bf16("x", x, 2, dev)
     _bf16("w1", w1, 3, dev)
@@ -397,7 +402,8 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
             raise ValueError("main_grads must be a pair of buffers, of w1 and of w2")
         _fp32("main_grads[0]", main_grads[0], w1.shape, dev)
         _fp32("main_grads[1]", main_grads[1], w2.shape, dev)
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w2, combine)):
+    if ((x.requires_grad or w1.requires_grad or w2.requires_grad or combine.requires_grad)
+            and torch.is_grad_enabled()):
         return _ExpertFFN.apply(x, w1, w2, combine, offsets, rows, pos, main_grads)
     if k == 0:
         return x.new_zeros((T, H))
