@@ -553,7 +553,8 @@ size_t do_expert_up_backward_workspace_size(int64_t T, int32_t k, int32_t F);
 /* Weight gradients: dW [E][M][N] fp32, dW[e] = sum over the expert's routed rows r
  * of P[p_rows[r]]^T Q[q_rows[r]] (P [Tp][M], Q [Tq][N] bf16; p_rows or q_rows
  * NULL: r itself); zero for an expert without rows.  accumulate = 1 adds it to dW
- * instead (each entry once). */
+ * instead.  fp32 throughout: 2048 rows at most are summed in a tensor-core
+ * accumulator, the sums of more of them are added in order. */
 do_status do_grouped_weight_grad(const void *P, const void *Q, const int32_t *p_rows,
                                  const int32_t *q_rows, const int32_t *offsets, int64_t Tp,
                                  int64_t Tq, int32_t M, int32_t N, int32_t E, int64_t R,

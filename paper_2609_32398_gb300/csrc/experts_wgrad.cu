@@ -8,14 +8,19 @@
 // of Q: by TMA where the rows lie in dispatch order, and gathered in 16-byte pieces
 // otherwise, so that neither the tokens nor the outputs' gradient is ever permuted
 // in memory.  An expert's last, partial step is gathered on both sides: what lies
-// past its end are zeros on both, whatever the next expert's rows hold.  Two accumulators in TMEM let one tile's 256 KB of fp32
-// leave while the next tile's products run; an expert without rows gets zeros
-// from the epilogue alone.  The result is stored (or added, once per entry) by
-// TMA from 32 x 32 blocks.
+// past its end are zeros on both, whatever the next expert's rows hold.  Two
+// accumulators in TMEM let one's 256 KB of fp32 leave while the next one's products
+// run; an expert without rows gets zeros from the epilogue alone.  The result is
+// stored by TMA from 32 x 32 blocks.
+//
+// The tensor cores cut off what an addition to an accumulator shifts out, so that its
+// error grows with the additions.  An accumulator therefore takes kSpan rows at
+// most: a tile's first one is stored (or added to dW), and the others, in order and each after
+// the one before has been written, are added to it in memory, where the fp32 sum is rounded.
 //
 // Warps: 0 TMA, 1 issues the MMAs (first CTA), 2-5 epilogue, 6-11 gather.
 //
-// What bounds it: at 16384 tokens (1024 rows an expert, H = 2048, 2F = 1536) 623 us, 1.32
+// What bounds it: at 16384 tokens (1024 rows an expert, H = 2048, 2F = 1536) 628 us, 1.31
 // PFLOP/s; the products and TMA copies alone run at 1.7, the gathering beside them costs
 // 90 us and the 1.6 GB of results another 100.  With few rows the results are all of it:
 // 201 MB in 37 us.
@@ -30,6 +35,12 @@ constexpr int kEpiWarps = 4;
 constexpr int kFirstLoader = 2 + kEpiWarps;
 constexpr int kThreads = (kFirstLoader + kLoadWarps) * 32;
 constexpr int kStep = 64;                       // rows of a step
+// Rows of an accumulator at most.  Error of dW by its norm, normal rows and, in brackets, all
+// terms positive: 2.1e-6 (5.6e-6) for any number of rows, against 1.5e-4 (8.2e-4) for 131072
+// in one accumulator.  With 1024 it is 1.0e-6 (2.2e-6) and dW1 of 16384 tokens takes 670 us
+// instead of 643 (632 in one accumulator each), that of 49152 tokens 1990 instead of 1925 (1784);
+// with 4096 4.4e-6 (1.4e-5).
+constexpr int kSpan = 2048;
 constexpr uint32_t kBlockBytes = kStep * 128;   // 64 columns of a step
 constexpr uint32_t kSide = 2 * kBlockBytes;     // a CTA's 128 columns of one operand
 constexpr uint32_t kStage = 2 * kSide;
@@ -73,6 +84,13 @@ struct Walk {
         return find();
     }
 };
+
+// A tile's rows, n of them, are added up in accumulators of span_of(n) rows each, whole steps
+// and all but the last equal.
+__device__ __forceinline__ int span_of(int n) {
+    const int parts = (n + kSpan - 1) / kSpan;
+    return parts > 1 ? ((n + parts - 1) / parts + kStep - 1) / kStep * kStep : n;
+}
 
 // One operand as a gathering warp sees it.
 struct Side {
@@ -256,35 +274,36 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
             const uint64_t pd0 = desc_mn_sw128(ring, kBlockBytes), qd0 = desc_mn_sw128(ring + kSide, kBlockBytes);
             const uint32_t acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
             Ring at{0, 0};
-            int done = 0;  // tiles with rows
+            int done = 0;  // accumulators
             bool good = true;
             for (bool any = w.find(); good && any; any = w.next()) {
-                if (w.r0 == w.r1) continue;
-                const uint32_t buf = done & 1, turns = (uint32_t)done >> 1;
-                good = pair_wait_all(acc_empty0 + 8 * buf, (turns & 1u) ^ 1u, a.status, abort);
-                if (!good) break;
-                tc_fence_after();
-                const uint32_t d = tmem + buf * 256;
-                uint32_t more = 0;
-                for (int r = w.r0; r < w.r1; r += kStep) {
-                    good = pair_wait_all(full0 + 8 * at.s, at.phase, a.status, abort);
+                const int span = span_of(w.r1 - w.r0);
+                for (int r = w.r0; good && r < w.r1; ++done) {
+                    const uint32_t buf = done & 1, turns = (uint32_t)done >> 1;
+                    good = pair_wait_all(acc_empty0 + 8 * buf, (turns & 1u) ^ 1u, a.status, abort);
                     if (!good) break;
                     tc_fence_after();
-                    const uint32_t off = at.s * (kStage / 16);
-                    if (one) {
+                    const uint32_t d = tmem + buf * 256;
+                    uint32_t more = 0;
+                    for (const int end = r + min(span, w.r1 - r); r < end; r += kStep) {
+                        good = pair_wait_all(full0 + 8 * at.s, at.phase, a.status, abort);
+                        if (!good) break;
+                        tc_fence_after();
+                        const uint32_t off = at.s * (kStage / 16);
+                        if (one) {
 #pragma unroll
-                        for (int kk = 0; kk < kStep / 16; ++kk)
-                            pair_mma(d, desc_at(pd0, off + kk * (2048 / 16)), desc_at(qd0, off + kk * (2048 / 16)), idesc,
-                                     kk > 0 ? 1u : more);
-                        pair_commit(empty0 + 8 * at.s);
+                            for (int kk = 0; kk < kStep / 16; ++kk)
+                                pair_mma(d, desc_at(pd0, off + kk * (2048 / 16)), desc_at(qd0, off + kk * (2048 / 16)),
+                                         idesc, kk > 0 ? 1u : more);
+                            pair_commit(empty0 + 8 * at.s);
+                        }
+                        __syncwarp();
+                        more = 1;
+                        at.next(kStages);
                     }
+                    if (good && one) pair_commit(acc_full0 + 8 * buf);
                     __syncwarp();
-                    more = 1;
-                    at.next(kStages);
                 }
-                if (good && one) pair_commit(acc_full0 + 8 * buf);
-                __syncwarp();
-                ++done;
             }
             if (!good && one) {  // the tensor cores are done with shared memory before the CTA ends
                 pair_commit(smem_u32(&drain));
@@ -298,15 +317,27 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
         unsigned char *places = smem + kStages * kStage + (warp - 2) * blocks * kOut;
         int turn = 0;  // the place of the next block
         const uint32_t empty_addr = map_to_rank(&acc_empty[0], 0);
-        int done = 0;
-        for (bool more = w.find(); more; more = w.next()) {
-            const bool any = w.r1 > w.r0;
+        int done = 0, left = 0, span = 0;  // of the tile: rows not yet accumulated, rows of an accumulator
+        bool first = true, more = w.find();
+        for (; more; first = left <= 0, more = first ? w.next() : true) {
+            if (first) {
+                left = w.r1 - w.r0;
+                span = span_of(left);
+            }
+            const bool any = left > 0;
             if (!any && a.accumulate) continue;
             const int buf = done & 1;
             if (any) {
                 const bool good = pair_wait_warp(smem_u32(&acc_full[buf]), (uint32_t)(done >> 1) & 1u, a.status, abort, lane);
                 if (!good) break;
                 tc_fence_after();
+                left -= span;
+            }
+            // an accumulator is added to what the ones before it left, which has been written then
+            const bool add = a.accumulate || !first;
+            if (!first) {
+                if (lane == 0) bulk_wait_all<0>();
+                __syncwarp();
             }
             const int m0 = w.m * 256 + (int)rank * 128 + 32 * quad;
             const uint32_t col = tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)(buf * 256);
@@ -336,7 +367,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if (a.accumulate) tma_reduce_add_3d(&omap, mine, n0, m0, w.e);
+                    if (add) tma_reduce_add_3d(&omap, mine, n0, m0, w.e);
                     else tma_store_3d(&omap, mine, n0, m0, w.e);
                     bulk_commit_group();
                 }

@@ -408,3 +408,56 @@ def test_weight_gradient_of_a_collapsed_router(ex):  # noqa: F811
     sums = torch.cumsum(steps, 0)
     within(dw[0], sums[-1], 34 * U * (sums.abs() + mags).sum(0))
     assert (dw[1] == 0).all()
+
+
+@pytest.mark.parametrize("n", [16384, 131072])
+@pytest.mark.parametrize("positive", [False, True])
+def test_long_weight_gradients_keep_fp32s_precision(ex, n, positive):  # noqa: F811
+    """However many rows an expert has, an accumulator takes at most 2048 of them: 128 additions of
+    16 rows, each losing at most a unit in the last place (2^-23) of the partial sum.  Those grow as
+    the root of the rows, or with them where all terms are positive, so that an accumulator is off by
+    128 * 2/3 * 2^-23 of its value at most, and the fp32 sum of the n / 2048 of them by another
+    n / 2048 * 2/3 * 2^-24."""
+    p, q = rnd(n, n, 64), rnd(n + 1, n, 48)
+    if positive:
+        p, q = p.abs(), q.abs()
+    gp, gq, go = gpu(p, q, ref.groups([0, n]))
+    want = p.double().T @ q.double()
+    tolerance = 2 / 3 * (128 * 2.0 ** -23 + n / 2048 * 2.0 ** -24)
+    dw = ex.grouped_weight_grad(gp, gq, go)
+    ok(ex)
+    assert float((dw[1].double().cpu() - want).norm() / want.norm()) <= tolerance
+    assert (dw[0] == 0).all()
+    # added to a gradient of the same size: the sum is twice as large, and so may the error be
+    total = ex.grouped_weight_grad(gp, gq, go, out=dw.clone(), accumulate=True)
+    ok(ex)
+    assert float((total[1].double().cpu() - 2 * want).norm() / (2 * want).norm()) <= tolerance
+    for _ in range(3):
+        assert torch.equal(ex.grouped_weight_grad(gp, gq, go), dw)
+        assert torch.equal(ex.grouped_weight_grad(gp, gq, go, out=dw.clone(), accumulate=True), total)
+
+
+@pytest.mark.parametrize("n", [2047, 2048, 2049, 2111, 4096, 4097, 6145])
+@pytest.mark.parametrize("side", ["none", "p", "q"])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_weight_gradients_at_the_accumulators_edges(ex, n, side, accumulate):  # noqa: F811
+    """Groups of one accumulator, of several, and of none in turn, on more tiles than pairs."""
+    counts, M, N, T = [3, n, 0, n + 64, 1, 2 * n], 264, 520, 37
+    off = ref.groups(counts)
+    R = sum(counts)
+    rows = torch.randint(0, T, (R,), generator=torch.Generator().manual_seed(n))
+    p, q = rnd(n, T if side == "p" else R, M), rnd(n + 1, T if side == "q" else R, N)
+    base = torch.randn(6, M, N, generator=torch.Generator().manual_seed(7)) if accumulate else None
+    gp, gq, go, gr, gb = gpu(p, q, off, rows, base)
+    got = ex.grouped_weight_grad(gp, gq, go, gr if side == "p" else None, gr if side == "q" else None, out=gb,
+                                 accumulate=accumulate)
+    ok(ex)
+    pd, qd = (p[rows] if side == "p" else p).double(), (q[rows] if side == "q" else q).double()
+    for e, m in enumerate(counts):
+        i, j = int(off[e]), int(off[e + 1])
+        want, mag = pd[i:j].T @ qd[i:j], pd[i:j].abs().T @ qd[i:j].abs()
+        bound = 2 * m * U * mag
+        if accumulate:
+            want = want + base[e].double()
+            bound = bound + 4 * U * (want.abs() + base[e].abs().double() + bound)
+        within(got[e], want, bound)
