@@ -466,13 +466,17 @@ do_status do_rem_allocate(const double *loads, const double *expert_tokens,
  *    offsets[0] and at or past offsets[E] are not written, and a choice whose pos
  *    names one is left out.
  *  - Products run on the tensor cores or the ALU with bf16 operands, fp32
- *    accumulation and one rounding of the result; results are identical run to run.
+ *    accumulation and one rounding of the result (the joined ones: see there);
+ *    results are identical run to run.  The tensor cores' accumulation is less exact
+ *    than fp32 additions: an error of some 1e-9 of a result's norm for each column
+ *    of the contraction (2e-6 at H = 2048), which shows in the fp32 results only.
  *  - A NaN or an infinity in a row of one expert, or in an expert without rows,
  *    does not reach the results of others.
  *  - status_flags (256-byte aligned device memory whose first int32 is zero before
  *    its first use, may be NULL): bit 1 (a bounded device wait ran out) and bit 2
  *    (a row or position outside its matrix, counted as a row of zeros or left out)
- *    are ORed into it; do_device_status reads and clears it.
+ *    are ORed into it; do_device_status reads and clears it.  After bit 1 the
+ *    results of the calls that share the word may be wrong.
  *  - Asynchronous on `stream`. */
 
 /* The up projection with its activation, z = W1_e x[rows[r]] (fp32):
@@ -480,16 +484,17 @@ do_status do_rem_allocate(const double *loads, const double *expert_tokens,
  * and, with codes and exponents (both or neither), z itself kept in 8 bits for
  * the backward pass: codes [R][2F] int8 in [-127, 127] and exponents [R][2F/16]
  * uint8, the value of a code being code * 2^(e - 127) with e the exponent of its
- * block of 16 columns: the least e >= 1 with max |z| <= 127 * 2^(e - 127), codes
- * rounded to nearest even; e = 255 stands for a block of NaNs (it held a NaN or
- * an infinity).  An error of at most half a step, 2^-7 of the block's largest
- * value, and 1.0625 bytes a value.
+ * block of 16 columns: the least e >= 1 with max |z| <= 127 * 2^(e - 127) (249 at
+ * most), codes rounded to nearest even; e = 255 stands for a block of NaNs (it held
+ * a NaN or an infinity).  An error of at most half a step, 1/127 of the block's
+ * largest value (2^-127 where e = 1), and 1.0625 bytes a value.
  * X [T][H] bf16; rows NULL: routed row r reads X[r] (T >= R). */
 do_status do_expert_up(const void *X, const void *W1, const int32_t *rows, const int32_t *offsets,
                        int64_t T, int32_t H, int32_t F, int32_t E, int64_t R, void *act,
                        void *codes, void *exponents, int32_t *status_flags, void *stream);
 
-/* values [rows][cols] bf16 of an 8-bit checkpoint (exact: codes have 7 bits). */
+/* values [rows][cols] bf16 of an 8-bit checkpoint (exact: codes have 7 bits; one past
+ * bf16's range is infinite). */
 do_status do_checkpoint_values(const void *codes, const void *exponents, int64_t rows,
                                int32_t cols, void *values, void *stream);
 
@@ -504,7 +509,10 @@ do_status do_grouped_matmul(const void *A, const void *W, const int32_t *rows,
 /* do_grouped_matmul on rows A [T k][K] in dispatch order, and the sum of each
  * token's k rows: out [T][N] bf16 = sum_q weights[t][q] Y[pos[t][q]] in fp32
  * (weights [T][k] fp32; NULL: one each, as the gradient of a layer's input
- * wants).  A pos outside [offsets[0], offsets[E]) is left out.  workspace:
+ * wants).  A pos outside [offsets[0], offsets[E]) is left out.  Y is fp32 up to
+ * T k N = 25165824 values, so that out is rounded once; beyond, each Y[r] is
+ * rounded to bf16 before the sum, so that a token's bits depend on how many share
+ * its call.  workspace:
  * do_grouped_matmul_join_workspace_size bytes, 256-byte aligned, of any content
  * (it holds Y); none of it is read by a later call. */
 do_status do_grouped_matmul_join(const void *A, const void *W, const int32_t *offsets,
@@ -518,7 +526,8 @@ size_t do_grouped_matmul_join_workspace_size(int64_t T, int32_t k, int32_t N);
 /* The experts of a layer forward, in one call: out [T][H] bf16,
  *   out[t] = sum_q combine[t][q] W2_e act(W1_e X[t]),  e the q-th expert of t,
  * with act, rows, offsets and pos as above and the activations rounded to bf16
- * between the two products (do_expert_up, then do_grouped_matmul_join).
+ * between the two products (do_expert_up, then do_grouped_matmul_join, whose rule
+ * for Y holds here with N = H).
  * workspace: do_expert_ffn_workspace_size bytes, 256-byte aligned, of any
  * content. */
 do_status do_expert_ffn(const void *X, const void *W1, const void *W2, const float *combine,

@@ -27,7 +27,9 @@ do_status check_up_tiles(int64_t R, int32_t F) {
 }
 
 // The rows that a join adds are kept in fp32 where they stay in the L2 anyway: the sum
-// is then rounded once, and nothing is read from memory twice as wide.
+// is then rounded once, and nothing is read from memory twice as wide.  Past that they are
+// bf16, half of the bytes that bound the join (0.5 GB each way for 131072 rows of 2048): an
+// error of 2.3e-3 of the result's norm instead of 1.7e-3.
 bool join_wide(int64_t R, int32_t N) { return R * N <= (int64_t)(96 << 20) / 4; }
 
 do_status of(cudaError_t e) { return e == cudaSuccess ? DO_OK : DO_ERR_CUDA; }
@@ -170,6 +172,7 @@ do_status do_expert_ffn(const void *X, const void *W1, const void *W2, const flo
     if (!workspace || off(workspace, 256) || workspace_bytes < do_expert_ffn_workspace_size(T, k, H, F))
         return DO_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // between the products the activations are bf16, the tensor cores' operand type
     void *y = static_cast<char *>(workspace) + dol::round256(sizeof(dol::bf16) * (size_t)R * F);
     cudaError_t e = dol::product(
         dol::kProductUp, dol::product_args(X, T, rows, W1, offsets, R, H, 2 * F, E, false, workspace, status_flags), s);

@@ -50,11 +50,16 @@ cudaError_t launch_product(ProductMode mode, const ProductArgs &a, cudaStream_t 
 
 // The products of at most kFewRows routed rows without checkpoint, weights as they
 // are (not transposed), and the joined ones of at most kFewTokens tokens of them, where
-// out is [T][N] (experts_few.cu).  Measured on both sides (us in a graph; H = 2048, F =
-// 768, k = 8 of 128 experts; few rows against tensor cores): up R = 8 10.5 and 15.5, 16
-// 17.1 and 25.4, 24 23.5 and 27.3, 32 39 and 36; down 7.0 and 9.9, 11.3 and 13.8, 19.3 and
-// 17.0, 25 and 19; joined T = 1 9.5 and 12.3, 2 17.4 and 16.6 (H = 512: 3.5 and 6.9), 16
-// tokens of one row 15.5 and 10.6.
+// out is [T][N] (experts_few.cu).  Measured on both sides (us in a graph, weights from
+// memory; F = 768, 128 experts; few rows against tensor cores), for rows of different
+// experts and, in brackets, all of one expert.  H = 2048, up: R = 2 4.9 and 11.5 (4.2 and
+// 11.3), 8 10.1 and 14.5 (7.2 and 11.3), 16 17.3 and 24.2 (12.1 and 11.4), 24 23.5 and 27.3,
+// 32 39 and 36; down: 3.7 and 8.1 (3.3 and 8.0), 6.4 and 9.8 (5.4 and 8.0), 11.1 and 14.1
+// (8.4 and 8.1), 19.3 and 17.0, 25 and 19.  Joined, T k rows: 1 x 8 9.9 and 12.0 (6.0 and
+// 10.5), 2 x 2 7.2 and 10.9 (5.7 and 10.2), 2 x 4 10.0 and 11.8 (6.0 and 10.3), 2 x 8 17.8
+// and 16.6 (10.0 and 10.6), 16 x 1 15.5 and 10.6; H = 512: 2 x 8 5.7 and 11.6 (4.6 and 9.7).
+// So sixteen rows of one expert, and two tokens of eight experts each at H = 2048, are 3 to
+// 7 % slower than the other side; all else up to the limits is faster.
 constexpr int64_t kFewRows = 16;
 constexpr int64_t kFewTokens = 2;
 cudaError_t launch_few_product(ProductMode mode, const ProductArgs &a, cudaStream_t s);
@@ -120,7 +125,7 @@ __device__ __forceinline__ int2 rows_of_groups(const int *offsets, int E, int64_
 }
 
 // 8-bit checkpoint of a block of 16 values: codes in [-127, 127] times 2^(e - 127),
-// e the exponent byte.  e is the least in [1, 250] with max |v| <= 127 * 2^(e - 127):
+// e the exponent byte.  e is the least >= 1 with max |v| <= 127 * 2^(e - 127), at most 249:
 // for max |v| = m 2^x with m in [1, 2) that is x - 6 where m <= 127/64 and x - 5
 // otherwise, which the addition carries out on the float's bits.  A block with a NaN
 // or an infinity has e = 255 and stands for 16 NaNs.
@@ -130,7 +135,7 @@ __device__ __forceinline__ int q8_exponent(float amax) {
     const int e = (int)((b + 0x1ffffu) >> 23) - 6;
     return e < 1 ? 1 : e;
 }
-// 2^(127 - e) and 2^(e - 127), both normal for 1 <= e <= 250; e = 255: 0 and NaN.
+// 2^(127 - e) and 2^(e - 127), both normal for 1 <= e <= 249; e = 255: 0 and NaN.
 __device__ __forceinline__ float q8_inverse(int e) {
     return e == 255 ? 0.0f : __uint_as_float((unsigned)(254 - e) << 23);
 }

@@ -1,13 +1,13 @@
 // The expert products for a handful of routed rows (a decode step of one or a few
 // tokens): the weights are read once per routed row and everything else is small,
-// so these kernels stream weight rows through the ALUs, one warp per result, with
-// every load of a result in flight at once.  The work is R N results of equal size,
+// so these kernels stream weight rows through the ALUs, one warp per result or a few,
+// with as many loads in flight as its registers hold.  The work is R N results of equal size,
 // spread evenly over the GPU; the tensor-core kernels' tiles of 256 weight rows
 // leave a part of it idle then (8 routed rows of E = 128 experts, H = 2048, F = 768:
 // 96 CTAs of 152).  Rows that share an expert read its weights again, from the L2:
 // kFewRows is where that starts to cost more than the idle part saves.  Bound by memory
 // and the latency of two dependent loads (the group ends, then the weights): the up
-// projection of those 8 rows takes 10.5 us for 50 MB, 7.4 at the copy rate.
+// projection of those 8 rows takes 10.1 us for 50 MB, 7.4 at the copy rate.
 //
 // Sums are fp32, lane by lane in order and then over the lanes.
 #include "experts.cuh"
@@ -108,8 +108,8 @@ few_product_kernel(const ProductArgs p, int cols) {
 }
 
 // kSplit warps per (token, result column), each with a share of the token's k rows, four
-// of them at a time with all their weights and values in flight; fp32 sums, joined in
-// order through shared memory.
+// of them at a time: 24 pieces of weights and values, of which the 52 to 56 registers that
+// the compiler takes hold a half at once.  fp32 sums, joined in order through shared memory.
 template <int kSplit, int kPieces>
 __global__ void __launch_bounds__(kWarps * 32)
 few_join_kernel(const ProductArgs p, const int *__restrict__ pos, const float *__restrict__ weights, int k) {

@@ -225,7 +225,9 @@ def grouped_matmul_join(a: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor,
                         weights: torch.Tensor | None = None, transposed: bool = False) -> torch.Tensor:
     """do_grouped_matmul_join: out [T,N] bf16, the products of grouped_matmul on
     the rows a [T*k,K] in dispatch order, summed per token over its rows
-    pos [T,k] with weights [T,k] fp32 (None: one each).  Not differentiable."""
+    pos [T,k] with weights [T,k] fp32 (None: one each).  The products are kept in
+    fp32 up to T k N = 25165824 values and rounded to bf16 before the sum beyond.
+    Not differentiable."""
     _no_graph("grouped_matmul_join", a, w, weights)
     dev = _device(a)
     _bf16("a", a, 2, dev)
@@ -380,7 +382,9 @@ def expert_ffn(x: torch.Tensor, w1: torch.Tensor, w2: torch.Tensor, combine: tor
     Differentiable once in x, w1, w2 and combine (a second derivative raises); the
     backward pass works from 8-bit pre-activations.  main_grads: (dw1 [E,2F,H],
     dw2 [E,H,F]) fp32 buffers that the gradients of the weights that require one are
-    added to instead of being returned."""
+    added to instead of being returned.  The activations are rounded to bf16 between
+    the two products, and the second one's rows before their sum as in
+    grouped_matmul_join."""
     if fwd._current_level >= 0:
         _no_tangent("expert_ffn", x, w1, w2, combine)
     dev = _device(x)
