@@ -1,22 +1,9 @@
 // C ABI of the expert operators (include/doloss.h): argument checks and launches.
-#include <climits>
-
-#include "doloss.h"
+#include "experts_abi.cuh"
 #include "experts_mma.cuh"
 
 namespace dol {
 namespace {
-
-bool off(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
-size_t round256(size_t x) { return (x + 255) / 256 * 256; }
-
-// Sizes that every call shares.  Columns are whole 16-byte pieces (8 bf16 values).
-do_status check(int64_t R, int32_t E, int32_t c0, int32_t c1, int step0, int step1) {
-    if (R < 1 || E < 1 || c0 < 1 || c1 < 1) return DO_ERR_INVALID_ARG;
-    if (E > 1024 || R > INT32_MAX - 256 || c0 % step0 || c1 % step1 || c0 > (1 << 17) || c1 > (1 << 17))
-        return DO_ERR_UNSUPPORTED;
-    return DO_OK;
-}
 
 // Whether the up projection's tiles of one expert (at most 256 rows each; narrower ones only
 // where there are few) are divided exactly by its weight tiles of 128 columns.  Of the
@@ -26,21 +13,9 @@ do_status check_up_tiles(int64_t R, int32_t F) {
     return (uint64_t)((R + 255) / 256) * tiles > divide_limit((uint32_t)tiles) ? DO_ERR_UNSUPPORTED : DO_OK;
 }
 
-// The rows that a join adds are kept in fp32 where they stay in the L2 anyway: the sum
-// is then rounded once, and nothing is read from memory twice as wide.  Past that they are
-// bf16, half of the bytes that bound the join (0.5 GB each way for 131072 rows of 2048): an
-// error of 2.3e-3 of the result's norm instead of 1.7e-3.
-bool join_wide(int64_t R, int32_t N) { return R * N <= (int64_t)(96 << 20) / 4; }
-
-do_status of(cudaError_t e) { return e == cudaSuccess ? DO_OK : DO_ERR_CUDA; }
-
 cudaError_t product(ProductMode mode, const ProductArgs &a, cudaStream_t s) {
     if (a.R <= kFewRows && !a.transposed && !a.codes) return launch_few_product(mode, a, s);
     return launch_product(mode, a, s);
-}
-
-size_t join_bytes(int64_t R, int32_t N) {
-    return round256((join_wide(R, N) ? sizeof(float) : sizeof(bf16)) * (size_t)R * (size_t)N);
 }
 
 // a.out: [T][N]; workspace: join_bytes (not used by the few-row kernel).
@@ -83,7 +58,7 @@ extern "C" {
 do_status do_expert_up(const void *X, const void *W1, const int32_t *rows, const int32_t *offsets, int64_t T,
                        int32_t H, int32_t F, int32_t E, int64_t R, void *act, void *codes, void *exponents,
                        int32_t *status_flags, void *stream) {
-    do_status st = dol::check(R, E, H, F, 8, dol::kQBlock);
+    do_status st = dol::check_sizes(R, E, H, F, 8, dol::kQBlock);
     if (st != DO_OK) return st;
     if (!X || !W1 || !offsets || !act || T < 1 || (!codes) != (!exponents)) return DO_ERR_INVALID_ARG;
     if (!rows && T < R) return DO_ERR_INVALID_ARG;
@@ -112,7 +87,7 @@ do_status do_checkpoint_values(const void *codes, const void *exponents, int64_t
 do_status do_grouped_matmul(const void *A, const void *W, const int32_t *rows, const int32_t *offsets, int64_t T,
                             int32_t K, int32_t N, int32_t E, int64_t R, int32_t transposed, void *Y,
                             int32_t *status_flags, void *stream) {
-    do_status st = dol::check(R, E, K, N, 8, 8);
+    do_status st = dol::check_sizes(R, E, K, N, 8, 8);
     if (st != DO_OK) return st;
     if (!A || !W || !offsets || !Y || T < 1 || (transposed != 0 && transposed != 1)) return DO_ERR_INVALID_ARG;
     if (!rows && T < R) return DO_ERR_INVALID_ARG;
@@ -136,7 +111,7 @@ do_status do_grouped_matmul_join(const void *A, const void *W, const int32_t *of
     if (T < 1 || k < 1) return DO_ERR_INVALID_ARG;
     if (T > INT32_MAX / k) return DO_ERR_UNSUPPORTED;
     const int64_t R = T * k;
-    do_status st = dol::check(R, E, K, N, 8, 8);
+    do_status st = dol::check_sizes(R, E, K, N, 8, 8);
     if (st != DO_OK) return st;
     if (!A || !W || !offsets || !pos || !out || (transposed != 0 && transposed != 1)) return DO_ERR_INVALID_ARG;
     if (off(A, 16) || off(W, 16) || off(out, 16) || off(offsets, 4) || off(pos, 4) || off(weights, 4) ||
@@ -161,7 +136,7 @@ do_status do_expert_ffn(const void *X, const void *W1, const void *W2, const flo
     if (T < 1 || k < 1) return DO_ERR_INVALID_ARG;
     if (T > INT32_MAX / k) return DO_ERR_UNSUPPORTED;
     const int64_t R = T * k;
-    do_status st = dol::check(R, E, H, F, 8, dol::kQBlock);
+    do_status st = dol::check_sizes(R, E, H, F, 8, dol::kQBlock);
     if (st != DO_OK) return st;
     if (!X || !W1 || !W2 || !combine || !rows || !offsets || !pos || !out) return DO_ERR_INVALID_ARG;
     if (off(X, 16) || off(W1, 16) || off(W2, 16) || off(out, 16) || off(combine, 4) || off(rows, 4) ||
@@ -196,7 +171,7 @@ do_status do_expert_up_backward(const void *dout, const void *W2, const void *co
     if (T < 1 || k < 1) return DO_ERR_INVALID_ARG;
     if (T > INT32_MAX / k) return DO_ERR_UNSUPPORTED;
     const int64_t R = T * k;
-    do_status st = dol::check(R, E, H, F, 8, dol::kQBlock);
+    do_status st = dol::check_sizes(R, E, H, F, 8, dol::kQBlock);
     if (st != DO_OK) return st;
     if (!dout || !W2 || !codes || !exponents || !combine || !rows || !offsets || !pos || !dz || !act || !dcombine)
         return DO_ERR_INVALID_ARG;
@@ -222,7 +197,7 @@ do_status do_expert_up_backward(const void *dout, const void *W2, const void *co
 do_status do_grouped_weight_grad(const void *P, const void *Q, const int32_t *p_rows, const int32_t *q_rows,
                                  const int32_t *offsets, int64_t Tp, int64_t Tq, int32_t M, int32_t N, int32_t E,
                                  int64_t R, int32_t accumulate, float *dW, int32_t *status_flags, void *stream) {
-    do_status st = dol::check(R, E, M, N, 8, 8);
+    do_status st = dol::check_sizes(R, E, M, N, 8, 8);
     if (st != DO_OK) return st;
     if (!P || !Q || !offsets || !dW || Tp < 1 || Tq < 1 || (accumulate != 0 && accumulate != 1))
         return DO_ERR_INVALID_ARG;

@@ -43,7 +43,7 @@
 // Every wait is bounded; one that runs out records kDevTimeout.
 #include <cstdint>
 
-#include "experts_mma.cuh"
+#include "experts_tiles.cuh"
 
 namespace dol {
 namespace {
@@ -81,36 +81,6 @@ struct PairArgs {
 // expert its first tile [E + 1], first row [E + 1] and the width of its tiles [E + 1].
 __host__ __device__ inline uint32_t table_bytes(int E) { return 4u * 3u * ((uint32_t)E + 1u); }
 __host__ __device__ inline uint32_t off_turn(int stages, uint32_t b_bytes) { return stages * (kABytes + b_bytes); }
-
-struct Tile {
-    int e, m, r0, n, width;  // expert, weight tile, first routed row, rows, MMA width
-};
-
-// The tiles of a pair in turn: t = pair, pair + pairs, ..., the expert found by going on
-// from the last one's.
-struct Walk {
-    const int *first, *start, *width;  // shared
-    int tiles, pairs, m_tiles;
-    uint32_t m_magic;
-    int t, e;
-    Tile tile;
-
-    __device__ __forceinline__ bool find() {
-        if (t >= tiles) return false;
-        while (first[e + 1] <= t) ++e;
-        const int i = t - first[e], j = divide_by(i, m_magic), w = width[e], a = start[e];
-        tile.e = e;
-        tile.m = i - j * m_tiles;
-        tile.r0 = a + j * w;
-        tile.n = min(w, start[e + 1] - tile.r0);
-        tile.width = (tile.n + 15) & ~15;
-        return true;
-    }
-    __device__ __forceinline__ bool next() {
-        t += pairs;
-        return find();
-    }
-};
 
 // 16 values to their codes and exponent.
 __device__ __forceinline__ uint4 quantise16(const float *v, int *exponent) {
@@ -217,34 +187,6 @@ __device__ __forceinline__ float finish_grad(const ProductArgs &p, int64_t r, in
     return lo + hi;
 }
 
-// Named barriers of a group of four epilogue warps.
-__device__ __forceinline__ void group_sync(int id) {
-    asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory");
-}
-__device__ __forceinline__ int group_and(int id, int ok) {
-    int all;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.s32 q, %1, 0;\n\t"
-        "bar.red.and.pred p, %2, 128, q;\n\t"
-        "selp.s32 %0, 1, 0, p;\n\t}"
-        : "=r"(all)
-        : "r"(ok), "r"(id)
-        : "memory");
-    return all;
-}
-
-// Where 16-byte piece j of row i of warp q's block lies in its 128 bytes.
-__device__ __forceinline__ int turn_slot(int j, int i, int q) { return (j ^ q ^ ((i & 1) << 2)) << 4; }
-
-__device__ __forceinline__ void load4(float *v, const unsigned char *from) {
-    const float4 f = *reinterpret_cast<const float4 *>(from);
-    v[0] = f.x;
-    v[1] = f.y;
-    v[2] = f.z;
-    v[3] = f.w;
-}
-
 template <int kMode, bool kGather, bool kTransposed>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kMode, kGather), 1)
 product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const PairArgs a) {
@@ -281,45 +223,8 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     pdl_wait();
     // not before: the kernel before may share this SM and still have to take its own
     if (warp == 1) pair_tmem_alloc(&tmem_slot, 512);
-    // The first tile of each expert: a scan of ceil(n / cap) m_tiles over the experts.  Tiles
-    // are 256 rows at most, or 128 or 64 while that leaves half of the pairs without one:
-    // a tile's time is mostly its epilogue then, which narrower tiles divide.  T = 1000, H = 512,
-    // F = 256, E = 8, k = 2, against 256 always: the gradient 17.9 to 13.4 us, up 9.7 to 8.4, a
-    // plain product 8.8 to 8.4; T = 1000, H = 2048, F = 768 (48 tiles, not divided) 20.6 either way.
     const int pairs = (int)(gridDim.x >> 1);
-    int carry;
-    for (int cap = kTileN;; cap /= 2) {
-        carry = 0;
-        int wide = 0;  // some group could be divided further
-        for (int base = 0; base <= E; base += kThreads) {
-            const int e = base + (int)threadIdx.x;
-            int c = 0, n = 0;
-            if (e <= E) start[e] = max(0, min(__ldg(p.offsets + e), (int)p.R));
-            if (e < E) {
-                n = max(0, max(0, min(__ldg(p.offsets + e + 1), (int)p.R)) - start[e]);
-                const int nt = (n + cap - 1) / cap;
-                width[e] = nt > 0 ? ((n + nt - 1) / nt + 15) & ~15 : 0;
-                c = nt * a.m_tiles;
-            }
-            int x = c;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(kFull, x, o);
-                if (lane >= o) x += y;
-            }
-            if (lane == 31) s_part[warp] = x;
-            wide |= __syncthreads_or(n > cap / 2);
-            int before = carry, all = 0;
-            for (int i = 0; i < kThreads / 32; ++i) {
-                if (i < warp) before += s_part[i];
-                all += s_part[i];
-            }
-            if (e < E) first[e] = before + x - c;
-            carry += all;
-            __syncthreads();
-        }
-        if (!wide || cap == 64 || 2 * carry > pairs) break;
-    }
+    const int carry = tile_table<kTileN, kThreads>(p.offsets, E, p.R, a.m_tiles, pairs, first, start, width, s_part);
     if (threadIdx.x == 0) first[E] = carry;
     tc_fence_before();
     __syncthreads();
@@ -562,14 +467,6 @@ product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     cluster_sync_all();
     tc_fence_after();
     if (warp == 1) pair_tmem_dealloc(tmem, 512);
-}
-
-int sm_count() {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return 0;
-    return n;
 }
 
 template <int kMode, bool kGather, bool kTransposed>
