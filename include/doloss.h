@@ -570,6 +570,72 @@ do_status do_grouped_weight_grad(const void *P, const void *Q, const int32_t *p_
                                  int32_t accumulate, float *dW, int32_t *status_flags,
                                  void *stream);
 
+/* ------------------------------------------------ experts in 8-bit blocks
+ *
+ * The experts' products with weights and activations in e4m3 and a power of two for each
+ * block of 128, forward only, for a server that keeps its weights in 8 bits.
+ *  - Format.  The value of a code c in a block of exponent byte e is c 2^(e - 127); e =
+ *    255 makes the block NaN.  Rows [M][K] have blocks of 1 x 128, exponents [M][ceil(K /
+ *    128)]; weights [E][N][K] blocks of 128 x 128, exponents [E][ceil(N / 128)][ceil(K /
+ *    128)]; the gate and the up rows of a gated W1 [E][2F][H] are blocked apart, exponents
+ *    [E][2][ceil(F / 128)][ceil(H / 128)].  A last block may be partly filled.
+ *  - Quantisation takes the least e >= 3 with max |v| <= 448 2^(e - 127), codes rounded to
+ *    nearest even: an error of at most 1/16 of a value, or of 2^-10 of the block's scale
+ *    where that is more; every value of a code is then a bf16 number, but for 2^128, which
+ *    what lies past (2 - 1/16) 2^127 is rounded to.  A block with a NaN or an infinity has
+ *    e = 255.  Operands of other makers may have any e.
+ *  - K (H, F where they are a product's inner size) is a multiple of 16, N of 8; codes
+ *    and bf16 matrices are 16-byte aligned, exponents of any alignment.  Other limits,
+ *    offsets, rows, pos and status_flags as for the bf16 experts above.
+ *  - Products run on the tensor cores, which apply the blocks' powers of two themselves, with
+ *    fp32 accumulation (its error: see there) and one rounding of the result; results are
+ *    identical run to run.
+ *  - Asynchronous on `stream`. */
+
+/* Rows X [M][K] bf16 in blocks of 1 x 128: codes [M][K], exponents [M][ceil(K/128)]. */
+do_status do_quantise_rows(const void *X, int64_t M, int32_t K, void *codes, void *exponents,
+                           void *stream);
+
+/* Weights W [E][N][K] bf16 in blocks of 128 x 128 (gated = 1: N = 2F, the F gate rows and
+ * the F up rows blocked apart). */
+do_status do_quantise_weights(const void *W, int32_t E, int32_t N, int32_t K, int32_t gated,
+                              void *codes, void *exponents, void *stream);
+
+/* values [planes][N][K] bf16 of codes with blocks of block_rows (1 or 128) x 128; exact for
+ * what the calls above write (rounded below bf16's smallest number, infinite past its largest
+ * otherwise).  Rows [M][K]: planes = 1, N = M, block_rows = 1; gated weights: planes = 2E,
+ * N = F. */
+do_status do_block_values(const void *codes, const void *exponents, int64_t planes, int64_t N,
+                          int32_t K, int32_t block_rows, void *values, void *stream);
+
+/* Y [R][N] bf16, Y[r] = W_e A[rows[r]] for rows A [T][K] and weights W [E][N][K] in blocks;
+ * rows NULL: routed row r reads A[r] (T >= R).  offsets NULL: one dense map (E = 1) on all R
+ * rows. */
+do_status do_grouped_matmul8(const void *A, const void *A_exponents, const void *W,
+                             const void *W_exponents, const int32_t *rows, const int32_t *offsets,
+                             int64_t T, int32_t K, int32_t N, int32_t E, int64_t R, void *Y,
+                             int32_t *status_flags, void *stream);
+
+/* The up projection with its activation, do_expert_up on operands in blocks, its result in
+ * blocks of 1 x 128 again: act [R][F] codes and act_exponents [R][ceil(F/128)] of
+ * silu(z[f]) z[F + f], z in fp32.  W1 gated. */
+do_status do_expert_up8(const void *X, const void *X_exponents, const void *W1,
+                        const void *W1_exponents, const int32_t *rows, const int32_t *offsets,
+                        int64_t T, int32_t H, int32_t F, int32_t E, int64_t R, void *act,
+                        void *act_exponents, int32_t *status_flags, void *stream);
+
+/* do_expert_ffn with weights in blocks (W1 gated): X [T][H] bf16 is quantised, do_expert_up8
+ * and do_grouped_matmul8 follow, and each token's k rows are summed with its combine weights,
+ * by the rule of do_grouped_matmul_join for Y.
+ * workspace: do_expert_ffn8_workspace_size bytes, 256-byte aligned, of any content. */
+do_status do_expert_ffn8(const void *X, const void *W1, const void *W1_exponents, const void *W2,
+                         const void *W2_exponents, const float *combine, const int32_t *rows,
+                         const int32_t *offsets, const int32_t *pos, int64_t T, int32_t k,
+                         int32_t H, int32_t F, int32_t E, void *out, int32_t *status_flags,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+size_t do_expert_ffn8_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F);
+
 /* A static description of a status code. */
 const char *do_status_string(int32_t status);
 

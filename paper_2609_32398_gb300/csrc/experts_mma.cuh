@@ -274,4 +274,10 @@ bool encode_gate_up_map(CUtensorMap *map, const void *base, uint64_t E, uint64_t
 // copy costs its thread 60 ns, whatever it carries).
 bool encode_mn_pair_map(CUtensorMap *map, const void *base, uint64_t planes, uint64_t rows, uint64_t cols);
 
+// The same for bytes (cols a multiple of 16): 128 columns where the bf16 maps have 64.
+bool encode_tensor_map_3d_u8(CUtensorMap *map, const void *base, uint64_t planes, uint64_t rows, uint64_t cols,
+                             uint32_t box_cols, uint32_t box_rows);
+bool encode_gather_map_u8(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols);
+bool encode_gate_up_map_u8(CUtensorMap *map, const void *base, uint64_t E, uint64_t F, uint64_t H);
+
 }  // namespace dol

@@ -76,6 +76,14 @@ EXPORTS = {
                                "p", "p", "p", "sz", "p"], "i32"),
     "do_grouped_weight_grad": (["p", "p", "p", "p", "p", "i64", "i64", "i32", "i32", "i32", "i64", "i32", "p", "p",
                                 "p"], "i32"),
+    "do_quantise_rows": (["p", "i64", "i32", "p", "p", "p"], "i32"),
+    "do_quantise_weights": (["p", "i32", "i32", "i32", "i32", "p", "p", "p"], "i32"),
+    "do_block_values": (["p", "p", "i64", "i64", "i32", "i32", "p", "p"], "i32"),
+    "do_grouped_matmul8": (["p", "p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i64", "p", "p", "p"], "i32"),
+    "do_expert_up8": (["p", "p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i64", "p", "p", "p", "p"], "i32"),
+    "do_expert_ffn8_workspace_size": (["i64", "i32", "i32", "i32"], "sz"),
+    "do_expert_ffn8": (["p", "p", "p", "p", "p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i32", "p", "p", "p",
+                        "sz", "p"], "i32"),
 }
 
 _CT = {"p": ctypes.c_void_p, "i64": ctypes.c_int64, "i32": ctypes.c_int32,
