@@ -636,6 +636,34 @@ do_status do_expert_ffn8(const void *X, const void *W1, const void *W1_exponents
 
 size_t do_expert_ffn8_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F);
 
+/* ---------------------------------------------- the layer for a few tokens */
+
+/* A whole MoE layer forward for the few tokens of a decode step, in two kernels:
+ *   z[t] = Wr X[t],  expert_ids[t] = the k largest of z[t], largest first, equal ones in
+ *   favour of the lower expert, combine[t] = their weights by `gate` (as do_routing's), and
+ *   out[t] = sum_q combine[t][q] W2_e (silu(W1g_e X[t]) * W1u_e X[t]),  e = expert_ids[t][q]
+ * X [T][H], the router's Wr [E][H] and out [T][H] bf16; W1 [E][2F][H] (gate rows first) and
+ * W2 [E][H][F] bf16, or codes in blocks with W1_exponents (gated) and W2_exponents (both or
+ * neither).  expert_ids and combine [T][k] are written.
+ *  - T <= 64, k <= 32, E <= 1024; H and F at most 4096 with bf16 weights and 8192 with codes;
+ *    H a multiple of 8 (codes: 16), F of 16.  16-byte aligned matrices.
+ *  - The logits are bf16 products summed to more than fp32 (some 2^-40 of the largest), so that
+ *    the choice does not hang on an order of addition.  They must be finite.
+ *  - The experts' products are summed in fp32 and their activations rounded to bf16 between
+ *    the two; a token's rows are summed in fp32, in the order of its choices, and rounded
+ *    once.  8-bit weights stand for their exact values; the activations stay bf16.
+ *  - Results are identical run to run.  A NaN or an infinity in a token stays in that
+ *    token's results.
+ * workspace: do_moe_layer_workspace_size bytes, 256-byte aligned, of any content; calls that
+ * may run at the same time need one each.  Asynchronous on `stream`. */
+do_status do_moe_layer(const void *X, const void *Wr, const void *W1, const void *W1_exponents,
+                       const void *W2, const void *W2_exponents, int64_t T, int32_t H, int32_t F,
+                       int32_t E, int32_t k, int32_t gate, void *out, int32_t *expert_ids,
+                       float *combine, int32_t *status_flags, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+size_t do_moe_layer_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F);
+
 /* A static description of a status code. */
 const char *do_status_string(int32_t status);
 

@@ -84,6 +84,9 @@ EXPORTS = {
     "do_expert_ffn8_workspace_size": (["i64", "i32", "i32", "i32"], "sz"),
     "do_expert_ffn8": (["p", "p", "p", "p", "p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i32", "p", "p", "p",
                         "sz", "p"], "i32"),
+    "do_moe_layer_workspace_size": (["i64", "i32", "i32", "i32"], "sz"),
+    "do_moe_layer": (["p", "p", "p", "p", "p", "p", "i64", "i32", "i32", "i32", "i32", "i32", "p", "p", "p", "p", "p",
+                      "sz", "p"], "i32"),
 }
 
 _CT = {"p": ctypes.c_void_p, "i64": ctypes.c_int64, "i32": ctypes.c_int32,
