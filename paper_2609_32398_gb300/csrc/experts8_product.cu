@@ -412,7 +412,8 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
                 // the other CTA's largest value of each row of the block has come
                 const int blk = held.n >> 5;
                 uint32_t &phase = waits[buf];
-                pair_wait_warp(smem_u32(&top_here[buf][blk][quad]), phase >> blk & 1u, p.status, abort, lane);
+                // (every lane waits for itself: what one lane has acquired, the others may read too early)
+                pair_wait_all(smem_u32(&top_here[buf][blk][quad]), phase >> blk & 1u, p.status, abort);
                 phase ^= 1u << blk;
                 const unsigned top = max(held.top, *reinterpret_cast<volatile unsigned *>(&top_of[buf][held.n]));
                 const int e = e8_exponent(top);

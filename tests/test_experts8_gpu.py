@@ -363,3 +363,36 @@ def test_empty_calls(ex, e8):
     empty = torch.empty(0, 2, device="cuda")
     assert e8.expert_ffn(x, w, w2, empty, off, none, none).shape == (0, 64)
     ok(ex)
+
+
+@pytest.mark.parametrize("gather", [False, True])
+def test_many_tiles_a_pair(ex, e8, gather):
+    """Tiles in long succession on each pair of CTAs, whose halves of a block's largest value cross
+    on the way: the same bits from thirty calls, and those of 64 bits."""
+    E, H, F, R = 16, 256, 768, 32000
+    counts = [2000 + 61 * (e % 5) - 122 for e in range(E)]
+    R = sum(counts)
+    T = 4001 if gather else R
+    off = ref.groups(counts)
+    rows = torch.randint(0, T, (R,), generator=torch.Generator().manual_seed(1)) if gather else None
+    x, w = rnd(1, T, H).cuda(), rnd(2, E, 2 * F, H, scale=H ** -0.5).cuda()
+    a, q = e8.quantise_rows(x), e8.quantise_weights(w, True)
+    go, gr = gpu(off, rows)
+    got = e8.expert_up(a, q, go, gr)
+    for _ in range(30):
+        again = e8.expert_up(a, q, go, gr)
+        assert torch.equal(again.exponents, got.exponents)
+        assert torch.equal(again.codes.view(torch.uint8), got.codes.view(torch.uint8))
+    ok(ex)
+    av, wv, v = a.values().double(), q.values().double(), got.values().double()
+    for e in range(E):
+        i, j = int(off[e]), int(off[e + 1])
+        ar = av[gr[i:j].long()] if gather else av[i:j]
+        z, m = ar @ wv[e].T, ar.abs() @ wv[e].abs().T
+        act, d = ref.swiglu(z), 2 * H * U * m
+        dg, du, gate, up = d[:, :F], d[:, F:], z[:, :F].abs(), z[:, F:].abs()
+        err = 1.1 * dg * up + gate * du + 2 * dg * du + FN * act.abs()
+        top = (act.abs() + err).reshape(j - i, -1, 128).amax(-1)
+        least = (top / 224 * 2.0 ** -10).repeat_interleave(128, 1)
+        off_by = (v[i:j] - act).abs() - err - torch.maximum(E4 * (act.abs() + err), least)
+        assert bool((off_by <= 0).all()), (e, float(off_by.max()))
