@@ -11,7 +11,7 @@ struct LayerRoom {
 };
 LayerRoom layer_room(int64_t R, int32_t H, int32_t F) {
     LayerRoom r = {};
-    r.act = r.counters + 1024;  // 2 + one for each block of columns, at most one an SM
+    r.act = r.counters + 256;
     r.y = r.act + round256(sizeof(bf16) * (size_t)R * F);
     r.all = r.y + round256(sizeof(float) * (size_t)R * H);
     return r;
@@ -71,10 +71,13 @@ do_status do_moe_layer(const void *X, const void *Wr, const void *W1, const void
     a.act = reinterpret_cast<dol::bf16 *>(ws + room.act);
     a.y = reinterpret_cast<float *>(ws + room.y);
     a.status = status_flags;
-    dol::layer_split(&a, sms);
+    a.ranges = sms;
+    a.blocks = H < sms ? H : sms;
+    const bool few = dol::layer_few(a, eight);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = dol::launch_layer_route(a, s);
-    return dol::of(e != cudaSuccess ? e : dol::launch_layer_experts(a, eight, sms, s));
+    if (e != cudaSuccess) return dol::of(e);
+    return dol::of(few ? dol::launch_layer_few(a, eight, sms, s) : dol::launch_layer_experts(a, eight, sms, s));
 }
 
 }  // extern "C"

@@ -23,16 +23,20 @@ struct LayerArgs {
     float *combine;        // [T][k]
     bf16 *act;             // [T k][F]
     float *y;              // [T k][H]
-    unsigned *counters;    // tickets, up ranges done, arrivals at each block of out's columns
+    unsigned *counters;    // kLayerCounters: tickets, ranges of W1 done, ranges of W2 done
     int *status;
-    int ranges;            // of the up projection
-    int blocks, subsets;   // of out's columns, and of the experts for each of them
+    int ranges;            // that the rows of all used weights are divided into
+    int blocks;            // of out's columns (few routed rows)
     int stage_bytes;       // shared memory for the products' rows
 };
 
-size_t layer_counters(const LayerArgs &a);
-// The split of both projections' work, for `sms` SMs.
-void layer_split(LayerArgs *a, int sms);
+constexpr int kLayerFewRows = 64;
+
+constexpr int kLayerCounters = 3;
+
+// Whether the kernel for few routed rows takes it.
+bool layer_few(const LayerArgs &a, bool eight);
+cudaError_t launch_layer_few(const LayerArgs &a, bool eight, int sms, cudaStream_t s);
 cudaError_t launch_layer_route(const LayerArgs &a, cudaStream_t s);
 cudaError_t launch_layer_experts(LayerArgs a, bool eight, int sms, cudaStream_t s);
 

@@ -9,8 +9,8 @@
 // values are exact in fp32, and their sums are kept as a pair of floats, the running sum
 // and the sum of its rounding errors: with s' = fl(a b + s), the error is a b - (s' - s),
 // exact but for the few steps on which the sum is smaller than the product.  That costs four
-// instructions a product instead of one, two with packed fp32 pairs.  What is compared is the
-// 64-bit value of the pair, equal ones in favour of the lower expert.
+// instructions a product instead of one, two with packed fp32 pairs.  The pairs are
+// what is compared, equal ones in favour of the lower expert.
 //
 // Bound by latency: a token's 0.5 MB of Wr (E = 128, H = 2048) come from the L2 in a
 // microsecond; see layer_experts.cu for the whole call.
@@ -21,7 +21,7 @@
 namespace dol {
 namespace {
 
-constexpr int kCluster = 8, kThreads = 256, kWarps = kThreads / 32;
+constexpr int kCluster = 8;
 typedef unsigned long long u64;
 
 // (s, c) += (s2, c2): s exact with its error in c
@@ -31,99 +31,128 @@ __device__ __forceinline__ void add_pair(float &s, float &c, float s2, float c2)
     s = t;
 }
 
-// Larger for a larger value, never 0; both zeros are one value.
-__device__ __forceinline__ u64 order_key(double z) {
-    const u64 b = (u64)__double_as_longlong(z + 0.0);
-    return (b >> 63) ? ~b : b | (1ull << 63);
+// Larger for a larger value, never 0: the value rounded to fp32, then what that leaves (both zeros
+// are one value; fp64 would order the same and takes 60 cycles an instruction).
+__device__ __forceinline__ unsigned order_of(float v) {
+    const unsigned b = __float_as_uint(v + 0.0f);
+    return (b >> 31) ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ double key_value(u64 key) {
-    return __longlong_as_double((long long)((key >> 63) ? key ^ (1ull << 63) : ~key));
+__device__ __forceinline__ float value_of(unsigned o) { return __uint_as_float((o >> 31) ? o ^ 0x80000000u : ~o); }
+__device__ __forceinline__ u64 order_key(float s, float c) {
+    const float z = s + c, d = z - s, rest = (s - (z - d)) + (c - d);
+    return (u64)order_of(z) << 32 | order_of(rest);
 }
 
 __device__ __forceinline__ void store_remote(uint32_t addr, u64 v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
 
-// The k largest keys of one token by one warp, and its weights.  keys are in this CTA's shared
-// memory; a lane owns experts lane, lane + 32, ...
-__device__ __forceinline__ void select(u64 *keys, const LayerArgs &p, int t, int lane) {
-    u64 best = 0, mine = 0;
-    int best_e = 0x7fffffff, id = 0;
-    auto scan = [&]() {
-        best = 0;
-        best_e = 0x7fffffff;
-        for (int e = lane; e < p.E; e += 32) {
-            const u64 v = keys[e];
-            if (v > best) {
-                best = v;
-                best_e = e;
+// The k largest keys of one token, by the whole CTA: chosen[q] and top[q]; keys are in its shared
+// memory.  Up to 256 experts each key counts the ones before it, a few threads a key (k rounds of
+// a maximum over a warp took 2.4 us for k = 8); with more a warp takes the rounds.
+template <int kThreads>
+__device__ __forceinline__ void select(u64 *keys, int E, int k, int *chosen, u64 *top) {
+    const int lane = threadIdx.x & 31;
+    if (E <= 256) {
+        // threads a key: as many as there are
+        const int shift = (E <= 32 ? 3 : E <= 64 ? 2 : E <= 128 ? 1 : 0) + (kThreads > 256 ? 1 : 0), share = 1 << shift;
+        for (int base = 0; base < E << shift; base += kThreads) {
+            const int i = base + (int)threadIdx.x, e = i >> shift, from = i & (share - 1);
+            const u64 mine = e < E ? keys[e] : 0;
+            int before = 0;
+#pragma unroll 8
+            for (int j = from; j < E; j += share) {
+                const u64 other = keys[j];
+                before += other > mine || (other == mine && j < e);
+            }
+            for (int o = 1; o < share; o *= 2) before += __shfl_xor_sync(kFull, before, o);
+            if (e < E && (i & (share - 1)) == 0 && before < k) {
+                chosen[before] = e;
+                top[before] = mine;
             }
         }
-    };
-    scan();
-    for (int q = 0; q < p.k; ++q) {
-        const unsigned hi = (unsigned)(best >> 32), top = __reduce_max_sync(kFull, hi);
-        const unsigned lo = hi == top ? (unsigned)best : 0u, low = __reduce_max_sync(kFull, lo);
-        const unsigned e = __reduce_min_sync(kFull, hi == top && lo == low ? (unsigned)best_e : 0x7fffffffu);
-        if (lane == q) {
-            mine = (u64)top << 32 | low;
-            id = (int)e;
-        }
-        if ((unsigned)best_e == e && e < 0x7fffffffu) {
-            keys[e] = 0;
-            scan();
+    } else if (threadIdx.x < 32) {  // a lane owns experts lane, lane + 32, ...
+        u64 best = 0;
+        int best_e = 0x7fffffff;
+        auto scan = [&]() {
+            best = 0;
+            best_e = 0x7fffffff;
+            for (int e = lane; e < E; e += 32) {
+                const u64 v = keys[e];
+                if (v > best) {
+                    best = v;
+                    best_e = e;
+                }
+            }
+        };
+        scan();
+        for (int q = 0; q < k; ++q) {
+            const unsigned hi = (unsigned)(best >> 32), high = __reduce_max_sync(kFull, hi);
+            const unsigned lo = hi == high ? (unsigned)best : 0u, low = __reduce_max_sync(kFull, lo);
+            const unsigned e = __reduce_min_sync(kFull, hi == high && lo == low ? (unsigned)best_e : 0x7fffffffu);
+            if ((unsigned)best_e == e) {
+                chosen[q] = (int)e;
+                top[q] = best;
+                keys[e] = 0;
+                scan();
+            }
         }
     }
-    // weights of the chosen, the sigmoids over a common factor where they could all underflow
+    __syncthreads();
+}
+
+// A token's choice and its weights, by one warp; the sigmoids over a common factor where they
+// could all underflow.
+__device__ __forceinline__ void write_choice(const int *chosen, const u64 *top, const LayerArgs &p, int t, int lane) {
     const bool in = lane < p.k;
-    const double z = in ? key_value(mine) : 0.0, first = __shfl_sync(kFull, z, 0);
-    const float zf = (float)z, d = (float)(z - first);
+    const float zf = in ? value_of((unsigned)(top[lane] >> 32)) : 0.0f, rest = in ? value_of((unsigned)top[lane]) : 0.0f;
+    const float first = __shfl_sync(kFull, zf, 0), d = (zf - first) + (rest - __shfl_sync(kFull, rest, 0));
     float w;
     if (p.gate == DO_GATE_SOFTMAX) w = expf(d);
-    else if (first >= 0.0) w = 1.0f / (1.0f + expf(-zf));
+    else if (first >= 0.0f) w = 1.0f / (1.0f + expf(-zf));
     else w = expf(d) / (1.0f + expf(zf));
     const float sum = warp_sum(in ? w : 0.0f);
     if (in) {
         const int at = t * p.k + lane;
-        p.ids[at] = id;
+        p.ids[at] = chosen[lane];
         p.combine[at] = w / sum;
     }
 }
 
-template <int kTokens>
+// A warp takes kExperts of the CTA's experts for kTokens tokens at a time.
+template <int kTokens, int kExperts, int kThreads>
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
-layer_route_kernel(const LayerArgs p, int n_counters) {
+layer_route_kernel(const LayerArgs p) {
+    constexpr int kWarps = kThreads / 32;
     __shared__ u64 keys[kLayerExperts];
-    pdl_trigger();  // the experts' CTAs come up meanwhile; they wait for this kernel's end
     pdl_wait();
+    pdl_trigger();  // the experts' CTAs come up meanwhile, read the tokens and wait for this kernel's end
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank(), t0 = (int)(blockIdx.x / kCluster) * kTokens;
-    if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i < n_counters; i += kThreads) p.counters[i] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < kLayerCounters) p.counters[threadIdx.x] = 0;
     const int per = (p.E + kCluster - 1) / kCluster, e1 = min(p.E, (rank + 1) * per), pieces = p.H / 8;
     const uint4 *x = reinterpret_cast<const uint4 *>(p.x), *wr = reinterpret_cast<const uint4 *>(p.router);
     const uint32_t keys_at = smem_u32(keys);
     const f32x2 minus = pair2(-1.0f, -1.0f);
     cluster_sync_all();  // every CTA of the cluster has begun: its shared memory may be written
-    for (int e = rank * per + 2 * warp; e < e1; e += 2 * kWarps) {
-        const int both = e + 1 < e1 ? 1 : 0;
-        f32x2 s[2][kTokens], c[2][kTokens];
+    for (int e = rank * per + kExperts * warp; e < e1; e += kExperts * kWarps) {
+        f32x2 s[kExperts][kTokens], c[kExperts][kTokens];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kExperts; ++i)
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) s[i][t] = c[i][t] = pair2(0.0f, 0.0f);
-#pragma unroll(kTokens == 1 ? 4 : 2)
+#pragma unroll(kTokens == 1 ? 8 : 2)
         for (int at = lane; at < pieces; at += 32) {
-            uint4 wv[2], xv[kTokens];
-            wv[0] = __ldg(wr + (int64_t)e * pieces + at);
-            wv[1] = __ldg(wr + (int64_t)(e + both) * pieces + at);
+            uint4 wv[kExperts], xv[kTokens];
+#pragma unroll
+            for (int i = 0; i < kExperts; ++i) wv[i] = __ldg(wr + (int64_t)min(e + i, e1 - 1) * pieces + at);
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) xv[t] = __ldg(x + (int64_t)min(t0 + t, p.T - 1) * pieces + at);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                f32x2 w2[2];
+                f32x2 w2[kExperts];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < kExperts; ++i) {
                     const unsigned w = j == 0 ? wv[i].x : j == 1 ? wv[i].y : j == 2 ? wv[i].z : wv[i].w;
                     w2[i] = pair2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
                 }
@@ -132,7 +161,7 @@ layer_route_kernel(const LayerArgs p, int n_counters) {
                     const unsigned w = j == 0 ? xv[t].x : j == 1 ? xv[t].y : j == 2 ? xv[t].z : xv[t].w;
                     const f32x2 v = pair2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
+                    for (int i = 0; i < kExperts; ++i) {
                         const f32x2 sum = fma2(w2[i], v, s[i][t]);
                         c[i][t] = add2(c[i][t], fma2(w2[i], v, fma2(sum, minus, s[i][t])));
                         s[i][t] = sum;
@@ -142,10 +171,10 @@ layer_route_kernel(const LayerArgs p, int n_counters) {
         }
         // over the two halves and the lanes: while there are several values, half of the lanes
         // go on with half of them
-        constexpr int kValues = 2 * kTokens;
+        constexpr int kValues = kExperts * kTokens;
         float vs[kValues], vc[kValues];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kExperts; ++i)
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) {
                 float s_hi, c_hi, &lo = vs[i * kTokens + t], &err = vc[i * kTokens + t];
@@ -176,19 +205,23 @@ layer_route_kernel(const LayerArgs p, int n_counters) {
         if ((lane & whole) == 0 && expert < e1) {
             uint32_t to;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(keys_at + 8u * (uint32_t)expert), "r"(token));
-            store_remote(to, order_key((double)vs[0] + (double)vc[0]));
+            store_remote(to, order_key(vs[0], vc[0]));
         }
     }
     cluster_sync_all();
-    if (warp == 0 && rank < kTokens && t0 + rank < p.T) select(keys, p, t0 + rank, lane);
+    if (rank < kTokens && t0 + rank < p.T) {
+        __shared__ int chosen[kLayerChoices];
+        __shared__ u64 top[kLayerChoices];
+        select<kThreads>(keys, p.E, p.k, chosen, top);
+        if (warp == 0) write_choice(chosen, top, p, t0 + rank, lane);
+    }
 }
 
 }  // namespace
 
 cudaError_t launch_layer_route(const LayerArgs &a, cudaStream_t s) {
-    const int n = (int)layer_counters(a);
-    if (a.T <= 8) return launch_after(layer_route_kernel<1>, dim3((unsigned)(kCluster * a.T)), kThreads, 0, s, a, n);
-    return launch_after(layer_route_kernel<4>, dim3((unsigned)(kCluster * ((a.T + 3) / 4))), kThreads, 0, s, a, n);
+    if (a.T <= 8) return launch_after(layer_route_kernel<1, 1, 512>, dim3((unsigned)(kCluster * a.T)), 512, 0, s, a);
+    return launch_after(layer_route_kernel<4, 2, 256>, dim3((unsigned)(kCluster * ((a.T + 3) / 4))), 256, 0, s, a);
 }
 
 }  // namespace dol
