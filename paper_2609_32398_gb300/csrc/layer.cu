@@ -11,7 +11,7 @@ struct LayerRoom {
 };
 LayerRoom layer_room(int64_t R, int32_t H, int32_t F) {
     LayerRoom r = {};
-    r.act = r.counters + 256;
+    r.act = r.counters + round256(sizeof(unsigned) * kLayerCounters);
     r.y = r.act + round256(sizeof(bf16) * (size_t)R * F);
     r.all = r.y + round256(sizeof(float) * (size_t)R * H);
     return r;
@@ -48,7 +48,7 @@ do_status do_moe_layer(const void *X, const void *Wr, const void *W1, const void
     if (!workspace || off(workspace, 256) || workspace_bytes < do_moe_layer_workspace_size(T, k, H, F))
         return DO_ERR_WORKSPACE;
     const int sms = dol::sm_count();
-    if (sms < 8 || sms > 200) return DO_ERR_CUDA;
+    if (sms < 8 || sms > dol::kLayerRanges) return DO_ERR_CUDA;
     const dol::LayerRoom room = dol::layer_room(T * k, H, F);
     char *ws = static_cast<char *>(workspace);
     dol::LayerArgs a = {};

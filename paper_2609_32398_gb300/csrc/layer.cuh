@@ -23,7 +23,7 @@ struct LayerArgs {
     float *combine;        // [T][k]
     bf16 *act;             // [T k][F]
     float *y;              // [T k][H]
-    unsigned *counters;    // kLayerCounters: tickets, ranges of W1 done, ranges of W2 done
+    unsigned *counters;    // kLayerCounters: tickets, ranges done, and one for each range
     int *status;
     int ranges;            // that the rows of all used weights are divided into
     int blocks;            // of out's columns (few routed rows)
@@ -32,7 +32,8 @@ struct LayerArgs {
 
 constexpr int kLayerFewRows = 64;
 
-constexpr int kLayerCounters = 3;
+constexpr int kLayerRanges = 200;   // at most
+constexpr int kLayerCounters = 2 + kLayerRanges;
 
 // Whether the kernel for few routed rows takes it.
 bool layer_few(const LayerArgs &a, bool eight);

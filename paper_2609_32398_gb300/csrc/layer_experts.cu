@@ -27,10 +27,11 @@
 // 2^-40 of that is lost, far below the sums' fp32).  Each block's sum is scaled by both powers
 // in fp32.
 //
-// Order.  CTAs take tickets: first the ranges of W1, then those of W2, then those of out.  One
-// of W2 waits until all of W1 are done, and those were all taken before, by CTAs that run, and
-// so on: none waits for one that may not have been started, whatever else the GPU runs.  All sums
-// have a fixed order; the waits are bounded.
+// Order.  CTAs take tickets for the ranges of W1 until there are none left, and then go on with
+// the same ranges of W2 and of out.  A range of W2 waits for those of W1 that have its experts'
+// activations, its neighbours, and out for all.  All of W1 were taken before anybody waits, by
+// CTAs that run: none waits for one that may not have been started, whatever else the GPU runs.
+// All sums have a fixed order; the waits are bounded.
 #include <cuda_fp16.h>
 
 #include "layer_device.cuh"
@@ -60,7 +61,8 @@ struct Lists {
     int start[kLayerExperts + 1];  // of each used expert
     unsigned short expert[kLayerExperts], row[kRoutes];
     int part[kWarps];
-    int ticket, good;
+    int ticket, queue, mine;
+    unsigned short range[kLayerRanges];  // that this CTA took
 };
 
 __device__ __forceinline__ void load_matrices(uint32_t (&v)[4], uint32_t addr) {
@@ -86,10 +88,11 @@ __device__ __forceinline__ void mma16(float (&d)[4], unsigned a0, unsigned a1, u
 struct Batch {
     int from, to, r0, r1;
 };
-// Where a warp's copies are: a tile, its place in the list and a step of its k.
+// Where a warp's copies are: a tile (of a batch whose first one has number `before` in the CTA's queue)
+// and a step of its k.
 struct Place {
     Batch in;
-    int slot, pos, row, n, r, end, step;
+    int before, slot, row, n, r, end, step;
     bool valid;
 };
 
@@ -98,8 +101,9 @@ struct StepRing {
     uint32_t data, out, in;
 };
 
-// One projection on this CTA's share, the rows [lo, hi) of the list of all used experts' rows of
-// W2 (up: pairs of gate and up rows).
+// One projection on this CTA's share, a range of the tiles of all used experts' rows of W2 (up: of
+// pairs of gate and up rows).  The warps take its tiles in turn, from a queue: a fixed share each
+// left some of them a tile, a fifth of the time, behind the others.
 template <bool kUp, bool k8>
 struct Phase {
     static constexpr int kTile = kUp ? 8 : 16;  // rows of a tile
@@ -107,8 +111,8 @@ struct Phase {
     Lists &s;
     unsigned char *stage;
     StepRing &ring;
-    int lo, hi, s0, s1;  // the warp's rows; the CTA's slots
-    int warp, lane, K, N, row_bytes, pieces, steps, stride, room;
+    int lo, hi, s0, s1;  // tiles, and their slots
+    int warp, lane, K, N, per, row_bytes, pieces, steps, stride, room;
     Place ahead;         // of the copies
     unsigned begun;      // tiles that they have begun
     const unsigned char *source;  // of the lane's copies at `ahead`
@@ -120,25 +124,21 @@ struct Phase {
         lane = threadIdx.x & 31;
         K = kUp ? p.H : p.F;
         N = kUp ? p.F : p.H;
+        per = (N + kTile - 1) / kTile;
         row_bytes = K * (k8 ? 1 : 2);
         pieces = (row_bytes + 127) / 128;
         steps = (pieces + kPieces - 1) / kPieces;
         stride = pieces * (k8 ? 256 : 128) + 16;
         room = p.stage_bytes / (stride + (k8 ? 8 * pieces : 0));
         if (room >= 8) room &= ~7;
-        const int all = slots * N;
+        const int all = slots * per;
         lo = (int)((int64_t)all * range / p.ranges);
-        const int end = (int)((int64_t)all * (range + 1) / p.ranges), len = end - lo;
-        s0 = lo / N;
-        s1 = len > 0 ? (end - 1) / N + 1 : s0;
-        hi = lo + len * (warp + 1) / kWarps;
-        lo += len * warp / kWarps;
-        Place w = {};
-        w.in = first_batch();
-        w.slot = w.in.from;
-        w.pos = lo;
-        settle(w);
-        ahead = w;
+        hi = (int)((int64_t)all * (range + 1) / p.ranges);
+        s0 = lo / per;
+        s1 = lo < hi ? (hi - 1) / per + 1 : s0;
+        ahead = Place{};
+        ahead.in = first_batch();
+        take_tile(ahead);
         begun = 0;
         begin_tile();
         if (k8 && ahead.valid) scales = exponents(ahead.slot, ahead.row);
@@ -168,22 +168,28 @@ struct Phase {
         return from >= s1 ? Batch{s1, s1, b.r1, b.r1} : batch(from, b.r1);
     }
 
-    // The tile at place w.pos, and its tokens; goes on to the next batches when it lies behind this one.
-    __device__ __forceinline__ void settle(Place &w) const {
+    // The next tile of the queue.  It counts the tiles of one batch after the other.
+    __device__ __forceinline__ void take_tile(Place &w) const {
+        int i = 0;
+        if (lane == 0) i = atomicAdd(&s.queue, 1);
+        i = __shfl_sync(kFull, i, 0);
         for (;;) {
             if (w.in.r0 >= w.in.r1) {
                 w.valid = false;
                 return;
             }
-            w.pos = max(w.pos, w.in.from * N);
-            while (w.pos >= (w.slot + 1) * N) ++w.slot;
-            w.row = w.pos - w.slot * N;
-            w.n = min(min(hi - w.pos, N - w.row), kTile);
-            if (k8) w.n = min(w.n, kBlock8 - w.row % kBlock8);  // one block of exponents
-            if (w.slot < w.in.to && w.pos < hi) break;
+            const int first = max(lo, w.in.from * per), n = min(hi, w.in.to * per) - first;
+            if (i - w.before < n) {
+                const int tile = first + i - w.before;
+                w.slot = max(w.slot, w.in.from);
+                while (tile >= (w.slot + 1) * per) ++w.slot;
+                w.row = (tile - w.slot * per) * kTile;
+                w.n = min(N - w.row, kTile);
+                break;
+            }
+            w.before += n;
             w.in = after(w.in);
             w.slot = w.in.from;
-            w.pos = lo;
         }
         w.r = max(s.start[w.slot], w.in.r0);
         w.end = min(s.start[w.slot + 1], w.in.r1);
@@ -194,9 +200,7 @@ struct Phase {
     __device__ __forceinline__ void next_tile(Place &w) const {
         w.step = 0;
         w.r += 8 * kCols;
-        if (w.r < w.end) return;
-        w.pos += w.n;
-        settle(w);
+        if (w.r >= w.end) take_tile(w);
     }
     __device__ __forceinline__ void move_ahead() {
         source += kPieces * 128;
@@ -323,27 +327,28 @@ struct Phase {
         const uint32_t a = ring.data + ring.out * kStepBytes + (lane & 15) * kRowStride + (lane >> 4) * 16;
         const uint32_t b = smem_u32(stage) + u0 * (k8 ? 256 : 128) + (lane >> 3) * 16;
         if constexpr (!k8) {
-            uint32_t w[8][4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < 4 || two) load_matrices(w[j], a + j * 32);
+            for (int u = 0; u < kPieces; ++u) {
+                if (u > 0 && !two) break;
+                uint32_t w[4][4];
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) {
-                if (c > 0 && r + 8 * c > last) break;
-                const uint32_t row = b + min(r + 8 * c + (lane & 7), last) * stride;
-                uint32_t v[4][4];
+                for (int j = 0; j < 4; ++j) load_matrices(w[j], a + u * 128 + j * 32);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < 2 || two) load_matrices(v[j], row + j * 64);
-                float odd[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (int c = 0; c < kCols; ++c) {
+                    if (c > 0 && r + 8 * c > last) break;
+                    const uint32_t row = b + min(r + 8 * c + (lane & 7), last) * stride + u * 128;
+                    uint32_t v[2][4];
 #pragma unroll
-                for (int j = 0; j < 8; j += 2)
-                    if (j < 4 || two) {
-                        mma16<false>(d[c], w[j][0], w[j][1], w[j][2], w[j][3], v[j / 2][0], v[j / 2][1]);
-                        mma16<false>(odd, w[j + 1][0], w[j + 1][1], w[j + 1][2], w[j + 1][3], v[j / 2][2], v[j / 2][3]);
+                    for (int j = 0; j < 2; ++j) load_matrices(v[j], row + j * 64);
+                    float odd[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        mma16<false>(d[c], w[2 * j][0], w[2 * j][1], w[2 * j][2], w[2 * j][3], v[j][0], v[j][1]);
+                        mma16<false>(odd, w[2 * j + 1][0], w[2 * j + 1][1], w[2 * j + 1][2], w[2 * j + 1][3], v[j][2], v[j][3]);
                     }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d[c][i] += odd[i];
+                    for (int i = 0; i < 4; ++i) d[c][i] += odd[i];
+                }
             }
         } else {
 #pragma unroll
@@ -356,14 +361,6 @@ struct Phase {
                 const float w0 = e8_scale(__shfl_sync(kFull, x.x, q & 31) >> shift & 255);
                 const float w1 = kUp ? e8_scale(__shfl_sync(kFull, x.y, q & 31) >> shift & 255) : w0;
                 const unsigned char *f = stage + room * stride + 8 * q;
-                uint32_t h[4][8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        h[j][2 * i] = codes_half2<0>(w[j][i]);
-                        h[j][2 * i + 1] = codes_half2<1>(w[j][i]);
-                    }
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) {
                     if (c > 0 && r + 8 * c > last) break;
@@ -374,10 +371,15 @@ struct Phase {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) load_matrices(v[j], row + j * 64);
                     float sum[2][4] = {};
+                    // (the codes are turned into fp16 again for every eight tokens, of which few experts have
+                    // more: held for all they would not fit the registers)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        mma16<true>(sum[0], h[j][0], h[j][2], h[j][1], h[j][3], v[j][0], v[j][1]);
-                        mma16<true>(sum[1], h[j][4], h[j][6], h[j][5], h[j][7], v[j][2], v[j][3]);
+                        const uint32_t *q4 = w[j];
+                        mma16<true>(sum[0], codes_half2<0>(q4[0]), codes_half2<0>(q4[1]), codes_half2<1>(q4[0]),
+                                    codes_half2<1>(q4[1]), v[j][0], v[j][1]);
+                        mma16<true>(sum[1], codes_half2<0>(q4[2]), codes_half2<0>(q4[3]), codes_half2<1>(q4[2]),
+                                    codes_half2<1>(q4[3]), v[j][2], v[j][3]);
                     }
                     d[c][0] += (sum[0][0] + sum[1][0]) * f0.x * w0 * f0.y;
                     d[c][1] += (sum[0][1] + sum[1][1]) * f1.x * w0 * f1.y;
@@ -501,58 +503,78 @@ __device__ __forceinline__ int make_lists(const LayerArgs &p, Lists &s) {
     return slots;
 }
 
+// The range that has tile i of n (range r: those from n r / ranges on).
+__device__ __forceinline__ int range_of(int i, int n, int ranges) {
+    return (int)((((int64_t)i + 1) * ranges - 1) / n);
+}
+
 template <bool k8>
 __global__ void __launch_bounds__(kThreads, 1) layer_experts_kernel(const LayerArgs p) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_align<128>(smem_raw);
     Lists &s = *reinterpret_cast<Lists *>(smem);
     unsigned char *stage = smem + (sizeof(Lists) + 127) / 128 * 128;
-    unsigned *tickets = p.counters, *up_done = p.counters + 1, *down_done = p.counters + 2;
+    unsigned *tickets = p.counters, *down_done = p.counters + 1, *up_done = p.counters + 2;
     const int warp = threadIdx.x >> 5;
     StepRing ring{smem_u32(stage) + warp * (kRing * kStepBytes), 0u, 0u};
     stage += kWarps * kRing * kStepBytes;
     pdl_wait();
-    if (threadIdx.x == 0) s.ticket = (int)atomicAdd(tickets, 1u);
+    if (threadIdx.x == 0) {
+        s.ticket = (int)atomicAdd(tickets, 1u);
+        s.mine = 0;
+    }
     const int slots = make_lists(p, s);
-    const auto tell = [&](unsigned *done) {
-        __threadfence();  // what this range wrote may be read
-        __syncthreads();
-        if (threadIdx.x == 0) atomicAdd(done, 1u);
-    };
-    const auto wait = [&](const unsigned *done) {
-        if (threadIdx.x == 0) s.good = wait_count(done, (unsigned)p.ranges, p.status);
-        __syncthreads();
-        return s.good != 0;
-    };
     for (;;) {
         __syncthreads();
-        const int ticket = s.ticket, range = ticket % p.ranges;
+        const int range = s.ticket;
+        if (range >= p.ranges) break;
         __syncthreads();
-        if (threadIdx.x == 0) s.ticket = (int)atomicAdd(tickets, 1u);  // the next one, taken while this one runs
-        if (ticket < p.ranges) {
-            Phase<true, k8> up(p, s, stage, ring, slots, range);
-            up.run([] { return true; });
-            tell(up_done);
-        } else if (ticket < 2 * p.ranges) {
-            Phase<false, k8> down(p, s, stage, ring, slots, range);
-            if (!down.run([&] { return wait(up_done); })) {
-                wait_copies<0>();
-                return;
-            }
-            tell(down_done);
-        } else if (ticket < 3 * p.ranges) {
-            if (!wait(down_done)) return;
-            const int n = p.T * p.H, lo = (int)((int64_t)n * range / p.ranges), hi = (int)((int64_t)n * (range + 1) / p.ranges);
-            for (int i = lo + (int)threadIdx.x; i < hi; i += kThreads) {
-                const int t = i / p.H, h = i - t * p.H;
-                float sum = 0.0f;
+        if (threadIdx.x == 0) {
+            s.range[s.mine++] = (unsigned short)range;
+            s.queue = 0;
+            s.ticket = (int)atomicAdd(tickets, 1u);
+        }
+        __syncthreads();
+        Phase<true, k8> up(p, s, stage, ring, slots, range);
+        up.run([] { return true; });
+        __threadfence();  // what this range wrote may be read
+        __syncthreads();
+        if (threadIdx.x == 0) atomicExch(up_done + range, 1u);
+    }
+    const int mine = s.mine;
+    for (int i = 0; i < mine; ++i) {
+        __syncthreads();
+        if (threadIdx.x == 0) s.queue = 0;
+        __syncthreads();
+        Phase<false, k8> down(p, s, stage, ring, slots, s.range[i]);
+        const bool good = down.run([&] {
+            // the ranges of W1's tiles of the slots
+            const int per = (p.F + 7) / 8, from = range_of(down.s0 * per, slots * per, p.ranges);
+            const int to = down.s0 < down.s1 ? range_of(down.s1 * per - 1, slots * per, p.ranges) : from - 1;
+            int ok = 1;
+            if (from + (int)threadIdx.x <= to) ok = wait_count(up_done + from + threadIdx.x, 1u, p.status);
+            return __syncthreads_and(ok) != 0;
+        });
+        if (!good) {
+            wait_copies<0>();
+            return;
+        }
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) atomicAdd(down_done, 1u);
+    }
+    int ok = 1;
+    if (mine && threadIdx.x == 0) ok = wait_count(down_done, (unsigned)p.ranges, p.status);
+    if (!__syncthreads_and(ok)) return;
+    for (int j = 0; j < mine; ++j) {
+        const int n = p.T * p.H, lo = (int)((int64_t)n * s.range[j] / p.ranges), hi = (int)((int64_t)n * (s.range[j] + 1) / p.ranges);
+        for (int i = lo + (int)threadIdx.x; i < hi; i += kThreads) {
+            const int t = i / p.H, h = i - t * p.H;
+            float sum = 0.0f;
 #pragma unroll 8
-                for (int q = 0; q < p.k; ++q)
-                    sum = fmaf(__ldcg(p.combine + t * p.k + q), __ldcg(p.y + (int64_t)(t * p.k + q) * p.H + h), sum);
-                p.out[i] = __float2bfloat16_rn(sum);
-            }
-        } else {
-            break;
+            for (int q = 0; q < p.k; ++q)
+                sum = fmaf(__ldcg(p.combine + t * p.k + q), __ldcg(p.y + (int64_t)(t * p.k + q) * p.H + h), sum);
+            p.out[i] = __float2bfloat16_rn(sum);
         }
     }
     pdl_trigger();
