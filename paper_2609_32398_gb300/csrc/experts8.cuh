@@ -35,7 +35,7 @@ struct Product8Args {
     float *wide;           // plain: Y [R][N] in fp32 instead of out (may be null)
     uint8_t *codes;        // up: [R][F]
     uint8_t *exponents;    //     [R][ceil(F / 128)]
-    bool words;            // rows of exponents are whole aligned words, set by the launch
+    int align;             // of rows of exponents in bytes: 4, 2 or 1, set by the launch
     int *status;
 };
 

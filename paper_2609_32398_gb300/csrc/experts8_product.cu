@@ -10,11 +10,13 @@
 // step has one exponent per weight block and per routed row.  240 and not 256: two
 // accumulators leave 32 TMEM columns for the exponents of two steps.
 //
-// Exponents.  The instruction wants a word of four bytes (one per 32 columns) for every
-// row, 32 rows to a TMEM column.  One warp of each CTA writes the four equal bytes of its 128
-// weight rows and of all the tile's routed rows to the step's place in shared memory,
-// reading four steps' bytes of a row at a time and a group ahead; the MMA's thread has
-// them copied to TMEM before the step's products, in order with them.
+// Exponents.  The instruction wants a word of four bytes for every row, 32 rows to a TMEM
+// column, and takes the byte that its descriptor names: a word is a row's exponents of four
+// steps, as they lie in memory.  One warp of each CTA writes those of its 128 weight rows and of
+// all the tile's routed rows to one of four places in shared memory, running ahead of the ring, and the
+// MMA's thread has them copied to TMEM before the four steps' products, in order with them.
+// (Written for every step, four equal bytes a word, that warp was the bound of short
+// contractions: 379 us for 131072 rows of 768 to 2048 columns, of which 195 without it.)
 //
 // Epilogues: the rows as they are (bf16, or fp32 for a join), and SwiGLU with its result
 // in blocks of 1 x 128 again.  A pair's tile is 128 gate rows and their up rows, 64 of each a
@@ -48,7 +50,8 @@ __host__ __device__ constexpr int threads_of(int mode, bool gather) {
 __host__ __device__ constexpr int block_rows(int mode) { return mode == kProduct8Up ? 32 : 16; }
 __host__ __device__ constexpr uint32_t turn_bytes(int mode) { return kGroups * 4 * block_rows(mode) * 128; }
 constexpr uint32_t kABytes = 128 * 128;       // a CTA's weight rows of one step
-constexpr uint32_t kScaleBytes = 512 + 1024;  // a CTA's exponents of one step: weights, routed rows
+constexpr uint32_t kScaleBytes = 512 + 1024;  // a CTA's exponents of four steps: weights, routed rows
+constexpr int kScalePlaces = 4;
 constexpr int kMaxStages = 12;
 constexpr uint32_t kSmemLimit = 232448;
 constexpr uint32_t kScaleColumn = 2 * kTileN;  // TMEM: 4 columns of weights, 8 of routed rows, twice
@@ -62,12 +65,12 @@ struct PairArgs8 {
     uint32_t b_bytes;  // room for a CTA's routed rows of one step
 };
 
-// Shared memory: ring [stages][weights | rows], exponents [stages][weights | rows], turn
+// Shared memory: ring [stages][weights | rows], exponents [places][weights | rows], turn
 // blocks, and for each expert its first tile, first row and the width of its tiles [E + 1].
 __host__ __device__ inline uint32_t table_bytes(int E) { return 4u * 3u * ((uint32_t)E + 1u); }
 __host__ __device__ inline uint32_t off_scales(int stages, uint32_t b_bytes) { return stages * (kABytes + b_bytes); }
 __host__ __device__ inline uint32_t off_turn(int stages, uint32_t b_bytes) {
-    return off_scales(stages, b_bytes) + stages * kScaleBytes;
+    return off_scales(stages, b_bytes) + kScalePlaces * kScaleBytes;
 }
 
 // D (+)= A B with block scales at the TMEM addresses sa and sb.
@@ -91,9 +94,9 @@ __device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
            ((uint64_t)1 << 46);
 }
 // Instruction descriptor: e4m3 A and B, both K-major, exponent bytes as scales, M = 256 over
-// the pair, N = n (a multiple of 16), the first of a word's four bytes.
-__host__ __device__ constexpr uint32_t pair_idesc8(int n) {
-    return ((uint32_t)(n / 8) << 17) | (1u << 23) | ((uint32_t)(256 / 16) << 24);
+// the pair, N = n (a multiple of 16), byte j of the exponents' words.
+__host__ __device__ constexpr uint32_t pair_idesc8(int n, int j) {
+    return ((uint32_t)(n / 8) << 17) | (1u << 23) | ((uint32_t)(256 / 16) << 24) | ((uint32_t)j << 4) | ((uint32_t)j << 29);
 }
 // A value into the other CTA's shared memory, its four bytes counted on a barrier there.
 __device__ __forceinline__ void send_word(uint32_t to, unsigned v, uint32_t bar) {
@@ -135,6 +138,7 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
     unsigned char *scales = smem + off_scales(stages, a.b_bytes), *turn = smem + off_turn(stages, a.b_bytes);
     int *first = reinterpret_cast<int *>(turn + turn_bytes(kMode)), *start = first + E + 1, *width = start + E + 1;
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+    __shared__ __align__(8) uint64_t scales_full[kScalePlaces], scales_empty[kScalePlaces];
     __shared__ __align__(8) uint64_t top_here[2][kUpBlocks][4];  // up: the other CTA's values are here
     __shared__ unsigned top_of[2][kUpBlocks * 32];
     __shared__ uint32_t tmem_slot;
@@ -144,8 +148,12 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
     const uint32_t rank = cluster_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < stages; ++i) {
-            mbar_init(&full[i], 1 + 2 + (kGather ? 2 * load_split(kMode) : 0));
+            mbar_init(&full[i], 1 + (kGather ? 2 * load_split(kMode) : 0));
             mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < kScalePlaces; ++i) {
+            mbar_init(&scales_full[i], 2);
+            mbar_init(&scales_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&acc_full[i], 1);
@@ -211,12 +219,17 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
         bool good = true;
         const int none = (int)p.a_rows;
         const int nb = kMode == kProduct8Up ? blocks8(p.N / 2) : blocks8(p.N);
-        const bool words = p.words;
         const unsigned unit = 0x7f7f7f7fu;  // scale 1, for what nobody reads
-        auto four = [&](const uint8_t *row, int k) -> unsigned {
+        const uint32_t empty_addr = smem_u32(scales_empty), full_addr = map_to_rank(scales_full, 0);
+        auto four = [&](const uint8_t *row, int k) -> unsigned {  // of steps k .. k + 3, k a multiple of 4
             if (!row) return unit;
-            if (words) return __ldg(reinterpret_cast<const unsigned *>(row + k));
+            if (p.align == 4) return __ldg(reinterpret_cast<const unsigned *>(row + k));
             unsigned w = 0;
+            if (p.align == 2) {
+                w = __ldg(reinterpret_cast<const unsigned short *>(row + k));
+                if (k + 2 < steps) w |= (unsigned)__ldg(reinterpret_cast<const unsigned short *>(row + k + 2)) << 16;
+                return w;
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (k + j < steps) w |= (unsigned)__ldg(row + k + j) << (8 * j);
@@ -241,7 +254,7 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
 #pragma unroll
             for (int c = 0; c < 8; ++c) next[c] = four(row[c], 0);
             next[8] = four(weight, 0);
-            for (int k = 0; good && k < steps; k += 4) {
+            for (int k = 0; k < steps; k += 4) {
 #pragma unroll
                 for (int c = 0; c < 9; ++c) now[c] = next[c];
                 if (k + 4 < steps) {
@@ -249,24 +262,16 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
                     for (int c = 0; c < 8; ++c) next[c] = four(row[c], k + 4);
                     next[8] = four(weight, k + 4);
                 }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (k + j >= steps) break;
-                    good = pair_wait_warp(empty0 + 8 * at.s, at.phase ^ 1u, p.status, abort, lane);
-                    if (!good) break;
-                    const unsigned pick = 0x1111u * (unsigned)j;  // byte j, four times
-                    uint4 *to = reinterpret_cast<uint4 *>(scales + at.s * kScaleBytes) + lane;
-                    const unsigned w = __byte_perm(now[8], 0, pick);
-                    to[0] = make_uint4(w, w, w, w);
-                    to[32] = make_uint4(__byte_perm(now[0], 0, pick), __byte_perm(now[1], 0, pick),
-                                        __byte_perm(now[2], 0, pick), __byte_perm(now[3], 0, pick));
-                    to[64] = make_uint4(__byte_perm(now[4], 0, pick), __byte_perm(now[5], 0, pick),
-                                        __byte_perm(now[6], 0, pick), __byte_perm(now[7], 0, pick));
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(full_pair + 8 * at.s);
-                    at.next(stages);
-                }
+                good = pair_wait_warp(empty_addr + 8 * at.s, at.phase ^ 1u, p.status, abort, lane);
+                if (!good) break;
+                uint4 *to = reinterpret_cast<uint4 *>(scales + at.s * kScaleBytes) + lane;
+                to[0] = make_uint4(now[8], now[8], now[8], now[8]);
+                to[32] = make_uint4(now[0], now[1], now[2], now[3]);
+                to[64] = make_uint4(now[4], now[5], now[6], now[7]);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(full_addr + 8 * at.s);
+                at.next(kScalePlaces);
             }
         }
         __syncwarp();
@@ -341,12 +346,13 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
         // ---------------------------------------------------------- MMA issuer
         if (rank == 0) {
             const bool one = elect_one();
-            Ring at{0, 0};
+            Ring at{0, 0}, place{0, 0};
             int done = 0;
             bool good = true;
             const uint64_t ad0 = umma_desc_sw128(ring), bd0 = umma_desc_sw128(ring + kABytes);
             const uint64_t sd0 = desc_scales(smem_u32(scales));
             const uint32_t acc_full0 = smem_u32(acc_full), acc_empty0 = smem_u32(acc_empty);
+            const uint32_t scales_full0 = smem_u32(scales_full), scales_empty0 = smem_u32(scales_empty);
             uint32_t sa = tmem + kScaleColumn;
             for (bool any = walk.find(); good && any; any = walk.next(), ++done) {
                 const uint32_t buf = done & 1, turns = (uint32_t)done >> 1;
@@ -354,25 +360,36 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
                 if (!good) break;
                 tc_fence_after();
                 const uint32_t d = tmem + buf * kTileN;
-                const uint32_t idesc = pair_idesc8(tl.width);
+                const uint32_t idesc = pair_idesc8(tl.width, 0);
                 uint32_t more = 0;
                 for (int k = 0; k < steps; ++k) {
+                    if ((k & 3) == 0) {
+                        good = pair_wait_all(scales_full0 + 8 * place.s, place.phase, p.status, abort);
+                        if (!good) break;
+                        tc_fence_after();
+                        sa = (tmem + kScaleColumn) + (tmem + kScaleColumn + 12 - sa);  // the other place
+                        const uint32_t off = place.s * (kScaleBytes / 16);
+                        if (one) {
+                            pair_copy_scales(sa, desc_at(sd0, off));
+                            pair_copy_scales(sa + 4, desc_at(sd0, off + 512 / 16));
+                            pair_copy_scales(sa + 8, desc_at(sd0, off + 1024 / 16));
+                            pair_commit(scales_empty0 + 8 * place.s);
+                        }
+                        __syncwarp();
+                        place.next(kScalePlaces);
+                    }
                     good = pair_wait_all(full0 + 8 * at.s, at.phase, p.status, abort);
                     if (!good) break;
                     tc_fence_after();
-                    const uint32_t off = at.s * (stage_bytes / 16), soff = at.s * (kScaleBytes / 16);
+                    const uint32_t off = at.s * (stage_bytes / 16), pick = (uint32_t)(k & 3) * ((1u << 4) | (1u << 29));
                     if (one) {
-                        pair_copy_scales(sa, desc_at(sd0, soff));
-                        pair_copy_scales(sa + 4, desc_at(sd0, soff + 512 / 16));
-                        pair_copy_scales(sa + 8, desc_at(sd0, soff + 1024 / 16));
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk)
-                            pair_mma8(d, desc_at(ad0, off + kk * (32 / 16)), desc_at(bd0, off + kk * (32 / 16)), idesc, sa,
+                            pair_mma8(d, desc_at(ad0, off + kk * (32 / 16)), desc_at(bd0, off + kk * (32 / 16)), idesc | pick, sa,
                                       sa + 4, kk > 0 ? 1u : more);
                         pair_commit(empty0 + 8 * at.s);
                     }
                     __syncwarp();
-                    sa = (tmem + kScaleColumn) + (tmem + kScaleColumn + 12 - sa);  // the other place
                     more = 1;
                     at.next(stages);
                 }
@@ -490,8 +507,8 @@ template <int kMode, bool kGather>
 cudaError_t launch(const Product8Args &p, cudaStream_t s) {
     PairArgs8 a = {};
     a.p = p;
-    a.p.words = blocks8(p.K) % 4 == 0 && reinterpret_cast<uintptr_t>(p.ax) % 4 == 0 &&
-                reinterpret_cast<uintptr_t>(p.wx) % 4 == 0;
+    const uintptr_t lowest = reinterpret_cast<uintptr_t>(p.ax) | reinterpret_cast<uintptr_t>(p.wx) | (uintptr_t)blocks8(p.K);
+    a.p.align = lowest % 4 == 0 ? 4 : lowest % 2 == 0 ? 2 : 1;
     CUtensorMap wmap, amap;
     const uint64_t E = p.E, N = p.N, K = p.K;
     a.m_tiles = kMode == kProduct8Up ? (p.N / 2 + 127) / 128 : (p.N + 255) / 256;
@@ -506,8 +523,8 @@ cudaError_t launch(const Product8Args &p, cudaStream_t s) {
                         : encode_tensor_map_3d_u8(&amap, p.A, 1, (uint64_t)p.a_rows, K, 128, half));
     const int sms = sm_count();
     if (!ok || sms < 2) return cudaErrorInvalidValue;
-    const uint32_t fixed = 1024 + turn_bytes(kMode) + table_bytes(p.E) + 4096;
-    a.stages = (int)((kSmemLimit - fixed) / (kABytes + a.b_bytes + kScaleBytes));
+    const uint32_t fixed = 1024 + kScalePlaces * kScaleBytes + turn_bytes(kMode) + table_bytes(p.E) + 4096;
+    a.stages = (int)((kSmemLimit - fixed) / (kABytes + a.b_bytes));
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     if (a.stages < kLoadSteps + 1) return cudaErrorInvalidConfiguration;
     const uint32_t smem = 1024 + off_turn(a.stages, a.b_bytes) + turn_bytes(kMode) + table_bytes(p.E);
