@@ -12,7 +12,7 @@
 //
 // Exponents.  The instruction wants a word of four bytes for every row, 32 rows to a TMEM
 // column, and takes the byte that its descriptor names: a word is a row's exponents of four
-// steps, as they lie in memory.  One warp of each CTA writes those of its 128 weight rows and of
+// steps, as they lie in memory.  Warps of each CTA write those of its 128 weight rows and of
 // all the tile's routed rows to one of four places in shared memory, running ahead of the ring, and the
 // MMA's thread has them copied to TMEM before the four steps' products, in order with them.
 // (Written for every step, four equal bytes a word, that warp was the bound of short
@@ -37,14 +37,19 @@ constexpr int kTileN = 240;               // routed rows of a tile at most
 constexpr int kEpiWarps = 8;
 constexpr int kGroups = kEpiWarps / 4;
 constexpr int kScaleWarp = 2 + kEpiWarps;
-constexpr int kFirstLoader = kScaleWarp + 1;
+// Warps that write exponents take the groups of four steps in turn, a place each: a group waits
+// for its rows' ids and then for their exponents, 1 to 2 us each under load, and a short contraction
+// has a tile of two groups every 2 us (131072 rows of 768: 323 us with one such warp).  Where rows
+// are gathered, the loaders leave registers for two.
+__host__ __device__ constexpr int scale_warps(bool gather) { return gather ? 2 : 4; }
+__host__ __device__ constexpr int first_loader(bool gather) { return kScaleWarp + scale_warps(gather); }
 // Gathering warps, as in the bf16 products: load_split of them share a step, kLoadSteps steps
 // are filled at a time.
 constexpr int kLoadSteps = 3;
 __host__ __device__ constexpr int load_split(int mode) { return mode == kProduct8Up ? 2 : 4; }
 __host__ __device__ constexpr int load_warps(int mode) { return kLoadSteps * load_split(mode); }
 __host__ __device__ constexpr int threads_of(int mode, bool gather) {
-    return (kFirstLoader + (gather ? load_warps(mode) : 1)) * 32;
+    return (first_loader(gather) + (gather ? load_warps(mode) : 1)) * 32;
 }
 // The epilogue's blocks of 32 (up) or 16 routed rows x 128 values.
 __host__ __device__ constexpr int block_rows(int mode) { return mode == kProduct8Up ? 32 : 16; }
@@ -131,7 +136,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kMode, kG
 product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap, const PairArgs8 a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_align<1024>(smem_raw);
-    constexpr int kThreads = threads_of(kMode, kGather);
+    constexpr int kThreads = threads_of(kMode, kGather), kFirstLoader = first_loader(kGather);
     const Product8Args &p = a.p;
     const int E = p.E, stages = a.stages;
     const uint32_t stage_bytes = kABytes + a.b_bytes;
@@ -211,7 +216,7 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
             for (int i = it > stages ? it - stages : 0; i < it; ++i)
                 mbar_wait(&full[i % stages], (uint32_t)(i / stages) & 1u, p.status);
         __syncwarp();
-    } else if (warp == kScaleWarp) {
+    } else if (warp >= kScaleWarp && warp < kFirstLoader) {
         // ---------------------------------------------------------- exponents
         // Lane l has rows l, 32 + l, ... of the weights (all of a block share one; up: 16 gate
         // rows and 16 up rows in turn) and of the tile.
@@ -221,6 +226,8 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
         const int nb = kMode == kProduct8Up ? blocks8(p.N / 2) : blocks8(p.N);
         const unsigned unit = 0x7f7f7f7fu;  // scale 1, for what nobody reads
         const uint32_t empty_addr = smem_u32(scales_empty), full_addr = map_to_rank(scales_full, 0);
+        constexpr int kTurns = scale_warps(kGather);
+        int turn = 0;  // whose the next group is
         auto four = [&](const uint8_t *row, int k) -> unsigned {  // of steps k .. k + 3, k a multiple of 4
             if (!row) return unit;
             if (p.align == 4) return __ldg(reinterpret_cast<const unsigned *>(row + k));
@@ -250,18 +257,12 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
             } else if (2 * tl.m + (int)rank < nb) {
                 weight = p.wx + ((int64_t)tl.e * nb + 2 * tl.m + (int)rank) * steps;
             }
-            unsigned next[9], now[9];
+            for (int k = 0; good && k < steps; k += 4, at.next(kScalePlaces), turn = turn + 1 == kTurns ? 0 : turn + 1) {
+                if (turn != warp - kScaleWarp) continue;
+                unsigned now[9];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) next[c] = four(row[c], 0);
-            next[8] = four(weight, 0);
-            for (int k = 0; k < steps; k += 4) {
-#pragma unroll
-                for (int c = 0; c < 9; ++c) now[c] = next[c];
-                if (k + 4 < steps) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) next[c] = four(row[c], k + 4);
-                    next[8] = four(weight, k + 4);
-                }
+                for (int c = 0; c < 8; ++c) now[c] = four(row[c], k);
+                now[8] = four(weight, k);
                 good = pair_wait_warp(empty_addr + 8 * at.s, at.phase ^ 1u, p.status, abort, lane);
                 if (!good) break;
                 uint4 *to = reinterpret_cast<uint4 *>(scales + at.s * kScaleBytes) + lane;
@@ -271,7 +272,6 @@ product8_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant_
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(full_addr + 8 * at.s);
-                at.next(kScalePlaces);
             }
         }
         __syncwarp();
