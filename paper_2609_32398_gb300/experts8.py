@@ -24,17 +24,31 @@ differentiable: an operand that wants a gradient while a graph is recorded is re
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 import torch.autograd.forward_ad as fwd
 
 from . import doloss as dl
-from .experts import _bf16, _device, _fp32, _index, _no_tangent, _positions, _raw_stream, _status
+from .experts import _bf16, _device, _flag_ptrs, _fp32, _index, _no_tangent, _positions, _raw_stream, _status
 
 BLOCK = 128
+_E4M3, _U8, _BF16 = torch.float8_e4m3fn, torch.uint8, torch.bfloat16
 
 
 def _blocks(n: int) -> int:
     return (n + BLOCK - 1) // BLOCK
+
+
+@functools.lru_cache(maxsize=256)
+def _exponent_shape(name: str, size: torch.Size, gated: bool) -> tuple:
+    if len(size) == 2:
+        return size[0], _blocks(size[1])
+    if not gated:
+        return size[0], _blocks(size[1]), _blocks(size[2])
+    if size[1] % 2:
+        raise ValueError(f"{name} is gated and needs an even number of rows")
+    return size[0], 2 * _blocks(size[1] // 2), _blocks(size[2])
 
 
 class Blocks:
@@ -52,23 +66,17 @@ class Blocks:
 
     def check(self, name: str, dim: int, gated: bool, device: int) -> None:
         c, e = self.codes, self.exponents
-        if (c.dtype is not torch.float8_e4m3fn or e.dtype is not torch.uint8 or c.dim() != dim
-                or not (c.is_contiguous() and e.is_contiguous())
-                or c.get_device() != device or e.get_device() != device or device < 0):
+        if (c.dtype is not _E4M3 or e.dtype is not _U8 or c.dim() != dim or device < 0
+                or c.get_device() != device or e.get_device() != device
+                or not (c.is_contiguous() and e.is_contiguous())):
             raise ValueError(f"{name} must be contiguous CUDA codes float8_e4m3fn of {dim} dimensions and "
                              "exponents uint8, all tensors on one device")
-        if self.gated != gated:
+        if self.gated is not gated:
             raise ValueError(f"{name} must be {'' if gated else 'not '}gated")
-        if dim == 2:
-            shape = (c.shape[0], _blocks(c.shape[1]))
-        elif gated:
-            if c.shape[1] % 2:
-                raise ValueError(f"{name} is gated and needs an even number of rows")
-            shape = (c.shape[0], 2 * _blocks(c.shape[1] // 2), _blocks(c.shape[2]))
-        else:
-            shape = (c.shape[0], _blocks(c.shape[1]), _blocks(c.shape[2]))
-        if e.shape != shape:
-            raise ValueError(f"the exponents of {name} must be {list(shape)}, here {list(e.shape)}")
+        size = c.shape
+        if e.shape != _exponent_shape(name, size, gated):
+            raise ValueError(f"the exponents of {name} must be {list(_exponent_shape(name, size, gated))}, "
+                             f"here {list(e.shape)}")
 
     def values(self) -> torch.Tensor:
         """do_block_values: the values it stands for, bf16, exact for what this module quantised."""
@@ -89,11 +97,16 @@ class Blocks:
         return out
 
 
-def _no_graph(name: str, *tensors) -> None:
+def _no_graph(name: str, x: torch.Tensor, combine: torch.Tensor | None = None) -> None:
     if fwd._current_level >= 0:
-        _no_tangent(name, *tensors)
-    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+        _no_tangent(name, x, combine)
+    if (x.requires_grad or (combine is not None and combine.requires_grad)) and torch.is_grad_enabled():
         raise RuntimeError(f"{name} is not differentiable: call it under torch.no_grad()")
+
+
+@functools.lru_cache(maxsize=256)
+def _ffn_bytes(T: int, k: int, H: int, F: int) -> int:
+    return int(dl.lib().do_expert_ffn8_workspace_size(T, k, H, F))
 
 
 def quantise_rows(x: torch.Tensor) -> Blocks:
@@ -102,12 +115,15 @@ def quantise_rows(x: torch.Tensor) -> Blocks:
     dev = _device(x)
     _bf16("x", x, 2, dev)
     M, K = x.shape
-    q = Blocks(torch.empty((M, K), dtype=torch.float8_e4m3fn, device=x.device),
-               torch.empty((M, _blocks(K)), dtype=torch.uint8, device=x.device))
+    device = x.device
+    codes = torch.empty((M, K), dtype=_E4M3, device=device)
+    exponents = torch.empty((M, (K + BLOCK - 1) // BLOCK), dtype=_U8, device=device)
     if M:
-        dl._check("do_quantise_rows", dl.lib().do_quantise_rows(
-            x.data_ptr(), M, K, q.codes.data_ptr(), q.exponents.data_ptr(), _raw_stream(dev)))
-    return q
+        st = (dl._lib or dl.lib()).do_quantise_rows(x.data_ptr(), M, K, codes.data_ptr(), exponents.data_ptr(),
+                                                    _raw_stream(dev))
+        if st:
+            dl._check("do_quantise_rows", st)
+    return Blocks(codes, exponents)
 
 
 def quantise_weights(w: torch.Tensor, gated: bool = False) -> Blocks:
@@ -137,13 +153,14 @@ def _operands(a: Blocks, w: Blocks, gated: bool, offsets, rows, dev: int):
     E, N, Kw = w.codes.shape
     if Kw != K:
         raise ValueError("the weights must be [E, N, K] for rows [., K]")
-    R = T if rows is None else rows.numel()
-    if offsets is None:
-        if E != 1:
-            raise ValueError("offsets may be left out for a dense map, [1, N, K], only")
-    else:
+    R = T
+    if rows is not None:
+        R = rows.numel()
+        _index("rows", rows, R, dev)
+    if offsets is not None:
         _index("offsets", offsets, E + 1, dev)
-    _index("rows", rows, R, dev)
+    elif E != 1:
+        raise ValueError("offsets may be left out for a dense map, [1, N, K], only")
     return T, K, E, N, R
 
 
@@ -153,11 +170,15 @@ def matmul(a: Blocks, w: Blocks, offsets: torch.Tensor | None = None,
     of its expert; without offsets all rows go through the one map w [1,N,K]."""
     dev = _device(a.codes) if isinstance(a, Blocks) else -1
     T, K, E, N, R = _operands(a, w, False, offsets, rows, dev)
-    y = torch.empty((R, N), dtype=torch.bfloat16, device=a.codes.device)
+    codes = a.codes
+    y = torch.empty((R, N), dtype=_BF16, device=codes.device)
     if R:
-        dl._check("do_grouped_matmul8", dl.lib().do_grouped_matmul8(
-            a.codes.data_ptr(), a.exponents.data_ptr(), w.codes.data_ptr(), w.exponents.data_ptr(), dl._ptr(rows),
-            dl._ptr(offsets), T, K, N, E, R, y.data_ptr(), _status(dev), _raw_stream(dev)))
+        st = (dl._lib or dl.lib()).do_grouped_matmul8(
+            codes.data_ptr(), a.exponents.data_ptr(), w.codes.data_ptr(), w.exponents.data_ptr(),
+            None if rows is None else rows.data_ptr(), None if offsets is None else offsets.data_ptr(), T, K, N, E, R,
+            y.data_ptr(), _flag_ptrs.get(dev) or _status(dev), _raw_stream(dev))
+        if st:
+            dl._check("do_grouped_matmul8", st)
     return y
 
 
@@ -203,13 +224,15 @@ def expert_ffn(x: torch.Tensor, w1: Blocks, w2: Blocks, combine: torch.Tensor, o
     pos = _positions(pos, T, k, dev)
     if k == 0:
         return x.new_zeros((T, H))
-    out = x.new_empty((T, H))
+    device = x.device
+    out = torch.empty((T, H), dtype=_BF16, device=device)
     if T:
-        L = dl.lib()
-        n = L.do_expert_ffn8_workspace_size(T, k, H, F)
-        ws = x.new_empty(n, dtype=torch.uint8)
-        dl._check("do_expert_ffn8", L.do_expert_ffn8(
+        n = _ffn_bytes(T, k, H, F)
+        ws = torch.empty(n, dtype=_U8, device=device)
+        st = (dl._lib or dl.lib()).do_expert_ffn8(
             x.data_ptr(), w1.codes.data_ptr(), w1.exponents.data_ptr(), w2.codes.data_ptr(), w2.exponents.data_ptr(),
             combine.data_ptr(), rows.data_ptr(), offsets.data_ptr(), pos.data_ptr(), T, k, H, F, E, out.data_ptr(),
-            _status(dev), ws.data_ptr(), n, _raw_stream(dev)))
+            _flag_ptrs.get(dev) or _status(dev), ws.data_ptr(), n, _raw_stream(dev))
+        if st:
+            dl._check("do_expert_ffn8", st)
     return out

@@ -13,14 +13,21 @@ For more tokens, and where gradients are wanted, the same layer is
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 import torch.autograd.forward_ad as fwd
 
 from . import doloss as dl
-from .experts import _bf16, _device, _no_tangent, _raw_stream, _status
+from .experts import _bf16, _device, _flag_ptrs, _no_tangent, _raw_stream, _status
 from .experts8 import Blocks
 
 MAX_TOKENS = 64
+
+
+@functools.lru_cache(maxsize=256)
+def _bytes(T: int, k: int, H: int, F: int) -> int:
+    return int(dl.lib().do_moe_layer_workspace_size(T, k, H, F))
 
 
 def moe_layer(x: torch.Tensor, wr: torch.Tensor, w1, w2, k: int, gate: int = dl.GATE_SIGMOID_NORM):
@@ -58,15 +65,17 @@ def moe_layer(x: torch.Tensor, wr: torch.Tensor, w1, w2, k: int, gate: int = dl.
         raise ValueError("k must be between 1 and the number of experts")
     if T > MAX_TOKENS:
         raise ValueError(f"moe_layer takes {MAX_TOKENS} tokens at most: doloss.route and expert_ffn take any number")
-    out = x.new_empty((T, H))
-    ids = x.new_empty((T, k), dtype=torch.int32)
-    combine = x.new_empty((T, k), dtype=torch.float32)
+    device = x.device
+    out = torch.empty((T, H), dtype=torch.bfloat16, device=device)
+    ids = torch.empty((T, k), dtype=torch.int32, device=device)
+    combine = torch.empty((T, k), dtype=torch.float32, device=device)
     if T:
-        L = dl.lib()
-        n = L.do_moe_layer_workspace_size(T, k, H, F)
-        ws = x.new_empty(n, dtype=torch.uint8)
-        dl._check("do_moe_layer", L.do_moe_layer(
+        n = _bytes(T, k, H, F)
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
+        st = (dl._lib or dl.lib()).do_moe_layer(
             x.data_ptr(), wr.data_ptr(), c1.data_ptr(), w1.exponents.data_ptr() if eight else None, c2.data_ptr(),
             w2.exponents.data_ptr() if eight else None, T, H, F, E, k, gate, out.data_ptr(), ids.data_ptr(),
-            combine.data_ptr(), _status(dev), ws.data_ptr(), n, _raw_stream(dev)))
+            combine.data_ptr(), _flag_ptrs.get(dev) or _status(dev), ws.data_ptr(), n, _raw_stream(dev))
+        if st:
+            dl._check("do_moe_layer", st)
     return out, ids, combine
