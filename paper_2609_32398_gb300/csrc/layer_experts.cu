@@ -6,12 +6,12 @@
 // the memory is what bounds it and the whole design is for keeping reads in flight:
 //
 //  - One CTA an SM.  The rows of all used experts' W1 form one list that is divided evenly,
-//    to the row: range i of n has its i-th n-th part; so do those of W2, and the elements of out.
+//    to the tile: range i of n has its i-th n-th part; so do those of W2, and the elements of out.
 //    A range meets the tokens of one or two experts.  (With a block of out's columns for each
 //    CTA no results would pass through memory, but every CTA would read the activations of all
 //    tokens, as much as the weights for 64 tokens.)
-//  - Each warp has tiles of its own, 16 weight rows (up: eight gate rows and their up rows)
-//    over the whole k, and a ring of its own of two steps of 256 bytes of each row, filled by
+//  - Each warp takes tiles of its own, 16 weight rows (up: eight gate rows and their up rows)
+//    over the whole k, and has a ring of two steps of 256 bytes of each row, filled by
 //    asynchronous copies: 128 KB in flight an SM and no register held by them.  (Straight
 //    to registers, the wait for one tile took in the loads of the next, and what there was to
 //    compute between them doubled the time.)  The next step's copies leave as soon as the
@@ -44,7 +44,6 @@ constexpr int kRing = 2;                       // steps in a warp's ring
 constexpr int kPieces = 2;                     // 128-byte pieces of a row in a step
 constexpr int kRowStride = kPieces * 128 + 16; // of a row in the ring: no bank conflicts
 constexpr int kStepBytes = 16 * kRowStride;
-constexpr int kCols = 4;                       // tiles of eight tokens that share a step
 constexpr int kRoutes = kLayerTokens * kLayerChoices;
 constexpr uint32_t kSmemLimit = 232448;
 
@@ -107,6 +106,7 @@ struct StepRing {
 template <bool kUp, bool k8>
 struct Phase {
     static constexpr int kTile = kUp ? 8 : 16;  // rows of a tile
+    static constexpr int kCols = k8 ? 2 : 4;    // eights of tokens that share a step (registers)
     const LayerArgs &p;
     Lists &s;
     unsigned char *stage;
