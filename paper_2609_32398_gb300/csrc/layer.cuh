@@ -30,7 +30,7 @@ struct LayerArgs {
     int stage_bytes;       // shared memory for the products' rows
 };
 
-constexpr int kLayerFewRows = 64;
+constexpr int kLayerFewRows = 40;
 
 constexpr int kLayerRanges = 200;   // at most
 constexpr int kLayerCounters = 2 + kLayerRanges;

@@ -3,7 +3,7 @@
 // stream of dot products.  Each warp has an equal share, to the pair of gate and up rows, of all
 // pairs of all routed rows: a lane loads 16 bytes of each 512 of both rows, 128 KB in flight
 // an SM.  For W2 each CTA has a block of out's columns, and its rows (all of them, 172 KB for one
-// token of eight experts of 768) are on their way to shared memory right behind the first of W1's, so that the memory is not idle while the grid waits for the last activation.  Rows
+// token of eight experts of 768) are on their way to shared memory right behind the last of W1's, so that the memory is not idle while the grid waits for the last activation.  Rows
 // that share an expert read its weights again, from the L2.
 //
 // Order: as in layer_experts.cu, ranges of W1 go by tickets, and nobody waits for one that has
@@ -135,7 +135,7 @@ struct UpStream {
             if (lane == 0) p.act[(int64_t)s.row * p.F + s.f] = __float2bfloat16_rn(gate * sigmoid_f(gate) * up);
         }
     }
-    // `then` runs when the first loads have left.
+    // `then` runs when the last loads have left.
     template <class Then>
     __device__ __forceinline__ void run(int lo, const Then &then) {
         pair = lo;
@@ -147,12 +147,13 @@ struct UpStream {
         Step step[kSteps];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) load(step[i]);
-        then();
+        if (pair >= hi) then();
         while (step[0].row >= 0) {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) sum(step[i], d);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) load(step[i]);
+            if (pair >= hi) then();
         }
     }
 };
@@ -264,18 +265,24 @@ __global__ void __launch_bounds__(kThreads, 1) layer_few_kernel(const LayerArgs 
                 if (k8) ex[j] = p.w2x + ((int64_t)expert * blocks8(p.H) + min(lo + c, p.H - 1) / kBlock8) * blocks8(p.F) + lane / 8;
                 advance(c, r);
             }
-            for (int at = lane * 16; at < room.w_stride; at += 512) {
-                int e[4][1];
+            const auto sum_all = [&](const auto &act_of) {
+                for (int at = lane * 16; at < room.w_stride; at += 512) {
+                    int e[4][1];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) e[j][0] = k8 && at < row_bytes ? (int)__ldg(ex[j] + at / 512 * 4) : 127;
+                    for (int j = 0; j < 4; ++j) e[j][0] = k8 && at < row_bytes ? (int)__ldg(ex[j] + at / 512 * 4) : 127;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint4 row[1] = {*reinterpret_cast<const uint4 *>(w[j] + at)};
-                    float sum[1] = {d[j]};
-                    dot16<k8, 1>(row, act[j] + at * (k8 ? 2 : 1), e[j], sum);
-                    d[j] = sum[0];
+                    for (int j = 0; j < 4; ++j) {
+                        const uint4 row[1] = {*reinterpret_cast<const uint4 *>(w[j] + at)};
+                        float sum[1] = {d[j]};
+                        dot16<k8, 1>(row, act_of(j) + at * (k8 ? 2 : 1), e[j], sum);
+                        d[j] = sum[0];
+                    }
                 }
-            }
+            };
+            // (where R divides the warps, a warp's units are all of one routed row, whose values are then
+            // unpacked once)
+            if (kWarps % R == 0) sum_all([&](int) { return act[0]; });
+            else sum_all([&](int j) { return act[j]; });
             // over the lanes: first half of them go on with two units, then a quarter with one
             const bool up16 = lane & 16, up8 = lane & 8;
 #pragma unroll
@@ -316,12 +323,16 @@ FewRoom few_room(const LayerArgs &a, bool eight) {
 
 }  // namespace
 
-// Up to 16 routed rows, and more where all of their weights, shared ones counted again, are less than
-// what the tensor-core kernel loses at its start: @@
+// Up to eight routed rows, and with bf16 weights up to 40 whose rows are at most 80 MB, shared ones
+// counted as often as they are used.  Measured on both sides (us in a graph, both kernels of the
+// layer; this against layer_experts.cu): H = 2048, F = 768, 128 experts: one token of eight experts
+// 26.7 and 32.2, in 8 bits 24.5 and 30.7; two tokens (151 MB) 44.0 and 42.0, 39.6 and 35.3.  R = 35, H
+// = 1008, F = 208 (44 MB) 21.1 and 24.2, in 8 bits 23.7 and 22.5; R = 32, H = 1024, F = 256 (50 MB) 23.0
+// and 27.6, 30.3 and 26.3, F = 512 (101 MB) 31.3 and 30.9; R = 64, H = 512, F = 256 24.1 and 24.0.
 bool layer_few(const LayerArgs &a, bool eight) {
     const int R = a.T * a.k;
-    const int64_t bytes = (int64_t)R * 3 * a.F * a.H * (eight ? 1 : 2);
-    return R <= kLayerFewRows && (R <= 16 || bytes <= (64 << 20)) && few_room(a, eight).slots > 0;
+    const int64_t bytes = (int64_t)R * 3 * a.F * a.H * 2;
+    return (R <= 8 || (!eight && R <= kLayerFewRows && bytes <= 80000000)) && few_room(a, eight).slots > 0;
 }
 
 cudaError_t launch_layer_few(const LayerArgs &a, bool eight, int sms, cudaStream_t s) {

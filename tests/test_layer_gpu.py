@@ -86,7 +86,8 @@ def run(layer, e8, x, wr, w1, w2, k, gate, eight):
 SIZES = [(1, 1, 1, 16, 16), (1, 8, 128, 2048, 768), (2, 2, 8, 272, 48), (3, 3, 5, 128, 16), (7, 5, 40, 1008, 208),
          (8, 8, 8, 512, 64), (9, 4, 33, 144, 272), (16, 2, 128, 256, 128), (33, 6, 24, 528, 80), (48, 8, 128, 512, 96),
          (64, 8, 16, 272, 64), (64, 1, 300, 64, 32), (64, 2, 2, 1040, 144), (5, 32, 40, 160, 32), (4, 3, 1024, 48, 16),
-         (2, 2, 4, 2992, 896), (64, 32, 64, 96, 32)]
+         (2, 2, 4, 2992, 896), (64, 32, 64, 96, 32), (8, 1, 5, 1040, 272), (4, 2, 3, 144, 400), (13, 3, 20, 1024, 128),
+         (40, 1, 9, 512, 64), (41, 1, 9, 512, 64)]
 
 
 @pytest.mark.parametrize("eight", [False, True])
@@ -114,12 +115,13 @@ def test_columns_that_are_not_whole_pieces(ex, layer, e8, H):
 
 @pytest.mark.parametrize("eight,H,F", [(False, 4096, 4096), (True, 8192, 32), (True, 64, 8192), (False, 4088, 16)])
 def test_the_widest_rows(ex, layer, e8, eight, H, F):
-    x, wr, w1, w2 = make(11, 2, 2, H, F, H + F)
-    v1, v2, (out, ids, _) = run(layer, e8, x, wr, w1, w2, 2, 1, eight)
-    ok(ex)
-    want, bound, want_ids, _ = reference(x, wr, v1, v2, 2, True)
-    assert torch.equal(ids.cpu().long(), want_ids)
-    within(out, want, bound)
+    for T in (11, 1):
+        x, wr, w1, w2 = make(T, 2, 2, H, F, H + F)
+        v1, v2, (out, ids, _) = run(layer, e8, x, wr, w1, w2, 2, 1, eight)
+        ok(ex)
+        want, bound, want_ids, _ = reference(x, wr, v1, v2, 2, True)
+        assert torch.equal(ids.cpu().long(), want_ids)
+        within(out, want, bound)
 
 
 @pytest.mark.parametrize("T", [1, 9])
@@ -285,6 +287,41 @@ def test_the_layers_calls_agree(ex, layer, e8):
     # bf16: two roundings of each side.  8-bit weights: a code is off by at most 2^-4 of
     # its value, two projections' worth; the activations' codes come on top
     assert off(out, a) < 4 * BF and off(c, out) < 2 * 2.0 ** -4 and off(b, out) < 4 * 2.0 ** -4
+
+
+@pytest.mark.parametrize("T", [1, 30])
+def test_views_into_larger_tensors(ex, layer, e8, T):
+    """Tokens and weights that begin anywhere on a 16-byte border, and other data around them."""
+    k, E, H, F = 3, 7, 264, 48
+    x, wr, w1, w2 = (t.cuda() for t in make(T, k, E, H, F, 31))
+    want = layer.moe_layer(x, wr, w1, w2, k)
+
+    def shifted(t):
+        big = torch.full((t.numel() + 72,), float("nan"), dtype=t.dtype, device="cuda")
+        big[8:8 + t.numel()] = t.reshape(-1)
+        return big[8:8 + t.numel()].view(t.shape)
+
+    got = layer.moe_layer(shifted(x), shifted(wr), shifted(w1), shifted(w2), k)
+    ok(ex)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_two_layers_share_a_workspace_in_turn(ex, layer, e8):
+    """The C call on one workspace of any content, for a small and then a large call."""
+    from paper_2609_32398_gb300 import doloss as dl
+    L = dl.lib()
+    ws = torch.full((1 << 24,), 255, dtype=torch.uint8, device="cuda")
+    for T, k, E, H, F in ((1, 2, 4, 64, 16), (50, 8, 16, 512, 96), (3, 1, 4, 64, 16)):
+        x, wr, w1, w2 = (t.cuda() for t in make(T, k, E, H, F, 37))
+        want = layer.moe_layer(x, wr, w1, w2, k)
+        out = torch.empty_like(want[0])
+        ids, combine = torch.empty_like(want[1]), torch.empty_like(want[2])
+        assert L.do_moe_layer_workspace_size(T, k, H, F) <= ws.numel()
+        assert 0 == L.do_moe_layer(x.data_ptr(), wr.data_ptr(), w1.data_ptr(), None, w2.data_ptr(), None, T, H, F, E, k, 0,
+                                   out.data_ptr(), ids.data_ptr(), combine.data_ptr(), None, ws.data_ptr(), ws.numel(),
+                                   torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(ids, want[1]) and torch.equal(combine, want[2])
 
 
 def test_empty_call(layer):
