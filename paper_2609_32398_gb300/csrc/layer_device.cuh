@@ -27,6 +27,11 @@ __device__ __forceinline__ unsigned codes_half2(unsigned w) {
 }
 __device__ __forceinline__ unsigned word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// A word's two bf16 values.
+__device__ __forceinline__ f32x2 unpack2(unsigned w) {
+    return pair2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
 __device__ __forceinline__ unsigned load_acquire(const unsigned *p) {
     unsigned v;
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");

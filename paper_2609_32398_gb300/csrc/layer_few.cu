@@ -32,9 +32,6 @@ __device__ __forceinline__ uint4 load_stream(const unsigned char *p, bool in) {
     return v;
 }
 
-__device__ __forceinline__ f32x2 unpack2(unsigned w) {
-    return pair2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-}
 __device__ __forceinline__ f32x2 halves2(unsigned h) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
     return pair2(f.x, f.y);

@@ -13,15 +13,16 @@
 // what is compared, equal ones in favour of the lower expert.
 //
 // Bound by latency: a token's 0.5 MB of Wr (E = 128, H = 2048) come from the L2 in a
-// microsecond; see layer_experts.cu for the whole call.
+// microsecond.  They come by asynchronous copies to shared memory, 4 KB of each row at a time, all
+// on their way together (loads to registers the compiler spread over the sums: @@).
 #include "doloss.h"
 #include "experts_mma.cuh"
-#include "layer.cuh"
+#include "layer_device.cuh"
 
 namespace dol {
 namespace {
 
-constexpr int kCluster = 8;
+constexpr int kCluster = 8, kChunk = 256;
 typedef unsigned long long u64;
 
 // (s, c) += (s2, c2): s exact with its error in c
@@ -134,37 +135,55 @@ layer_route_kernel(const LayerArgs p) {
     const uint4 *x = reinterpret_cast<const uint4 *>(p.x), *wr = reinterpret_cast<const uint4 *>(p.router);
     const uint32_t keys_at = smem_u32(keys);
     const f32x2 minus = pair2(-1.0f, -1.0f);
+    // tokens [kTokens], then each warp's experts, kChunk pieces of 8 columns of them at a time
+    extern __shared__ __align__(16) uint4 rows[];
+    uint4 *mine = rows + (kTokens + warp * kExperts) * kChunk;
     cluster_sync_all();  // every CTA of the cluster has begun: its shared memory may be written
-    for (int e = rank * per + kExperts * warp; e < e1; e += kExperts * kWarps) {
+    for (int first = rank * per; first < e1; first += kExperts * kWarps) {
+        const int e = first + kExperts * warp;
         f32x2 s[kExperts][kTokens], c[kExperts][kTokens];
 #pragma unroll
         for (int i = 0; i < kExperts; ++i)
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) s[i][t] = c[i][t] = pair2(0.0f, 0.0f);
-#pragma unroll(kTokens == 1 ? 8 : 2)
-        for (int at = lane; at < pieces; at += 32) {
-            uint4 wv[kExperts], xv[kTokens];
+        for (int from = 0; from < pieces; from += kChunk) {
+            const int n = min(kChunk, pieces - from);
+            __syncthreads();  // the chunk before has been read
 #pragma unroll
-            for (int i = 0; i < kExperts; ++i) wv[i] = __ldg(wr + (int64_t)min(e + i, e1 - 1) * pieces + at);
+            for (int i = 0; i < kExperts; ++i)
+                if (e + i < e1)
+                    for (int at = lane; at < n; at += 32)
+                        copy16(smem_u32(mine + i * kChunk + at), wr + (int64_t)(e + i) * pieces + from + at, true);
 #pragma unroll
-            for (int t = 0; t < kTokens; ++t) xv[t] = __ldg(x + (int64_t)min(t0 + t, p.T - 1) * pieces + at);
+            for (int t = 0; t < kTokens; ++t)
+                for (int at = threadIdx.x; at < n; at += kThreads)
+                    copy16(smem_u32(rows + t * kChunk + at), x + (int64_t)min(t0 + t, p.T - 1) * pieces + from + at, true);
+            copies_sent();
+            wait_copies<0>();
+            __syncthreads();
+            if (e < e1) {
+#pragma unroll 2
+                for (int at = lane; at < n; at += 32) {
+                    uint4 wv[kExperts], xv[kTokens];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                f32x2 w2[kExperts];
+                    for (int i = 0; i < kExperts; ++i) wv[i] = mine[(e + i < e1 ? i : 0) * kChunk + at];
 #pragma unroll
-                for (int i = 0; i < kExperts; ++i) {
-                    const unsigned w = j == 0 ? wv[i].x : j == 1 ? wv[i].y : j == 2 ? wv[i].z : wv[i].w;
-                    w2[i] = pair2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-                }
+                    for (int t = 0; t < kTokens; ++t) xv[t] = rows[t * kChunk + at];
 #pragma unroll
-                for (int t = 0; t < kTokens; ++t) {
-                    const unsigned w = j == 0 ? xv[t].x : j == 1 ? xv[t].y : j == 2 ? xv[t].z : xv[t].w;
-                    const f32x2 v = pair2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+                    for (int j = 0; j < 4; ++j) {
+                        f32x2 w2[kExperts];
 #pragma unroll
-                    for (int i = 0; i < kExperts; ++i) {
-                        const f32x2 sum = fma2(w2[i], v, s[i][t]);
-                        c[i][t] = add2(c[i][t], fma2(w2[i], v, fma2(sum, minus, s[i][t])));
-                        s[i][t] = sum;
+                        for (int i = 0; i < kExperts; ++i) w2[i] = unpack2(word(wv[i], j));
+#pragma unroll
+                        for (int t = 0; t < kTokens; ++t) {
+                            const f32x2 v = unpack2(word(xv[t], j));
+#pragma unroll
+                            for (int i = 0; i < kExperts; ++i) {
+                                const f32x2 sum = fma2(w2[i], v, s[i][t]);
+                                c[i][t] = add2(c[i][t], fma2(w2[i], v, fma2(sum, minus, s[i][t])));
+                                s[i][t] = sum;
+                            }
+                        }
                     }
                 }
             }
@@ -217,11 +236,20 @@ layer_route_kernel(const LayerArgs p) {
     }
 }
 
+template <int kTokens, int kExperts, int kThreads>
+cudaError_t launch(const LayerArgs &a, cudaStream_t s) {
+    constexpr auto kernel = layer_route_kernel<kTokens, kExperts, kThreads>;
+    constexpr size_t smem = (size_t)(kTokens + kThreads / 32 * kExperts) * kChunk * sizeof(uint4);
+    const cudaError_t e = ensure_smem_limit<kernel>(smem);
+    if (e != cudaSuccess) return e;
+    return launch_after(kernel, dim3((unsigned)(kCluster * ((a.T + kTokens - 1) / kTokens))), kThreads, smem, s, a);
+}
+
 }  // namespace
 
 cudaError_t launch_layer_route(const LayerArgs &a, cudaStream_t s) {
-    if (a.T <= 8) return launch_after(layer_route_kernel<1, 1, 512>, dim3((unsigned)(kCluster * a.T)), 512, 0, s, a);
-    return launch_after(layer_route_kernel<4, 2, 256>, dim3((unsigned)(kCluster * ((a.T + 3) / 4))), 256, 0, s, a);
+    if (a.T <= 8) return launch<1, 1, 512>(a, s);
+    return launch<4, 2, 256>(a, s);
 }
 
 }  // namespace dol
