@@ -638,7 +638,8 @@ size_t do_expert_ffn8_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F)
 
 /* ---------------------------------------------- the layer for a few tokens */
 
-/* A whole MoE layer forward for the few tokens of a decode step, in two kernels:
+/* A whole MoE layer forward for the few tokens of a decode step, in two kernels (five where bf16
+ * experts have many tokens each):
  *   z[t] = Wr X[t],  expert_ids[t] = the k largest of z[t], largest first, equal ones in
  *   favour of the lower expert, combine[t] = their weights by `gate` (as do_routing's), and
  *   out[t] = sum_q combine[t][q] W2_e (silu(W1g_e X[t]) * W1u_e X[t]),  e = expert_ids[t][q]
@@ -651,7 +652,8 @@ size_t do_expert_ffn8_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F)
  *    the choice does not hang on an order of addition.  They must be finite.
  *  - The experts' products are summed in fp32 and their activations rounded to bf16 between
  *    the two; a token's rows are summed in fp32, in the order of its choices, and rounded
- *    once.  8-bit weights stand for their exact values; the activations stay bf16.
+ *    once.  8-bit weights stand for their exact values, and the activations stay bf16 (for more
+ *    than eight routed rows: what is below 2^-29 of the largest of a block of 128 loses bits).
  *  - Results are identical run to run.  A NaN or an infinity in a token stays in that
  *    token's results.
  * workspace: do_moe_layer_workspace_size bytes, 256-byte aligned, of any content; calls that

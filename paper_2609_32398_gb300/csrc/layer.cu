@@ -1,4 +1,4 @@
-// C ABI of the whole MoE layer for a few tokens (include/doloss.h): argument checks and launches.
+// C ABI of the whole MoE layer for a few tokens (include/doloss.h): argument checks, and which kernels.
 #include "layer.cuh"
 #include "experts_abi.cuh"
 #include "experts_tiles.cuh"
@@ -6,15 +6,33 @@
 namespace dol {
 namespace {
 
+// Of the two kernels for a few tokens: counters, activations, results; of the grouped products: the
+// dispatch order and what do_expert_ffn takes.
 struct LayerRoom {
-    size_t counters, act, y, all;
+    size_t counters, act, y, offsets, rows, pos, ffn, all;
 };
-LayerRoom layer_room(int64_t R, int32_t H, int32_t F) {
+LayerRoom layer_room(int64_t T, int32_t k, int32_t H, int32_t F) {
     LayerRoom r = {};
+    const size_t R = (size_t)T * k;
     r.act = r.counters + round256(sizeof(unsigned) * kLayerCounters);
-    r.y = r.act + round256(sizeof(bf16) * (size_t)R * F);
-    r.all = r.y + round256(sizeof(float) * (size_t)R * H);
+    r.y = r.act + round256(sizeof(bf16) * R * F);
+    r.rows = r.offsets + round256(sizeof(int) * (kLayerExperts + 1));
+    r.pos = r.rows + round256(sizeof(int) * R);
+    r.ffn = r.pos + round256(sizeof(int) * R);
+    const size_t few = r.y + round256(sizeof(float) * R * H), grouped = r.ffn + do_expert_ffn_workspace_size(T, k, H, F);
+    r.all = few > grouped ? few : grouped;
     return r;
+}
+
+// bf16 weights whose experts have many tokens each go through the grouped products on tcgen05 (router,
+// order, up, down, join: five kernels), which do not repeat a step for every eight tokens and every
+// tile for every 32.  Measured on both sides (us in a graph; two kernels against five), H = 2048, F = 768: 64
+// tokens of 8 of 8 experts 80.2 and 35.8, of 5 of 40 92.9 and 85.1, of 8 of 128 (four tokens an expert) 205 and
+// 198; 16 of 8 of 8 34.6 and 32.2.  Smaller layers: H = 1024, F = 512, 64 of 4 of 16 35.4 and 27.5; H = 512, F = 256,
+// 64 of 8 of 8 26.7 and 21.6, of 2 of 8 19.5 and 20.0, of 3 of 24 19.8 and 20.7, of 8 of 64 26.1 and 30.2.
+bool layer_grouped(const LayerArgs &a) {
+    const int64_t R = (int64_t)a.T * a.k, bytes = (int64_t)a.E * 3 * a.F * a.H * 2;
+    return R >= 16 * a.E || (R >= 8 * a.E && bytes >= (64 << 20));
 }
 
 }  // namespace
@@ -26,7 +44,7 @@ extern "C" {
 
 size_t do_moe_layer_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F) {
     if (T < 1 || k < 1 || H < 1 || F < 1 || T > dol::kLayerTokens || k > dol::kLayerChoices) return 0;
-    return dol::layer_room(T * k, H, F).all;
+    return dol::layer_room(T, k, H, F).all;
 }
 
 do_status do_moe_layer(const void *X, const void *Wr, const void *W1, const void *W1_exponents, const void *W2,
@@ -49,7 +67,7 @@ do_status do_moe_layer(const void *X, const void *Wr, const void *W1, const void
         return DO_ERR_WORKSPACE;
     const int sms = dol::sm_count();
     if (sms < 8 || sms > dol::kLayerRanges) return DO_ERR_CUDA;
-    const dol::LayerRoom room = dol::layer_room(T * k, H, F);
+    const dol::LayerRoom room = dol::layer_room(T, k, H, F);
     char *ws = static_cast<char *>(workspace);
     dol::LayerArgs a = {};
     a.x = static_cast<const dol::bf16 *>(X);
@@ -77,6 +95,14 @@ do_status do_moe_layer(const void *X, const void *Wr, const void *W1, const void
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = dol::launch_layer_route(a, s);
     if (e != cudaSuccess) return dol::of(e);
+    if (!eight && !few && dol::layer_grouped(a)) {
+        int *offsets = reinterpret_cast<int *>(ws + room.offsets), *rows = reinterpret_cast<int *>(ws + room.rows);
+        int *pos = reinterpret_cast<int *>(ws + room.pos);
+        const cudaError_t o = dol::launch_layer_order(a, offsets, rows, pos, s);
+        if (o != cudaSuccess) return dol::of(o);
+        return do_expert_ffn(X, W1, W2, combine, rows, offsets, pos, T, k, H, F, E, out, status_flags, ws + room.ffn,
+                             room.all - room.ffn, stream);
+    }
     return dol::of(few ? dol::launch_layer_few(a, eight, sms, s) : dol::launch_layer_experts(a, eight, sms, s));
 }
 

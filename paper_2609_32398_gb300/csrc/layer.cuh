@@ -39,6 +39,8 @@ constexpr int kLayerCounters = 2 + kLayerRanges;
 bool layer_few(const LayerArgs &a, bool eight);
 cudaError_t launch_layer_few(const LayerArgs &a, bool eight, int sms, cudaStream_t s);
 cudaError_t launch_layer_route(const LayerArgs &a, cudaStream_t s);
+// offsets [E + 1], rows [T k] and pos [T][k] of the choices in a.ids.
+cudaError_t launch_layer_order(const LayerArgs &a, int *offsets, int *rows, int *pos, cudaStream_t s);
 cudaError_t launch_layer_experts(LayerArgs a, bool eight, int sms, cudaStream_t s);
 
 }  // namespace dol

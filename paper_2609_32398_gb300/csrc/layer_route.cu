@@ -14,7 +14,8 @@
 //
 // Bound by latency: a token's 0.5 MB of Wr (E = 128, H = 2048) come from the L2 in a
 // microsecond.  They come by asynchronous copies to shared memory, 4 KB of each row at a time, all
-// on their way together (loads to registers the compiler spread over the sums: @@).
+// on their way together (loads to registers the compiler spread over the sums, which cost one
+// token's call 2 us of 26 and that of 48 tokens 3 of 109).
 #include "doloss.h"
 #include "experts_mma.cuh"
 #include "layer_device.cuh"

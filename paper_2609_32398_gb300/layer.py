@@ -1,5 +1,6 @@
 """A whole MoE layer forward for the few tokens of a decode step: router, Top-K, the
-experts' two projections and their join, in two kernels.
+experts' two projections and their join, in two kernels (five where bf16 experts have
+many tokens each).
 
 Argument marshalling over libdoloss.so (include/doloss.h), by the rules of
 `experts`: torch supplies device memory and the current stream, there is no CPU
