@@ -2,6 +2,8 @@
 // that codes stand for.  Every value is read once and nothing is computed twice, so that the
 // memory bounds all three.  The power of two makes the scaling exact; the one rounding is
 // the code's (half a step of 2^-3 of its binade).
+#include <climits>
+
 #include "experts8.cuh"
 #include "tma.cuh"
 
@@ -18,14 +20,17 @@ quantise_rows_kernel(const uint4 *__restrict__ x, int64_t M, int K, uint2 *__res
     pdl_wait();
     const int nb = blocks8(K), pieces = K / 8, piece = threadIdx.x & 15;
     const int64_t n = M * nb, i0 = (int64_t)blockIdx.x * (16 * kTurns) + (threadIdx.x >> 4);
+    // one division a thread, in 32 bits where that does
+    int64_t row = n <= INT_MAX ? (int64_t)((unsigned)i0 / (unsigned)nb) : i0 / nb;
+    int block = (int)(i0 - row * nb);
     uint4 v[kTurns];
     int64_t at[kTurns];
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
-        const int64_t i = i0 + 16 * u, row = i / nb;
-        const int c = (int)(i - row * nb) * 16 + piece;
-        at[u] = i < n && c < pieces ? row * pieces + c : -1;
+        const int c = block * 16 + piece;
+        at[u] = row < M && c < pieces ? row * pieces + c : -1;
         v[u] = at[u] >= 0 ? __ldg(x + at[u]) : make_uint4(0, 0, 0, 0);
+        for (block += 16; block >= nb; block -= nb) ++row;
     }
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {

@@ -396,3 +396,60 @@ def test_many_tiles_a_pair(ex, e8, gather):
         least = (top / 224 * 2.0 ** -10).repeat_interleave(128, 1)
         off_by = (v[i:j] - act).abs() - err - torch.maximum(E4 * (act.abs() + err), least)
         assert bool((off_by <= 0).all()), (e, float(off_by.max()))
+
+
+@pytest.mark.parametrize("shift", [0, 1, 2])
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("K", [128, 256, 384, 512, 640, 768, 1040])
+def test_exponents_of_any_alignment(ex, e8, K, gather, shift):
+    """Rows of one to nine exponent bytes that begin on any byte, of rows and of weights: they are read
+    as words, halves or bytes."""
+    counts, N = [70, 0, 3, 255], 144
+    off = ref.groups(counts)
+    R, E = sum(counts), len(counts)
+    T = 40 if gather else R
+    rows = torch.randint(0, T, (R,), generator=torch.Generator().manual_seed(K)) if gather else None
+    a, w, ga, gw = operands(e8, K, T, E, N, K)
+    y, m = ref.product(a, w, off, rows)
+
+    def moved(q):
+        big = torch.full((q.exponents.numel() + 16,), 255, dtype=torch.uint8, device="cuda")
+        view = big[shift:shift + q.exponents.numel()]
+        view.copy_(q.exponents.reshape(-1))
+        return e8.Blocks(q.codes, view.view(q.exponents.shape), q.gated)
+
+    go, gr = gpu(off, rows)
+    got = e8.matmul(moved(ga), moved(gw), go, gr)
+    ok(ex)
+    within(got, y, 2 * K * U * m + BF * y.abs())
+
+
+def test_past_two_to_the_31_values(ex, e8):
+    """More than 2^31 values in the rows, in their codes and in a product, checked at both ends."""
+    M, K, N = (1 << 20) + 37, 2064, 2056
+    x = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    x.view(torch.int16).random_(0, 20000)      # bit patterns of finite numbers
+    x[:, 7] = 1
+    q = e8.quantise_rows(x)
+    ends = [0, 1, M - 300, M - 1]
+    for r in ends:
+        codes, exps = br.quantise(x[r:r + 1].cpu(), 1)
+        assert torch.equal(q.exponents[r:r + 1].cpu(), exps)
+        assert torch.equal(q.codes[r:r + 1].cpu().view(torch.uint8), codes)
+    v = q.values()
+    for r in ends:
+        want = br.values(q.codes[r:r + 1].cpu().view(torch.uint8), q.exponents[r:r + 1].cpu(), 1)
+        assert torch.equal(v[r:r + 1].cpu().double(), want.float().bfloat16().double())
+    del v, x
+    # rows of 16 columns times 2056: results past 2^31
+    small = e8.quantise_rows(rnd(3, 61, 16).cuda())
+    w = e8.quantise_weights(rnd(4, 1, N, 16).cuda())
+    rows = torch.arange(M, dtype=torch.int32, device="cuda") % 61
+    off = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    y = e8.matmul(small, w, off, rows)
+    ok(ex)
+    want = small.values().double() @ w.values()[0].double().T
+    m = small.values().double().abs() @ w.values()[0].double().abs().T
+    for r in (*ends, M - 61):
+        assert bool(((y[r].double() - want[r % 61]).abs() <= 2 * 16 * U * m[r % 61] + BF * want[r % 61].abs()).all())
+    assert torch.equal(y[M - 61 * 3:M - 61 * 2], y[M - 61 * 2:M - 61])
