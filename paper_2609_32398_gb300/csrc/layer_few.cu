@@ -3,8 +3,9 @@
 // stream of dot products.  Each warp has an equal share, to the pair of gate and up rows, of all
 // pairs of all routed rows: a lane loads 16 bytes of each 512 of both rows, 128 KB in flight
 // an SM.  For W2 each CTA has a block of out's columns, and its rows (all of them, 172 KB for one
-// token of eight experts of 768) are on their way to shared memory right behind the last of W1's, so that the memory is not idle while the grid waits for the last activation.  Rows
-// that share an expert read its weights again, from the L2.
+// token of eight experts of 768) are on their way to shared memory right behind the last of W1's, so
+// that the memory is not idle while the grid waits for the last activation.  Rows that share an
+// expert read its weights again, from the L2.
 //
 // Order: as in layer_experts.cu, ranges of W1 go by tickets, and nobody waits for one that has
 // not been taken by a running CTA.  Sums are fp32, lane by lane in order, then over the

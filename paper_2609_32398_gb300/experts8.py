@@ -66,6 +66,9 @@ class Blocks:
 
     def check(self, name: str, dim: int, gated: bool, device: int) -> None:
         c, e = self.codes, self.exponents
+        if c.requires_grad and torch.is_grad_enabled():
+            raise RuntimeError(f"the codes of {name} want a gradient, which the 8-bit experts do not have: call them "
+                               "under torch.no_grad()")
         if (c.dtype is not _E4M3 or e.dtype is not _U8 or c.dim() != dim or device < 0
                 or c.get_device() != device or e.get_device() != device
                 or not (c.is_contiguous() and e.is_contiguous())):

@@ -173,3 +173,26 @@ def test_no_tile_is_empty(name):
             width = (-(-n // tiles) + 15) & ~15
             rows = [min(width, n - j * width) for j in range(tiles)]
             assert width <= cap and min(rows) >= 1 and sum(rows) == n
+
+
+@pytest.mark.parametrize("call", ["values", "matmul", "expert_up", "weights", "gated weights"])
+def test_codes_that_want_a_gradient_are_refused(call):
+    from paper_2609_32398_gb300 import experts8
+
+    def blocks(*size, gated=False, grad=False):
+        exps = [*size[:-2], 2 if gated else size[-2] if len(size) == 2 else 1, 1]
+        codes = torch.zeros(size).to(torch.float8_e4m3fn)
+        return experts8.Blocks(codes.requires_grad_(grad), torch.zeros(exps, dtype=torch.uint8), gated)
+
+    b = blocks(4, 64, grad=True)
+    w = blocks(2, 64, 64, grad=True)
+    g = blocks(2, 128, 64, gated=True, grad=True)
+    run = {"values": b.values,
+           "matmul": lambda: experts8.matmul(b, w),
+           "expert_up": lambda: experts8.expert_up(b, g, torch.zeros(3, dtype=torch.int32)),
+           "weights": lambda: w.check("w2", 3, False, 0),
+           "gated weights": lambda: g.check("w1", 3, True, 0)}[call]
+    with pytest.raises(RuntimeError, match="gradient"):
+        run()
+    with torch.no_grad(), pytest.raises(ValueError):  # on the CPU, which is refused next
+        w.check("w2", 3, False, -1)
