@@ -648,8 +648,10 @@ size_t do_expert_ffn8_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F)
  * neither).  expert_ids and combine [T][k] are written.
  *  - T <= 64, k <= 32, E <= 1024; H and F at most 4096 with bf16 weights and 8192 with codes;
  *    H a multiple of 8 (codes: 16), F of 16.  16-byte aligned matrices.
- *  - The logits are bf16 products summed to more than fp32 (some 2^-40 of the largest), so that
- *    the choice does not hang on an order of addition.  They must be finite.
+ *  - The logits are bf16 products summed with their rounding errors, so that the choice does not
+ *    hang on an order of addition: to 2^-38 (H = 2048) or 2^-34 (H = 8192) of the sum of
+ *    the products' magnitudes at worst, and exactly where that sum is at most 2^48 / (4 ceil(H /
+ *    256) + 6) of a power of two that divides all products.  They must be finite.
  *  - The experts' products are summed in fp32 and their activations rounded to bf16 between
  *    the two; a token's rows are summed in fp32, in the order of its choices, and rounded
  *    once.  8-bit weights stand for their exact values, and the activations stay bf16 (for more

@@ -6,11 +6,16 @@
 // and the logits go through distributed shared memory to the CTA that selects for the token.
 //
 // The order of two experts should not hang on how a sum was split: products of two bf16
-// values are exact in fp32, and their sums are kept as a pair of floats, the running sum
-// and the sum of its rounding errors: with s' = fl(a b + s), the error is a b - (s' - s),
-// exact but for the few steps on which the sum is smaller than the product.  That costs four
-// instructions a product instead of one, two with packed fp32 pairs.  The pairs are
-// what is compared, equal ones in favour of the lower expert.
+// values are exact in fp32, and their sums are kept as a pair of floats, the running sum s
+// and the sum of its rounding errors.  With s' = fl(a b + s) and b' = fl(s' - s), the error is (s -
+// fl(s' - b')) + (a b - b'), exact whichever of s and a b is the larger (Knuth's two-sum; a b -
+// (s' - s) alone, three packed operations cheaper, is off where the product is: experts of the same
+// columns in another order then differed by up to 2^-26 of the largest logit).  That costs seven
+// packed operations for two products.  The pairs are what is compared, equal ones in favour of the lower
+// expert.  With n = 4 ceil(H / 256) + 6 additions on a product's way, U = 2^-24 and A the sum of the
+// products' magnitudes, the errors' sum is at most n U A: what its own roundings lose is at
+// most 2^-38 A (H = 2048) to 2^-34 A (8192), and nothing where all products are multiples of a g
+// >= n A 2^-48.
 //
 // Bound by latency: a token's 0.5 MB of Wr (E = 128, H = 2048) come from the L2 in a
 // microsecond.  They come by asynchronous copies to shared memory, 4 KB of each row at a time, all
@@ -123,7 +128,7 @@ __device__ __forceinline__ void write_choice(const int *chosen, const u64 *top, 
 
 // A warp takes kExperts of the CTA's experts for kTokens tokens at a time.
 template <int kTokens, int kExperts, int kThreads>
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1)
 layer_route_kernel(const LayerArgs p) {
     constexpr int kWarps = kThreads / 32;
     __shared__ u64 keys[kLayerExperts];
@@ -180,8 +185,9 @@ layer_route_kernel(const LayerArgs p) {
                             const f32x2 v = unpack2(word(xv[t], j));
 #pragma unroll
                             for (int i = 0; i < kExperts; ++i) {
-                                const f32x2 sum = fma2(w2[i], v, s[i][t]);
-                                c[i][t] = add2(c[i][t], fma2(w2[i], v, fma2(sum, minus, s[i][t])));
+                                const f32x2 sum = fma2(w2[i], v, s[i][t]), back = fma2(sum, minus, s[i][t]);  // -b'
+                                const f32x2 of_s = fma2(add2(sum, back), minus, s[i][t]), of_ab = fma2(w2[i], v, back);
+                                c[i][t] = add2(c[i][t], add2(of_s, of_ab));
                                 s[i][t] = sum;
                             }
                         }
@@ -250,6 +256,12 @@ cudaError_t launch(const LayerArgs &a, cudaStream_t s) {
 
 cudaError_t launch_layer_route(const LayerArgs &a, cudaStream_t s) {
     if (a.T <= 8) return launch<1, 1, 512>(a, s);
+    // Sixteen warps a CTA hide the sums' latency better than eight with two experts each, but fill an SM,
+    // and sixteen clusters then take turns.  The layer's call in a graph, H = 2048, F = 768, 8 of 128
+    // experts, bf16 and codes (us, 4 x 1 x 512 against 4 x 2 x 256): 12 tokens 114.4 and 74.4 against 119.6 and
+    // 79.6, 48 tokens 193.8 and 123.6 against 198.8 and 128.0, 60 tokens 199.3 and 127.0 against 204.2 and
+    // 131.6, 64 tokens 210.0 and 142.3 against 208.0 and 140.4.
+    if (a.T <= 60) return launch<4, 1, 512>(a, s);
     return launch<4, 2, 256>(a, s);
 }
 
