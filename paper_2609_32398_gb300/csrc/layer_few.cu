@@ -9,7 +9,8 @@
 //
 // Order: as in layer_experts.cu, ranges of W1 go by tickets, and nobody waits for one that has
 // not been taken by a running CTA.  Sums are fp32, lane by lane in order, then over the
-// lanes; the codes of a block of 8-bit weights are summed before its power of two is applied.
+// lanes; sixteen codes of a block of 8-bit weights are summed before most of its power of two is
+// applied (dot16).
 #include <cuda_fp16.h>
 
 #include "layer.cuh"
@@ -33,16 +34,28 @@ __device__ __forceinline__ uint4 load_stream(const unsigned char *p, bool in) {
     return v;
 }
 
-__device__ __forceinline__ f32x2 halves2(unsigned h) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-    return pair2(f.x, f.y);
+// Two fp16 values times the fp16 number c, in fp32: exact.
+__device__ __forceinline__ f32x2 halves2(unsigned h, unsigned short c) {
+    float lo, hi;
+    asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\t"
+        "fma.rn.f32.f16 %0, l, %3, %4;\n\tfma.rn.f32.f16 %1, u, %3, %4;\n\t}"
+        : "=f"(lo), "=f"(hi)
+        : "r"(h), "h"(c), "f"(0.0f));
+    return pair2(lo, hi);
 }
 // kRows weight rows' 16 bytes (8 values, or 16 codes of one block) with the values at x; sums +=.
+// Codes of ordinary weights are some 2^12 times the weights: up to 2^-14 of a block's power of two goes
+// to each code, on its way from fp16 to fp32, where it costs nothing, and the rest to the sum, so that
+// neither a product nor a sum of sixteen leaves fp32's range at either end where the result does not.
 template <bool k8, int kRows>
 __device__ __forceinline__ void dot16(const uint4 (&w)[kRows], const unsigned char *x, const int (&e)[kRows], float (&sum)[kRows]) {
     f32x2 s[kRows];
+    unsigned short first[kRows];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) s[i] = pair2(0.0f, 0.0f);
+    for (int i = 0; i < kRows; ++i) {
+        s[i] = pair2(0.0f, 0.0f);
+        first[i] = (unsigned short)((k8 ? min(max(e[i] - 112, 1), 15) : 0) << 10);  // an fp16 power of two, 2^-14 to 1
+    }
 #pragma unroll
     for (int h = 0; h < (k8 ? 2 : 1); ++h) {
         const uint4 v = *reinterpret_cast<const uint4 *>(x + 16 * h);
@@ -52,7 +65,7 @@ __device__ __forceinline__ void dot16(const uint4 (&w)[kRows], const unsigned ch
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 const unsigned c = word(w[i], k8 ? 2 * h + j / 2 : j);
-                const f32x2 wv = k8 ? halves2(j & 1 ? codes_half2<1>(c) : codes_half2<0>(c)) : unpack2(c);
+                const f32x2 wv = k8 ? halves2(j & 1 ? codes_half2<1>(c) : codes_half2<0>(c), first[i]) : unpack2(c);
                 s[i] = fma2(wv, xv, s[i]);
             }
         }
@@ -61,7 +74,8 @@ __device__ __forceinline__ void dot16(const uint4 (&w)[kRows], const unsigned ch
     for (int i = 0; i < kRows; ++i) {
         float a, b;
         split2(s[i], a, b);
-        sum[i] = k8 ? fmaf(a + b, e8_scale(e[i]), sum[i]) : sum[i] + (a + b);
+        const int rest = k8 ? max(e[i], min(e[i] + 14, 127)) : 0;
+        sum[i] = k8 ? fmaf(a + b, __uint_as_float(rest == 255 ? 0x7fc00000u : (unsigned)rest << 23), sum[i]) : sum[i] + (a + b);
     }
 }
 
