@@ -651,13 +651,14 @@ size_t do_expert_ffn8_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F)
  *  - The logits are bf16 products summed with their rounding errors, so that the choice does not
  *    hang on an order of addition: to 2^-38 (H = 2048) or 2^-34 (H = 8192) of the sum of
  *    the products' magnitudes at worst, and exactly where that sum is at most 2^48 / (4 ceil(H /
- *    256) + 6) of a power of two that divides all products.  They must be finite.
+ *    256) + 6) of a power of two that divides all products.  They must be finite: otherwise the
+ *    token has k different experts of [0, E) still, but weights and results that are NaN.
  *  - The experts' products are summed in fp32 and their activations rounded to bf16 between
  *    the two; a token's rows are summed in fp32, in the order of its choices, and rounded
  *    once.  8-bit weights stand for their exact values, and the activations stay bf16 (for more
  *    than eight routed rows: what is below 2^-29 of the largest of a block of 128 loses bits).
- *  - Results are identical run to run.  A NaN or an infinity in a token stays in that
- *    token's results.
+ *  - Results are identical run to run.  A NaN or an infinity in a token, or in what its products
+ *    come to, stays in that token's results.
  * workspace: do_moe_layer_workspace_size bytes, 256-byte aligned, of any content; calls that
  * may run at the same time need one each.  Asynchronous on `stream`. */
 do_status do_moe_layer(const void *X, const void *Wr, const void *W1, const void *W1_exponents,

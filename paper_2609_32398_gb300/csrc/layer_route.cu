@@ -39,10 +39,11 @@ __device__ __forceinline__ void add_pair(float &s, float &c, float s2, float c2)
 }
 
 // Larger for a larger value, never 0: the value rounded to fp32, then what that leaves (both zeros
-// are one value; fp64 would order the same and takes 60 cycles an instruction).
+// are one value; fp64 would order the same and takes 60 cycles an instruction).  NaNs are one value above
+// all others, whatever their bits, so that a token that holds one still has k different experts.
 __device__ __forceinline__ unsigned order_of(float v) {
     const unsigned b = __float_as_uint(v + 0.0f);
-    return (b >> 31) ? ~b : b | 0x80000000u;
+    return v != v ? 0xffffffffu : (b >> 31) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(unsigned o) { return __uint_as_float((o >> 31) ? o ^ 0x80000000u : ~o); }
 __device__ __forceinline__ u64 order_key(float s, float c) {

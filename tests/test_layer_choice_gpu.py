@@ -9,7 +9,7 @@ integers.  The inputs here are made so, and every test checks that they are."""
 import pytest
 import torch
 
-from test_experts_gpu import U, ok
+from test_experts_gpu import U, ok, rnd
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,31 @@ def test_differences_of_two_pow_minus_38(ex, layer, T):
     z = whole(x, wr, 2.0 ** -37)
     assert bool((z[:, 1::2] != z[:, ::2]).all())
     assert torch.equal(chosen(ex, layer, x, wr, E), first(z, E))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("T,k,E", [(1, 4, 6), (7, 4, 256), (7, 32, 257), (20, 8, 40), (20, 5, 1000), (64, 2, 300)])
+@pytest.mark.parametrize("eight", [False, True])
+def test_a_token_that_is_not_finite(ex, layer, T, k, E, bad, eight):
+    """Its experts are k different ones all the same, its weights and results are NaN, and every
+    other token's stay as they were, to the bit."""
+    from paper_2609_32398_gb300 import experts8 as e8
+
+    H, hit = 272, [T // 2, T - 1]
+    x, wr = rnd(T, T, H).cuda(), rnd(E, E, H, scale=H ** -0.5).cuda()
+    w1, w2 = rnd(1, E, 2 * F, H, scale=H ** -0.5).cuda(), rnd(2, E, H, F, scale=F ** -0.5).cuda()
+    if eight:
+        w1, w2 = e8.quantise_weights(w1, True), e8.quantise_weights(w2)
+    broken = x.clone()
+    broken[hit, [5, 200][:len(hit)]] = bad
+    good = torch.ones(T, dtype=torch.bool)
+    good[hit] = False
+    for gate in (0, 1):
+        want = layer.moe_layer(x, wr, w1, w2, k, gate)
+        out, ids, combine = layer.moe_layer(broken, wr, w1, w2, k, gate)
+        ok(ex)
+        for a, b in zip((out, ids, combine), want):
+            assert torch.equal(a[good.cuda()], b[good.cuda()])
+        chosen = ids.cpu().sort(1)[0]
+        assert bool((chosen >= 0).all()) and bool((chosen < E).all()) and bool((chosen.diff(dim=1) > 0).all())
+        assert bool(torch.isnan(combine[~good.cuda()]).all()) and bool(torch.isnan(out[~good.cuda()]).all())
