@@ -244,25 +244,30 @@ layer_route_kernel(const LayerArgs p) {
     }
 }
 
+// While all clusters fit that way, a CTA asks for more than half of an SM's shared memory and has it to
+// itself: with room for two, a cluster's eight share four SMs.  The layer's call in a graph, H = 2048, F =
+// 768, 8 of 128 experts, bf16 and codes (us, alone against shared): 12 tokens 114.4 and 74.4 against 119.6
+// and 79.6, 48 tokens 193.8 and 123.6 against 198.8 and 128.0, 60 tokens 199.3 and 127.0 against 204.2
+// and 131.6; 64 tokens, whose sixteenth cluster then waits for another's end, 210.0 and 142.3 against 208.0
+// and 140.4.
+constexpr unsigned kAloneClusters = 15;
+constexpr size_t kAlone = 116 * 1024;
+
 template <int kTokens, int kExperts, int kThreads>
 cudaError_t launch(const LayerArgs &a, cudaStream_t s) {
     constexpr auto kernel = layer_route_kernel<kTokens, kExperts, kThreads>;
-    constexpr size_t smem = (size_t)(kTokens + kThreads / 32 * kExperts) * kChunk * sizeof(uint4);
-    const cudaError_t e = ensure_smem_limit<kernel>(smem);
+    constexpr size_t rows = (size_t)(kTokens + kThreads / 32 * kExperts) * kChunk * sizeof(uint4);
+    static_assert(rows <= kAlone, "");
+    const cudaError_t e = ensure_smem_limit<kernel>(kAlone);
     if (e != cudaSuccess) return e;
-    return launch_after(kernel, dim3((unsigned)(kCluster * ((a.T + kTokens - 1) / kTokens))), kThreads, smem, s, a);
+    const unsigned clusters = (unsigned)(a.T + kTokens - 1) / kTokens;
+    return launch_after(kernel, dim3(kCluster * clusters), kThreads, clusters <= kAloneClusters ? kAlone : rows, s, a);
 }
 
 }  // namespace
 
 cudaError_t launch_layer_route(const LayerArgs &a, cudaStream_t s) {
     if (a.T <= 8) return launch<1, 1, 512>(a, s);
-    // Sixteen warps a CTA hide the sums' latency better than eight with two experts each, but fill an SM,
-    // and sixteen clusters then take turns.  The layer's call in a graph, H = 2048, F = 768, 8 of 128
-    // experts, bf16 and codes (us, 4 x 1 x 512 against 4 x 2 x 256): 12 tokens 114.4 and 74.4 against 119.6 and
-    // 79.6, 48 tokens 193.8 and 123.6 against 198.8 and 128.0, 60 tokens 199.3 and 127.0 against 204.2 and
-    // 131.6, 64 tokens 210.0 and 142.3 against 208.0 and 140.4.
-    if (a.T <= 60) return launch<4, 1, 512>(a, s);
     return launch<4, 2, 256>(a, s);
 }
 
