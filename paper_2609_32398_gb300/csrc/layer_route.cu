@@ -1,7 +1,7 @@
 // The router of a few tokens: logits z = x Wr^T, the k largest of each token and its
 // combine weights, in one kernel.
 //
-// A cluster of eight CTAs has one token (or four, where there are more than eight tokens: Wr
+// A cluster of eight CTAs has one token (or four or five, where there are more than eight tokens: Wr
 // is then read from the L2 a quarter as often); each CTA takes an eighth of the experts,
 // and the logits go through distributed shared memory to the CTA that selects for the token.
 //
@@ -28,7 +28,7 @@
 namespace dol {
 namespace {
 
-constexpr int kCluster = 8, kChunk = 256;
+constexpr int kCluster = 8, kChunk = 256, kThreads = 512, kWarps = kThreads / 32;
 typedef unsigned long long u64;
 
 // (s, c) += (s2, c2): s exact with its error in c
@@ -58,12 +58,11 @@ __device__ __forceinline__ void store_remote(uint32_t addr, u64 v) {
 // The k largest keys of one token, by the whole CTA: chosen[q] and top[q]; keys are in its shared
 // memory.  Up to 256 experts each key counts the ones before it, a few threads a key (k rounds of
 // a maximum over a warp took 2.4 us for k = 8); with more a warp takes the rounds.
-template <int kThreads>
 __device__ __forceinline__ void select(u64 *keys, int E, int k, int *chosen, u64 *top) {
     const int lane = threadIdx.x & 31;
     if (E <= 256) {
         // threads a key: as many as there are
-        const int shift = (E <= 32 ? 3 : E <= 64 ? 2 : E <= 128 ? 1 : 0) + (kThreads > 256 ? 1 : 0), share = 1 << shift;
+        const int shift = E <= 32 ? 4 : E <= 64 ? 3 : E <= 128 ? 2 : 1, share = 1 << shift;
         for (int base = 0; base < E << shift; base += kThreads) {
             const int i = base + (int)threadIdx.x, e = i >> shift, from = i & (share - 1);
             const u64 mine = e < E ? keys[e] : 0;
@@ -127,11 +126,10 @@ __device__ __forceinline__ void write_choice(const int *chosen, const u64 *top, 
     }
 }
 
-// A warp takes kExperts of the CTA's experts for kTokens tokens at a time.
-template <int kTokens, int kExperts, int kThreads>
+// A warp takes one of the CTA's experts for kTokens tokens at a time.
+template <int kTokens>
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1)
 layer_route_kernel(const LayerArgs p) {
-    constexpr int kWarps = kThreads / 32;
     __shared__ u64 keys[kLayerExperts];
     pdl_wait();
     pdl_trigger();  // the experts' CTAs come up meanwhile, read the tokens and wait for this kernel's end
@@ -142,25 +140,20 @@ layer_route_kernel(const LayerArgs p) {
     const uint4 *x = reinterpret_cast<const uint4 *>(p.x), *wr = reinterpret_cast<const uint4 *>(p.router);
     const uint32_t keys_at = smem_u32(keys);
     const f32x2 minus = pair2(-1.0f, -1.0f);
-    // tokens [kTokens], then each warp's experts, kChunk pieces of 8 columns of them at a time
+    // tokens [kTokens], then each warp's expert, kChunk pieces of 8 columns of them at a time
     extern __shared__ __align__(16) uint4 rows[];
-    uint4 *mine = rows + (kTokens + warp * kExperts) * kChunk;
+    uint4 *mine = rows + (kTokens + warp) * kChunk;
     cluster_sync_all();  // every CTA of the cluster has begun: its shared memory may be written
-    for (int first = rank * per; first < e1; first += kExperts * kWarps) {
-        const int e = first + kExperts * warp;
-        f32x2 s[kExperts][kTokens], c[kExperts][kTokens];
+    for (int first = rank * per; first < e1; first += kWarps) {
+        const int e = first + warp;
+        f32x2 s[kTokens], c[kTokens];
 #pragma unroll
-        for (int i = 0; i < kExperts; ++i)
-#pragma unroll
-            for (int t = 0; t < kTokens; ++t) s[i][t] = c[i][t] = pair2(0.0f, 0.0f);
+        for (int t = 0; t < kTokens; ++t) s[t] = c[t] = pair2(0.0f, 0.0f);
         for (int from = 0; from < pieces; from += kChunk) {
             const int n = min(kChunk, pieces - from);
             __syncthreads();  // the chunk before has been read
-#pragma unroll
-            for (int i = 0; i < kExperts; ++i)
-                if (e + i < e1)
-                    for (int at = lane; at < n; at += 32)
-                        copy16(smem_u32(mine + i * kChunk + at), wr + (int64_t)(e + i) * pieces + from + at, true);
+            if (e < e1)
+                for (int at = lane; at < n; at += 32) copy16(smem_u32(mine + at), wr + (int64_t)e * pieces + from + at, true);
 #pragma unroll
             for (int t = 0; t < kTokens; ++t)
                 for (int at = threadIdx.x; at < n; at += kThreads)
@@ -171,26 +164,20 @@ layer_route_kernel(const LayerArgs p) {
             if (e < e1) {
 #pragma unroll 2
                 for (int at = lane; at < n; at += 32) {
-                    uint4 wv[kExperts], xv[kTokens];
-#pragma unroll
-                    for (int i = 0; i < kExperts; ++i) wv[i] = mine[(e + i < e1 ? i : 0) * kChunk + at];
+                    const uint4 wv = mine[at];
+                    uint4 xv[kTokens];
 #pragma unroll
                     for (int t = 0; t < kTokens; ++t) xv[t] = rows[t * kChunk + at];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        f32x2 w2[kExperts];
-#pragma unroll
-                        for (int i = 0; i < kExperts; ++i) w2[i] = unpack2(word(wv[i], j));
+                        const f32x2 w2 = unpack2(word(wv, j));
 #pragma unroll
                         for (int t = 0; t < kTokens; ++t) {
                             const f32x2 v = unpack2(word(xv[t], j));
-#pragma unroll
-                            for (int i = 0; i < kExperts; ++i) {
-                                const f32x2 sum = fma2(w2[i], v, s[i][t]), back = fma2(sum, minus, s[i][t]);  // -b'
-                                const f32x2 of_s = fma2(add2(sum, back), minus, s[i][t]), of_ab = fma2(w2[i], v, back);
-                                c[i][t] = add2(c[i][t], add2(of_s, of_ab));
-                                s[i][t] = sum;
-                            }
+                            const f32x2 sum = fma2(w2, v, s[t]), back = fma2(sum, minus, s[t]);  // -b'
+                            const f32x2 of_s = fma2(add2(sum, back), minus, s[t]), of_ab = fma2(w2, v, back);
+                            c[t] = add2(c[t], add2(of_s, of_ab));
+                            s[t] = sum;
                         }
                     }
                 }
@@ -198,22 +185,21 @@ layer_route_kernel(const LayerArgs p) {
         }
         // over the two halves and the lanes: while there are several values, half of the lanes
         // go on with half of them
-        constexpr int kValues = kExperts * kTokens;
-        float vs[kValues], vc[kValues];
+        constexpr int kValues = kTokens == 1 ? 1 : kTokens <= 4 ? 4 : 8;  // zeros past kTokens
+        static_assert(kTokens <= kCluster, "");
+        float vs[kValues] = {}, vc[kValues] = {};
 #pragma unroll
-        for (int i = 0; i < kExperts; ++i)
-#pragma unroll
-            for (int t = 0; t < kTokens; ++t) {
-                float s_hi, c_hi, &lo = vs[i * kTokens + t], &err = vc[i * kTokens + t];
-                split2(s[i][t], lo, s_hi);
-                split2(c[i][t], err, c_hi);
-                add_pair(lo, err, s_hi, c_hi);
-            }
-        int value = 0, o = 16;
+        for (int t = 0; t < kTokens; ++t) {
+            float s_hi, c_hi;
+            split2(s[t], vs[t], s_hi);
+            split2(c[t], vc[t], c_hi);
+            add_pair(vs[t], vc[t], s_hi, c_hi);
+        }
+        int token = 0, o = 16;
 #pragma unroll
         for (int n = kValues / 2; n >= 1; n >>= 1, o >>= 1) {
             const bool up = lane & o;
-            value += up ? n : 0;
+            token += up ? n : 0;
 #pragma unroll
             for (int i = 0; i < n; ++i) {
                 const float other_s = __shfl_xor_sync(kFull, up ? vs[i] : vs[i + n], o);
@@ -228,10 +214,9 @@ layer_route_kernel(const LayerArgs p) {
             const float other_s = __shfl_xor_sync(kFull, vs[0], o), other_c = __shfl_xor_sync(kFull, vc[0], o);
             add_pair(vs[0], vc[0], other_s, other_c);
         }
-        const int expert = e + value / kTokens, token = value % kTokens;
-        if ((lane & whole) == 0 && expert < e1) {
+        if ((lane & whole) == 0 && token < kTokens && e < e1) {
             uint32_t to;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(keys_at + 8u * (uint32_t)expert), "r"(token));
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(keys_at + 8u * (uint32_t)e), "r"(token));
             store_remote(to, order_key(vs[0], vc[0]));
         }
     }
@@ -239,36 +224,31 @@ layer_route_kernel(const LayerArgs p) {
     if (rank < kTokens && t0 + rank < p.T) {
         __shared__ int chosen[kLayerChoices];
         __shared__ u64 top[kLayerChoices];
-        select<kThreads>(keys, p.E, p.k, chosen, top);
+        select(keys, p.E, p.k, chosen, top);
         if (warp == 0) write_choice(chosen, top, p, t0 + rank, lane);
     }
 }
 
-// While all clusters fit that way, a CTA asks for more than half of an SM's shared memory and has it to
-// itself: with room for two, a cluster's eight share four SMs.  The layer's call in a graph, H = 2048, F =
-// 768, 8 of 128 experts, bf16 and codes (us, alone against shared): 12 tokens 114.4 and 74.4 against 119.6
-// and 79.6, 48 tokens 193.8 and 123.6 against 198.8 and 128.0, 60 tokens 199.3 and 127.0 against 204.2
-// and 131.6; 64 tokens, whose sixteenth cluster then waits for another's end, 210.0 and 142.3 against 208.0
-// and 140.4.
-constexpr unsigned kAloneClusters = 15;
+// A CTA asks for more than half of an SM's shared memory and has it to itself: with room for two, a
+// cluster's eight share four SMs.  Fifteen clusters fit that way, so that more than 60 tokens go by fives.
+// The layer's call in a graph, H = 2048, F = 768, 8 of 128 experts, bf16 (us): CTAs alone against two to an
+// SM, 8 tokens 87.6 and 89.9, 48 tokens 193.8 and 198.8; 64 tokens by fives 204.1, by fours alone, whose
+// sixteenth cluster waits for another's end, 210.0, by fours two to an SM 207.6.
 constexpr size_t kAlone = 116 * 1024;
 
-template <int kTokens, int kExperts, int kThreads>
+template <int kTokens>
 cudaError_t launch(const LayerArgs &a, cudaStream_t s) {
-    constexpr auto kernel = layer_route_kernel<kTokens, kExperts, kThreads>;
-    constexpr size_t rows = (size_t)(kTokens + kThreads / 32 * kExperts) * kChunk * sizeof(uint4);
-    static_assert(rows <= kAlone, "");
+    constexpr auto kernel = layer_route_kernel<kTokens>;
+    static_assert((kTokens + kWarps) * kChunk * sizeof(uint4) <= kAlone, "");
     const cudaError_t e = ensure_smem_limit<kernel>(kAlone);
     if (e != cudaSuccess) return e;
-    const unsigned clusters = (unsigned)(a.T + kTokens - 1) / kTokens;
-    return launch_after(kernel, dim3(kCluster * clusters), kThreads, clusters <= kAloneClusters ? kAlone : rows, s, a);
+    return launch_after(kernel, dim3((unsigned)(kCluster * ((a.T + kTokens - 1) / kTokens))), kThreads, kAlone, s, a);
 }
 
 }  // namespace
 
 cudaError_t launch_layer_route(const LayerArgs &a, cudaStream_t s) {
-    if (a.T <= 8) return launch<1, 1, 512>(a, s);
-    return launch<4, 2, 256>(a, s);
+    return a.T <= 8 ? launch<1>(a, s) : a.T <= 60 ? launch<4>(a, s) : launch<5>(a, s);
 }
 
 }  // namespace dol

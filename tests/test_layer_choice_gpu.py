@@ -66,7 +66,7 @@ def test_products_larger_than_the_sum_so_far(ex, layer, T):
     assert torch.equal(first(whole(x, wr, 2.0 ** -25), E), torch.tensor([3, 1, 0, 2]).expand(T, E))
 
 
-@pytest.mark.parametrize("T", [1, 8, 9, 64])
+@pytest.mark.parametrize("T", [1, 8, 9, 61, 64])
 @pytest.mark.parametrize("H,E", [(64, 33), (264, 8), (1000, 40), (2048, 128), (4096, 300)])
 def test_rows_of_the_same_columns_in_any_order(ex, layer, T, H, E):
     """Experts whose rows are one row's columns in other orders, half of them with a column moved by a
