@@ -653,10 +653,13 @@ size_t do_expert_ffn8_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F)
  *    the products' magnitudes at worst, and exactly where that sum is at most 2^48 / (4 ceil(H /
  *    256) + 6) of a power of two that divides all products.  They must be finite: otherwise the
  *    token has k different experts of [0, E) still, but weights and results that are NaN.
- *  - The experts' products are summed in fp32 and their activations rounded to bf16 between
- *    the two; a token's rows are summed in fp32, in the order of its choices, and rounded
- *    once.  8-bit weights stand for their exact values, and the activations stay bf16 (for more
- *    than eight routed rows: what is below 2^-29 of the largest of a block of 128 loses bits).
+ *  - The experts' products are summed in fp32; a token's rows are summed in fp32, in the order
+ *    of its choices, and rounded once.  With bf16 weights the activations are rounded to bf16
+ *    between the two products, as do_expert_up's are (the result's error: 2.3e-3 of its norm,
+ *    1.7e-3 without).  8-bit weights stand for their exact values; with them the activations
+ *    stay fp32 for up to eight routed rows that fit an SM's shared memory, and are held in
+ *    11 bits otherwise, as the tokens then are, below the power of two of a block of 128's
+ *    largest (what is below 2^-29 of that loses bits).
  *  - Results are identical run to run.  A NaN or an infinity in a token, or in what its products
  *    come to, stays in that token's results.
  * workspace: do_moe_layer_workspace_size bytes, 256-byte aligned, of any content; calls that

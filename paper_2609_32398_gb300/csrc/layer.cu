@@ -15,7 +15,7 @@ LayerRoom layer_room(int64_t T, int32_t k, int32_t H, int32_t F) {
     LayerRoom r = {};
     const size_t R = (size_t)T * k;
     r.act = r.counters + round256(sizeof(unsigned) * kLayerCounters);
-    r.y = r.act + round256(sizeof(bf16) * R * F);
+    r.y = r.act + round256(sizeof(float) * R * F);
     r.rows = r.offsets + round256(sizeof(int) * (kLayerExperts + 1));
     r.pos = r.rows + round256(sizeof(int) * R);
     r.ffn = r.pos + round256(sizeof(int) * R);
@@ -86,7 +86,7 @@ do_status do_moe_layer(const void *X, const void *Wr, const void *W1, const void
     a.ids = expert_ids;
     a.combine = combine;
     a.counters = reinterpret_cast<unsigned *>(ws + room.counters);
-    a.act = reinterpret_cast<dol::bf16 *>(ws + room.act);
+    a.act = ws + room.act;
     a.y = reinterpret_cast<float *>(ws + room.y);
     a.status = status_flags;
     a.ranges = sms;

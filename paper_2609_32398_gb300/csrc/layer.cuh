@@ -21,7 +21,7 @@ struct LayerArgs {
     bf16 *out;             // [T][H]
     int *ids;              // [T][k]
     float *combine;        // [T][k]
-    bf16 *act;             // [T k][F]
+    void *act;             // [T k][F]: bf16, or fp32 with codes
     float *y;              // [T k][H]
     unsigned *counters;    // kLayerCounters: tickets, ranges done, and one for each range
     int *status;

@@ -4,8 +4,9 @@ import pytest
 import torch
 
 import blocks_ref as br
+import experts_ref as ref
 from test_experts8_gpu import blocks
-from test_experts_gpu import ok
+from test_experts_gpu import BF, FN, U, ok
 from test_layer_gpu import e8, ex, layer, make, reference, run, within  # noqa: F401  (fixtures)
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +42,32 @@ def test_exponents_of_any_size(ex, layer, e8, d, T, k, E, H, F):  # noqa: F811
     want, bound, want_ids, _ = reference(x, wr, v1 * 2.0 ** d, v2 * 2.0 ** d, k, True)
     assert torch.equal(ids.cpu().long(), want_ids)
     within(out, want, bound)
+
+
+@pytest.mark.parametrize("T,grain", [(1, 0.0), (8, 0.0), (9, 2.0 ** -11), (40, 2.0 ** -11)])
+def test_activations_between_products_with_codes(ex, layer, e8, T, grain):  # noqa: F811
+    """Results that are the differences of two activations a few hundredths apart, so that what the
+    activations lose between the projections shows: nothing of their fp32 for up to eight routed rows, a
+    rounding to 11 bits for more (and bits below 2^-39 of the largest)."""
+    E, H, F = 3, 272, 144
+    x, wr, w1, w2 = make(T, 1, E, H, F, 41)
+    x[:, 0] = 1
+    for rows in (slice(0, F), slice(F, 2 * F)):
+        w1[:, rows][:, 1::2] = w1[:, rows][:, ::2]
+    w1[:, F + 1::2, 0] += 2.0 ** -6
+    w2[:] = 0
+    for h in range(F // 2):
+        w2[:, h, 2 * h], w2[:, h, 2 * h + 1] = 1, -1
+    v1, _, (out, ids, combine) = run(layer, e8, x, wr, w1, w2, 1, 1, True)
+    ok(ex)
+    assert bool((combine == 1).all())
+    e = ids.cpu().long()[:, 0]
+    xd, v = x.double(), v1.double()[e]                        # [T, 2F, H]
+    z, m = torch.einsum("tfh,th->tf", v, xd), torch.einsum("tfh,th->tf", v.abs(), xd.abs())
+    act, d = ref.swiglu(z), 2 * H * U * m
+    g, u, dg, du = z[:, :F].abs(), z[:, F:].abs(), d[:, :F], d[:, F:]
+    err = 1.1 * dg * u + g * du + 2 * dg * du + (grain + FN + 2 * U) * act.abs() + 2.0 ** -39 * act.abs().amax(1, True)
+    want, room = act[:, ::2] - act[:, 1::2], err[:, ::2] + err[:, 1::2]
+    assert float((want.abs() / act[:, ::2].abs()).median()) < 0.1
+    within(out[:, :F // 2], want, room + BF * want.abs())
+    assert not bool(out[:, F // 2:].any())
