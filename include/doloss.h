@@ -657,9 +657,9 @@ size_t do_expert_ffn8_workspace_size(int64_t T, int32_t k, int32_t H, int32_t F)
  *    of its choices, and rounded once.  With bf16 weights the activations are rounded to bf16
  *    between the two products, as do_expert_up's are (the result's error: 2.3e-3 of its norm,
  *    1.7e-3 without).  8-bit weights stand for their exact values; with them the activations
- *    stay fp32 for up to eight routed rows that fit an SM's shared memory, and are held in
- *    11 bits otherwise, as the tokens then are, below the power of two of a block of 128's
- *    largest (what is below 2^-29 of that loses bits).
+ *    stay fp32 in the smallest calls (up to eight routed rows of layers that are not large), and
+ *    are held in 11 bits otherwise, as the tokens then are, below the power of two of a block of
+ *    128's largest (what is below 2^-29 of that loses bits).
  *  - Results are identical run to run.  A NaN or an infinity in a token, or in what its products
  *    come to, stays in that token's results.
  * workspace: do_moe_layer_workspace_size bytes, 256-byte aligned, of any content; calls that

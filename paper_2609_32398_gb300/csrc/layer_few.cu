@@ -363,16 +363,22 @@ FewRoom few_room(const LayerArgs &a, bool eight) {
 
 }  // namespace
 
-// Up to eight routed rows, and with bf16 weights up to 40 whose rows are at most 80 MB, shared ones
-// counted as often as they are used.  Measured on both sides (us in a graph, both kernels of the
-// layer; this against layer_experts.cu): H = 2048, F = 768, 128 experts: one token of eight experts
-// 26.7 and 32.2, in 8 bits 24.5 and 30.7; two tokens (151 MB) 44.0 and 42.0, 39.6 and 35.3.  R = 35, H
+// Up to four routed rows whose weights would be at most 180 MB in bf16, up to eight of 110 MB, and with
+// bf16 weights up to 40 of 80 MB, shared ones counted as often as they are used.  Measured on both sides
+// (us in a graph, both kernels of the layer; this against layer_experts.cu).  Eight rows, one token or
+// eight, bf16 and codes: H = 2048, F = 768 (75 MB) 23.8 and 28.7, 23.8 and 26.9, all of one expert 17.8 and
+// 20.8, 19.8 and 22.5; F = 1024 (101 MB) 31.8 and 31.4, 25.8 and 28.6; F = 1280 (126 MB) 34.0 and 32.3, 31.7
+// and 28.3; H = 4096, F = 1536 (302 MB) 68.2 and 60.3, 54.5 and 42.7, of one expert 61.6 and 35.6, 63.2 and 33.2.
+// Four: H = 4096, F = 1536 (151 MB) 38.6 and 41.0, 31.8 and 36.1; F = 2048 (201 MB) 49.0 and 47.1, 41.2 and 39.6;
+// two with F = 3584 (176 MB) 48.4 and 48.4, 37.0 and 40.2.  More: two tokens of eight experts, H = 2048, F =
+// 768 (151 MB), 44.0 and 42.0, 39.6 and 35.3.  R = 35, H
 // = 1008, F = 208 (44 MB) 21.1 and 24.2, in 8 bits 23.7 and 22.5; R = 32, H = 1024, F = 256 (50 MB) 23.0
 // and 27.6, 30.3 and 26.3, F = 512 (101 MB) 31.3 and 30.9; R = 64, H = 512, F = 256 24.1 and 24.0.
 bool layer_few(const LayerArgs &a, bool eight) {
     const int R = a.T * a.k;
     const int64_t bytes = (int64_t)R * 3 * a.F * a.H * 2;
-    return (R <= 8 || (!eight && R <= kLayerFewRows && bytes <= 80000000)) && few_room(a, eight).slots > 0;
+    if (bytes > (R <= 4 ? 180000000 : R <= 8 ? 110000000 : 80000000)) return false;
+    return R <= (eight ? 8 : kLayerFewRows) && few_room(a, eight).slots > 0;
 }
 
 cudaError_t launch_layer_few(const LayerArgs &a, bool eight, int sms, cudaStream_t s) {
