@@ -8,7 +8,7 @@
 // are the M side, 256 rows over a CTA pair; the ragged rows are the N side in equal
 // tiles of at most 240; a step of the ring is 128 columns of k, one block, so that a
 // step has one exponent per weight block and per routed row.  240 and not 256: two
-// accumulators leave 32 TMEM columns for the exponents of two steps.
+// accumulators leave 32 TMEM columns, of which two groups of four steps' exponents take 24.
 //
 // Exponents.  The instruction wants a word of four bytes for every row, 32 rows to a TMEM
 // column, and takes the byte that its descriptor names: a word is a row's exponents of four

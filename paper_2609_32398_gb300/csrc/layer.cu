@@ -7,7 +7,8 @@ namespace dol {
 namespace {
 
 // Of the two kernels for a few tokens: counters, activations, results; of the grouped products: the
-// dispatch order and what do_expert_ffn takes.
+// dispatch order and what do_expert_ffn takes.  Both begin at 0: the second part's offsets are written after
+// the router has cleared the counters, which nothing reads then.
 struct LayerRoom {
     size_t counters, act, y, offsets, rows, pos, ffn, all;
 };

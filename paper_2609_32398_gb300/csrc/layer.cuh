@@ -1,6 +1,7 @@
-// Internal declarations of the whole MoE layer for a few tokens (layer.cu holds its C ABI):
-// two kernels, the router (layer_route.cu) and the experts with their join
-// (layer_experts.cu).
+// Internal declarations of the whole MoE layer for a few tokens (layer.cu holds its C ABI): the router
+// (layer_route.cu), then the experts with their join, in one kernel for few routed rows (layer_few.cu) or
+// more (layer_experts.cu); or, where bf16 experts have many tokens each, the dispatch order
+// (layer_order.cu) and the grouped products.
 #pragma once
 
 #include "experts8.cuh"

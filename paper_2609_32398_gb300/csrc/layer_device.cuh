@@ -1,15 +1,11 @@
-// What the two kernels of a layer's experts share.
+// What the kernels of a layer for a few tokens share.
 #pragma once
 
+#include "experts_mma.cuh"
 #include "layer.cuh"
-#include "tma.cuh"
 
 namespace dol {
 
-// 16 bytes global -> shared through the L2; zeros where !in (nothing is read then).
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool in) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kBehind>
 __device__ __forceinline__ void wait_copies() {

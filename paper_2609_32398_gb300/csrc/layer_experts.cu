@@ -253,7 +253,7 @@ struct Phase {
             if (c < ((left + 127) & ~127)) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (i < n) copy16(to + i * (kUp ? kRowStride : 2 * kRowStride), w, in);
+                    if (i < n) cp_async16(to + i * (kUp ? kRowStride : 2 * kRowStride), w, in);
                     w += jump;
                 }
             }

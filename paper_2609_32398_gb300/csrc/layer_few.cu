@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1) layer_few_kernel(const LayerArgs 
             const unsigned char *w = static_cast<const unsigned char *>(p.w2) + ((int64_t)expert * p.H + lo + c) * row_bytes;
 #pragma unroll 3
             for (int at = lane * 16; at < room.w_stride; at += 512)
-                copy16(smem_u32(rows + i * room.w_stride + at), at < row_bytes ? w + at : w, at < row_bytes);
+                cp_async16(smem_u32(rows + i * room.w_stride + at), at < row_bytes ? w + at : w, at < row_bytes);
         }
         copies_sent();
     };

@@ -153,11 +153,11 @@ layer_route_kernel(const LayerArgs p) {
             const int n = min(kChunk, pieces - from);
             __syncthreads();  // the chunk before has been read
             if (e < e1)
-                for (int at = lane; at < n; at += 32) copy16(smem_u32(mine + at), wr + (int64_t)e * pieces + from + at, true);
+                for (int at = lane; at < n; at += 32) cp_async16(smem_u32(mine + at), wr + (int64_t)e * pieces + from + at, true);
 #pragma unroll
             for (int t = 0; t < kTokens; ++t)
                 for (int at = threadIdx.x; at < n; at += kThreads)
-                    copy16(smem_u32(rows + t * kChunk + at), x + (int64_t)min(t0 + t, p.T - 1) * pieces + from + at, true);
+                    cp_async16(smem_u32(rows + t * kChunk + at), x + (int64_t)min(t0 + t, p.T - 1) * pieces + from + at, true);
             copies_sent();
             wait_copies<0>();
             __syncthreads();
